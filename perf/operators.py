@@ -1,0 +1,591 @@
+"""The 4-bit key/value cache and the attention that reads it, as measurable cases.
+
+Four kinds of case:
+
+  write    quantise new keys and values into the cache, and read them back as
+           a prompt's own attention wants them (kv4_append, kv4_read)
+  read     gather tokens of the cache back to a float type (kv4_read)
+  attend   attention of new tokens over the cache, all visible tokens
+           (kv4_attention); "sparse": over a list of pages for each token
+  select   score every page by the signs of its keys and list the best
+           (kv4_select)
+
+A cache is a uint8 tensor [pages, kv_heads, 76 * dim]: for one page of 64 tokens of one
+head, dim = 32 * groups channels,
+
+  key codes     32 * dim bytes  [token][dim / 2], channel 2i in the low nibble
+  value codes   32 * dim bytes  [token / 4][16][token % 4][dim / 32], channels in order
+                                 over the third [16] and the last axis
+  key scales     2 * dim bytes  [token % 16][group][token / 16]
+  value scales   2 * dim bytes  [group][token % 16 / 4][token / 16][token % 4]
+  key signs      8 * dim bytes  [token][dim / 8], channel c at bit c % 8
+
+A code is a sign and an e2m1 magnitude, a scale the exponent byte of a power of two.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DEVICE = "cuda"
+PAGE = 64
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def listed():
+    return [
+        # one new token of each of 32 sequences: the write of a decoding step
+        dict(name="write_step", kind="write", tokens=32, kv_heads=8, dim=128, dtype="bf16",
+             fused=False),
+        # the prompts of a batch, keys and values as views of one projection's rows
+        dict(name="write_prompt", kind="write", tokens=12001, kv_heads=8, dim=128, dtype="f16",
+             fused=True),
+        # a short history moved out, small heads
+        dict(name="read_short", kind="read", tokens=777, kv_heads=4, dim=64, dtype="f32"),
+        # a long context read back
+        dict(name="read_long", kind="read", tokens=65536, kv_heads=8, dim=128, dtype="bf16"),
+        # one interactive sequence, one token
+        dict(name="decode_one", kind="attend", seqs=1, longest=20001, queries=1, heads=32,
+             kv_heads=8, dim=128, dtype="bf16", causal=True, window=0, count=0, ragged=1),
+        # a serving batch, one token each, lengths of all kinds
+        dict(name="decode_batch", kind="attend", seqs=64, longest=8192, queries=1, heads=64,
+             kv_heads=8, dim=128, dtype="bf16", causal=True, window=0, count=0, ragged=2),
+        # a few drafted tokens of each sequence checked at once, sliding window
+        dict(name="verify", kind="attend", seqs=16, longest=16000, queries=5, heads=24,
+             kv_heads=4, dim=64, dtype="f16", causal=True, window=4096, count=0, ragged=3),
+        # prompts on top of what the cache already holds
+        dict(name="prompt", kind="attend", seqs=4, longest=6000, queries=1777, heads=32,
+             kv_heads=8, dim=128, dtype="bf16", causal=True, window=0, count=0, ragged=4),
+        # choosing pages for a small batch
+        dict(name="select_step", kind="select", seqs=8, longest=8192, queries=1, heads=32,
+             kv_heads=8, dim=128, dtype="bf16", causal=True, count=32, ragged=5),
+        # choosing pages of long contexts
+        dict(name="select_long", kind="select", seqs=32, longest=32768, queries=1, heads=64,
+             kv_heads=8, dim=128, dtype="f16", causal=True, count=64, ragged=6),
+        # attention over the pages chosen, an ordinary step
+        dict(name="sparse_step", kind="attend", seqs=16, longest=32768, queries=1, heads=32,
+             kv_heads=8, dim=128, dtype="bf16", causal=True, window=0, count=64, ragged=7),
+        # the same with wide heads and two tokens a sequence
+        dict(name="sparse_wide", kind="attend", seqs=40, longest=8000, queries=2, heads=16,
+             kv_heads=2, dim=256, dtype="f16", causal=True, window=0, count=24, ragged=8),
+    ]
+
+
+# ---- drawn cases
+
+# What one drawn case may cost: no more than the largest listed one, in bytes that a
+# pass reads and writes, in operations, and in what the plain form holds at once.
+MOST_BYTES = 4.0e8
+MOST_FLOPS = 1.8e11
+MOST_PLAIN = 2.2e9
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _plain_values(case):
+    """Elements of the plain form's largest tensors: padded keys, scores."""
+    n = case["seqs"] * case["queries"]
+    if case["count"] and case["kind"] == "attend":
+        span, per = case["count"] * PAGE, n
+    else:
+        span, per = case["longest"] + PAGE, case["seqs"]
+    return max(per * span * case["kv_heads"] * case["dim"], n * case["heads"] * span)
+
+
+def draw(rng):
+    kind = rng.choice(("write", "read", "decode", "decode", "prompt", "verify", "select", "sparse"))
+    dtype = rng.choice(("bf16", "bf16", "f16"))
+    dim = rng.choice((64, 128, 128, 256))
+    kv_heads = rng.choice((1, 2, 4, 8, 8))
+    while True:
+        if kind in ("write", "read"):
+            case = dict(kind=kind, tokens=_log(rng, 1, 65536), kv_heads=kv_heads, dim=dim,
+                        dtype=rng.choice(("bf16", "f16", "f32")))
+            if kind == "write":
+                case["fused"] = rng.random() < 0.5
+        else:
+            case = dict(kind="attend" if kind != "select" else kind, seqs=_log(rng, 1, 64),
+                        longest=_log(rng, 40, 100000), queries=1, heads=0, kv_heads=kv_heads,
+                        dim=dim, dtype=dtype, causal=True, window=0, count=0,
+                        ragged=rng.randrange(1 << 20))
+            case["heads"] = kv_heads * rng.choice((1, 2, 4, 4, 5, 8, 8, 16))
+            if kind == "prompt":
+                case.update(seqs=rng.randint(1, 6), queries=_log(rng, 30, 4000),
+                            longest=_log(rng, 60, 12000), causal=rng.random() < 0.8)
+                case["longest"] = max(case["longest"], case["queries"])
+            if kind == "verify":
+                case.update(queries=rng.randint(2, 8), causal=rng.random() < 0.8)
+            if kind in ("prompt", "verify", "decode") and rng.random() < 0.25:
+                case["window"] = _log(rng, 16, 8192)
+            if kind in ("select", "sparse"):
+                case.update(count=_log(rng, 4, 128), queries=rng.choice((1, 1, 1, 2, 3)))
+            if kind == "select":
+                del case["window"]
+            if _plain_values(case) > MOST_PLAIN:
+                continue
+        w = work(case)
+        if w["bytes"] <= MOST_BYTES and w["flops"] <= MOST_FLOPS:
+            return case
+
+
+# ---- sizes: from the case alone
+
+def _lengths(case):
+    """Cached tokens and new tokens of each sequence; the first has the longest."""
+    rng = random.Random(case["ragged"])
+    lengths, queries = [], []
+    for b in range(case["seqs"]):
+        n = case["longest"] if b == 0 else _log(rng, max(1, case["longest"] // 16), case["longest"])
+        q = case["queries"] if b == 0 else rng.randint((case["queries"] + 1) // 2, case["queries"])
+        lengths.append(n)
+        queries.append(min(q, n))
+    return lengths, queries
+
+
+def _pages(n):
+    return -(-n // PAGE)
+
+
+def _visible(case, n, q):
+    """Tokens that the queries of one sequence see: over all, and different ones."""
+    total, low, high = 0, n, 0
+    for i in range(q):
+        p = n - q + i
+        hi = p + 1 if case["causal"] else n
+        lo = max(0, p - case.get("window", 0) + 1) if case.get("window", 0) else 0
+        total += hi - lo
+        low, high = min(low, lo), max(high, hi)
+    return total, high - low
+
+
+def work(case):
+    d, h = case["dim"], case["kv_heads"]
+    held = d + d // 16                        # bytes of a token's codes and scales, one head
+    if case["kind"] in ("write", "read"):
+        size = 4 if case["dtype"] == "f32" else 2
+        n = case["tokens"] * h
+        back = held + 2 * d * size
+        put = 2 * d * size + held + d // 8
+        return {"bytes": n * (back + (put if case["kind"] == "write" else 0)) + 8 * case["tokens"],
+                "flops": 4 * n * d}
+    lengths, queries = _lengths(case)
+    rows = sum(queries) * case["heads"]
+    if case["kind"] == "select":
+        seen = [_visible(case, n, q) for n, q in zip(lengths, queries)]
+        return {"bytes": h * (d // 8) * sum(s[1] for s in seen) + rows * d * 2
+                + 4 * sum(queries) * h * case["count"],
+                "flops": 2 * d * case["heads"] * sum(s[0] for s in seen)}
+    if case["count"]:
+        seen = [min(n, case["count"] * PAGE) * q for n, q in zip(lengths, queries)]
+        keys = sum(min(n, s) for n, s in zip(lengths, seen))
+        return {"bytes": h * held * keys + rows * d * 4, "flops": 4 * d * case["heads"] * sum(seen)}
+    seen = [_visible(case, n, q) for n, q in zip(lengths, queries)]
+    return {"bytes": h * held * sum(s[1] for s in seen) + rows * d * 4,
+            "flops": 4 * d * case["heads"] * sum(s[0] for s in seen)}
+
+
+# ---- inputs
+
+def _generator(seed):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(seed)
+    return g
+
+
+def _keys_values(g, shape, dim):
+    """Keys with a few loud channels, as projections give them, and values."""
+    k = torch.randn(*shape, dim, device=DEVICE, generator=g)
+    k *= torch.where(torch.arange(dim, device=DEVICE) % 37 == 5, 4.0, 1.0)
+    v = torch.randn(*shape, dim, device=DEVICE, generator=g) * 0.7
+    return k, v
+
+
+def _handle(case, cache):
+    """What a program keeps beside the cache's memory: the library's handle on it."""
+    import paper_2011_09398_amd as lce
+    return lce.KV4Cache(case["kv_heads"], case["dim"], data=cache)
+
+
+def _random_pages(g, case, pages):
+    """A cache of `pages` pages of random keys and values."""
+    h, d = case["kv_heads"], case["dim"]
+    cache = torch.empty(pages, h, 76 * d, dtype=torch.uint8, device=DEVICE)
+    step = max(1, (1 << 26) // (PAGE * h * d))
+    for at in range(0, pages, step):
+        n = min(step, pages - at)
+        k, v = _keys_values(g, (n, h, PAGE), d)
+        cache[at:at + n] = _pack(k, v)
+    return cache
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    h, d, dtype = case["kv_heads"], case["dim"], TYPES[case["dtype"]]
+    if case["kind"] in ("write", "read"):
+        n = case["tokens"]
+        pages = _pages(n) + 3
+        order = torch.randperm(pages, device=DEVICE, generator=g)[:_pages(n)]
+        t = torch.arange(n, device=DEVICE)
+        state = dict(case=case, slots=order[t // PAGE] * PAGE + t % PAGE)
+        if case["kind"] == "read":
+            state["cache"] = _random_pages(g, case, pages)
+        else:
+            state["cache"] = torch.zeros(pages, h, 76 * d, dtype=torch.uint8, device=DEVICE)
+            k, v = _keys_values(g, (n, h), d)
+            if case["fused"]:                  # rows of queries, keys and values
+                rows = torch.empty(n, 6 * h, d, dtype=dtype, device=DEVICE)
+                rows[:, 4 * h:5 * h] = k
+                rows[:, 5 * h:] = v
+                state["k"], state["v"] = rows[:, 4 * h:5 * h], rows[:, 5 * h:]
+            else:
+                state["k"], state["v"] = k.to(dtype), v.to(dtype)
+        if own:
+            state["handle"] = _handle(case, state["cache"])
+        return state
+    lengths, queries = _lengths(case)
+    used = [_pages(n) for n in lengths]
+    pages, width = sum(used) + 5, max(used)
+    order = torch.randperm(pages, device=DEVICE, generator=g).to(torch.int32)
+    table = torch.zeros(case["seqs"], width, dtype=torch.int32, device=DEVICE)
+    at = 0
+    for b, n in enumerate(used):
+        table[b, :n] = order[at:at + n]
+        at += n
+    start = [0]
+    for q in queries:
+        start.append(start[-1] + q)
+    total = start[-1]
+    state = dict(case=case, cache=_random_pages(g, case, pages), table=table,
+                 start=torch.tensor(start, dtype=torch.int32, device=DEVICE),
+                 lengths=torch.tensor(lengths, dtype=torch.int32, device=DEVICE),
+                 q=torch.randn(total, case["heads"], d, device=DEVICE, generator=g).to(dtype),
+                 most=max(queries), longest=max(lengths))
+    if case["kind"] == "attend" and case["count"]:
+        # each token's list: its first and last page, and others at random
+        seq, _, _, limit = _places(state)
+        last = (limit - 1) // PAGE
+        score = torch.rand(total, h, width, device=DEVICE, generator=g)
+        page = torch.arange(width, device=DEVICE)
+        score[..., 0] = 2.0
+        score = torch.where(page == last[:, None, None], 3.0, score)
+        score = torch.where(page <= last[:, None, None], score, -1.0)
+        if width < case["count"]:
+            score = torch.nn.functional.pad(score, (0, case["count"] - width), value=-1.0)
+        top, index = torch.topk(score, case["count"], dim=-1)
+        index = torch.where(top >= 0, index, 1 << 30).sort(dim=-1).values
+        state["pages"] = torch.where(index < 1 << 30, index, -1).to(torch.int32).contiguous()
+    if own:
+        import paper_2011_09398_amd as lce
+        state["handle"] = _handle(case, state["cache"])
+        state["workspace"] = lce.kv4_workspace(state["handle"], state["q"], state["table"],
+                                               max_len=state["longest"])
+    return state
+
+
+# ---- plain form
+
+CODES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _pair_table(device):
+    """Byte -> the values of its low and its high nibble."""
+    one = torch.tensor(CODES + tuple(-c for c in CODES), device=device)
+    b = torch.arange(256, device=device)
+    return torch.stack((one[b % 16], one[b // 16]), -1)
+
+
+def _power(byte):
+    """The power of two that an exponent byte stands for."""
+    bits = torch.where(byte == 0, 1 << 22, byte.to(torch.int32) << 23)
+    return torch.where(byte == 255, 0x7FC00000, bits).view(torch.float32)
+
+
+def _quantise(x):
+    """float32 [..., dim] -> codes (0 to 15), exponent bytes [..., dim / 32], finite."""
+    x = x.unflatten(-1, (-1, 32))
+    fine = torch.isfinite(x).all(-1)
+    x = torch.where(fine[..., None], x, 0.0)
+    top = x.abs().amax(-1)
+    byte = (((top.view(torch.int32) >> 23) & 255) - 2).clamp(min=0)
+    y = (x * ((254 - byte) << 23).view(torch.float32)[..., None])
+    a = y.abs()
+    code = ((a > 0.25).byte() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5)
+            + (a > 5.0))
+    code = code + 8 * torch.signbit(y)
+    return code.flatten(-2), torch.where(fine, byte, 255).to(torch.uint8), fine
+
+
+def _quantised(k, v):
+    """Key and value codes and exponent bytes; a token that holds no number has no key."""
+    kc, ks, kf = _quantise(k)
+    vc, vs, vf = _quantise(v)
+    fine = (kf.all(-1) & vf.all(-1))[..., None]
+    return torch.where(fine, kc, 0), torch.where(fine, ks, 255), vc, vs
+
+
+def _bytes(codes):
+    c = codes.to(torch.uint8).unflatten(-1, (-1, 2))
+    return c[..., 0] | (c[..., 1] << 4)
+
+
+def _signs(k):
+    b = (k < 0).unflatten(-1, (-1, 8)).to(torch.uint8)
+    return (b << torch.arange(8, dtype=torch.uint8, device=k.device)).sum(-1, dtype=torch.uint8)
+
+
+def _layout(kb, vb, ks, vs, signs):
+    """Parts [n, h, 64, *] -> records [n, h, 76 dim]."""
+    n, h = kb.shape[:2]
+    d = 2 * kb.shape[-1]
+    return torch.cat((
+        kb.reshape(n, h, -1),
+        vb.reshape(n, h, 16, 4, 16, d // 32).transpose(3, 4).reshape(n, h, -1),
+        ks.reshape(n, h, 4, 16, d // 32).permute(0, 1, 3, 4, 2).reshape(n, h, -1),
+        vs.reshape(n, h, 4, 4, 4, d // 32).permute(0, 1, 5, 3, 2, 4).reshape(n, h, -1),
+        signs.reshape(n, h, -1)), -1)
+
+
+def _pack(k, v):
+    kc, ks, vc, vs = _quantised(k, v)
+    return _layout(_bytes(kc), _bytes(vc), ks, vs, _signs(k))
+
+
+def _offsets(t, d):
+    """Byte offsets in a record of the parts of token t (a tensor) of a page."""
+    dev = t.device
+    t = t[:, None]
+    half, group, eighth = (torch.arange(d // n, device=dev) for n in (2, 32, 8))
+    k = t * (d // 2) + half
+    v = 32 * d + (t // 4) * 2 * d + (half // (d // 32)) * (d // 8) + (t % 4) * (d // 32) \
+        + half % (d // 32)
+    ks = 64 * d + (t % 16) * (d // 8) + group * 4 + t // 16
+    vs = 66 * d + group * 64 + (t % 16 // 4) * 16 + (t // 16) * 4 + t % 4
+    return k, v, ks, vs, 68 * d + t * (d // 8) + eighth
+
+
+def _plain_write(state):
+    cache, slots = state["cache"], state["slots"]
+    k, v = state["k"].float(), state["v"].float()
+    kc, ks, vc, vs = _quantised(k, v)
+    head = torch.arange(cache.shape[1], device=cache.device)[None, :, None]
+    page = (slots // PAGE)[:, None, None]
+    parts = (_bytes(kc), _bytes(vc), ks, vs, _signs(k))
+    at = torch.cat(_offsets(slots % PAGE, k.shape[-1]), -1)[:, None]
+    cache[page, head, at] = torch.cat(parts, -1)
+    return _plain_read(state)
+
+
+def _plain_read(state):
+    cache, slots, dtype = state["cache"], state["slots"], TYPES[state["case"]["dtype"]]
+    head = torch.arange(cache.shape[1], device=cache.device)[None, :, None]
+    page = (slots // PAGE)[:, None, None]
+    k, v, ks, vs, _ = (cache[page, head, at[:, None]]
+                       for at in _offsets(slots % PAGE, state["case"]["dim"]))
+    pair = _pair_table(cache.device)
+    return {n: (pair[c.int()].flatten(-2).unflatten(-1, (-1, 32))
+                * _power(s)[..., None]).flatten(-2).to(dtype) for n, c, s in (("k", k, ks), ("v", v, vs))}
+
+
+def _unpack(rec, d):
+    """Records [..., 76 dim] -> keys, values float32 [..., 64, dim]."""
+    lead = rec.shape[:-1]
+    pair = _pair_table(rec.device)
+    k = pair[rec[..., :32 * d].int()].view(*lead, PAGE, d // 32, 32)
+    v = pair[rec[..., 32 * d:64 * d].int()].view(*lead, 16, 16, 4, d // 16).transpose(-2, -3)
+    ks = _power(rec[..., 64 * d:66 * d]).view(*lead, 16, d // 32, 4).movedim(-1, -3)
+    vs = _power(rec[..., 66 * d:68 * d]).view(*lead, d // 32, 4, 4, 4).movedim(-4, -1)
+    k = k * ks.reshape(*lead, PAGE, d // 32, 1)
+    v = v.reshape(*lead, PAGE, d // 32, 32) * vs.transpose(-3, -4).reshape(*lead, PAGE, d // 32, 1)
+    return k.flatten(-2), v.flatten(-2)
+
+
+def _places(state):
+    """Of each new token: its sequence, its place there, its position, its visible length."""
+    start, lengths = state["start"].long(), state["lengths"].long()
+    token = torch.arange(state["q"].shape[0], device=start.device)
+    seq = torch.bucketize(token, start[1:], right=True)
+    place = token - start[seq]
+    position = lengths[seq] - (start[seq + 1] - start[seq]) + place
+    limit = position + 1 if state["case"]["causal"] else lengths[seq]
+    return seq, place, position, limit
+
+
+def _softmax_product(s, seen, v):
+    """Rows of scores, which of them count, values -> output and log of the sum."""
+    s = torch.where(seen, s, -math.inf)
+    top = s.amax(-1, keepdim=True).clamp(min=-1e30)
+    p = torch.exp(s - top)
+    total = p.sum(-1, keepdim=True)
+    out = torch.matmul(p, v) / torch.where(total == 0, 1.0, total)
+    return out, (top + torch.log(total))[..., 0]
+
+
+def _plain_attend(state):
+    case, q = state["case"], state["q"]
+    h, d = case["kv_heads"], case["dim"]
+    g = case["heads"] // h
+    scale = 1.0 / math.sqrt(d)
+    seq, place, position, limit = _places(state)
+    if case["count"]:
+        pages = state["pages"].long()                            # [T, h, count]
+        phys = state["table"].long()[seq[:, None, None], pages.clamp(min=0)]
+        rec = state["cache"][phys, torch.arange(h, device=q.device)[None, :, None]]
+        k, v = _unpack(rec, d)                                   # [T, h, count, 64, d]
+        j = pages[..., None] * PAGE + torch.arange(PAGE, device=q.device)
+        seen = ((pages >= 0)[..., None] & (j < limit[:, None, None, None])).flatten(2)[:, :, None]
+        s = torch.matmul(q.float().view(-1, h, g, d) * scale,
+                         k.flatten(2, 3).transpose(-1, -2).contiguous())
+        out, lse = _softmax_product(s, seen, v.flatten(2, 3))
+        return {"out": out.flatten(1, 2).to(q.dtype), "lse": lse.flatten(1)}
+    b, most = case["seqs"], state["most"]
+    k, v = _unpack(state["cache"][state["table"].long()].transpose(1, 2), d)
+    k, v = k.flatten(2, 3), v.flatten(2, 3)                      # [b, h, tokens, d]
+    padded = torch.zeros(b, most, case["heads"], d, device=q.device)
+    padded[seq, place] = q.float() * scale
+    rows = padded.view(b, most, h, g, d).transpose(1, 2).reshape(b, h, most * g, d)
+    high = torch.zeros(b, most, dtype=torch.long, device=q.device)
+    high[seq, place] = limit
+    low = torch.zeros_like(high)
+    if case["window"]:
+        low[seq, place] = position - case["window"] + 1
+    j = torch.arange(k.shape[2], device=q.device)
+    seen = (j < high[..., None]) & (j >= low[..., None])         # [b, most, tokens]
+    seen = seen[:, None, :, None].expand(b, 1, most, g, -1).flatten(2, 3)
+    out, lse = _softmax_product(torch.matmul(rows, k.transpose(-1, -2).contiguous()), seen, v)
+    out = out.view(b, h, most, g, d).transpose(1, 2).flatten(2, 3)
+    lse = lse.view(b, h, most, g).transpose(1, 2).flatten(2, 3)
+    return {"out": out[seq, place].to(q.dtype), "lse": lse[seq, place]}
+
+
+def _plain_select(state):
+    case, q = state["case"], state["q"]
+    h, d, count = case["kv_heads"], case["dim"], case["count"]
+    seq, place, _, limit = _places(state)
+    total = (1.0 - 2.0 * (q < 0)).view(-1, h, case["heads"] // h, d).sum(2)   # [T, h, d]
+    rec = state["cache"][:, :, 68 * d:][state["table"].long()]
+    b, width = rec.shape[:2]
+    bit = torch.arange(8, dtype=torch.uint8, device=q.device)
+    sign = 1.0 - 2.0 * ((rec.view(b, width, h, PAGE, d // 8, 1) >> bit) & 1).flatten(-2).float()
+    padded = torch.zeros(b, state["most"], h, d, device=q.device)
+    padded[seq, place] = total
+    s = torch.matmul(sign.permute(0, 2, 1, 3, 4).reshape(b, h, width * PAGE, d),
+                     padded.permute(0, 2, 3, 1).contiguous())    # [b, h, tokens, most]
+    s = s.permute(0, 3, 1, 2)[seq, place].view(-1, h, width, PAGE)
+    page = torch.arange(width, device=q.device)
+    j = page[:, None] * PAGE + torch.arange(PAGE, device=q.device)
+    score = torch.where(j < limit[:, None, None, None], s, -1e9).amax(-1)
+    pages = ((limit + PAGE - 1) // PAGE)[:, None, None]
+    score = torch.where((page < 1) | (page >= pages - 1), 1e9, score)
+    # larger scores first, then lower pages: one whole number for both
+    key = torch.where(page < pages, score.long() * (1 << 20) - page, -(1 << 60))
+    if width < count:
+        key = torch.nn.functional.pad(key, (0, count - width), value=-(1 << 60))
+    top, index = torch.topk(key, count, dim=-1)
+    index = torch.where(top > -(1 << 60), index, 1 << 30).sort(dim=-1).values
+    return {"pages": torch.where(index < 1 << 30, index, -1).to(torch.int32)}
+
+
+# ---- the library
+
+def _own(state):
+    import paper_2011_09398_amd as lce
+    case, cache = state["case"], state["handle"]
+    if case["kind"] == "write":
+        lce.kv4_append(cache, state["k"], state["v"], state["slots"])
+    if case["kind"] in ("write", "read"):
+        k, v = lce.kv4_read(cache, state["slots"], dtype=TYPES[case["dtype"]])
+        return {"k": k, "v": v}
+    if case["kind"] == "select":
+        return {"pages": lce.kv4_select(
+            cache, state["q"], state["table"], state["start"], state["lengths"], case["count"],
+            keep_first=1, keep_last=1, causal=case["causal"], max_len=state["longest"],
+            workspace=state["workspace"])}
+    out, lse = lce.kv4_attention(
+        cache, state["q"], state["table"], state["start"], state["lengths"],
+        causal=case["causal"], window=case["window"], pages=state.get("pages"),
+        max_q=state["most"], max_len=state["longest"], return_lse=True,
+        workspace=state["workspace"])
+    return {"out": out, "lse": lse}
+
+
+def run(state):
+    if own:
+        return _own(state)
+    return {"write": _plain_write, "read": _plain_read, "attend": _plain_attend,
+            "select": _plain_select}[state["case"]["kind"]](state)
+
+
+# ---- 64 bits, from the definitions
+
+def _exact_quantised(x):
+    """The nearest value of the 4-bit format to each of x, in float64."""
+    x = x.double().unflatten(-1, (-1, 32))
+    top = x.abs().amax(-1, keepdim=True)
+    e = torch.frexp(top)[1] - 3                     # floor(log2) - 2
+    e = torch.where(top == 0, -127, e).clamp(min=-127).double()
+    y = x / torch.exp2(e)
+    binade = torch.frexp(y.abs().clamp(min=1.0))[1].double() - 1.0
+    step = torch.exp2(binade - 1.0)                 # one mantissa bit
+    return ((y / step).round() * step).clamp(-6.0, 6.0).mul(torch.exp2(e)).flatten(-2)
+
+
+def _exact_tokens(cache, h, page, t, d):
+    """Keys and values, float64, of tokens (page, t) of head h: one code at a time."""
+    rec = cache[page, h].long()                     # [n, 76 d]
+    c = torch.arange(d, device=cache.device)[None]
+    t = t[:, None]
+
+    def value(byte_at, scale_at):
+        code = (rec.gather(1, byte_at) >> (4 * (c % 2))) & 15
+        m, e = code % 2, code // 2 % 4
+        mag = torch.where(e == 0, 0.5 * m.double(), (1 + 0.5 * m.double()) * torch.exp2(e.double() - 1))
+        mag = torch.where(code >= 8, -mag, mag)
+        return mag * torch.exp2(rec.gather(1, scale_at).double() - 127)
+
+    k = value(t * (d // 2) + c // 2, 64 * d + ((t % 16) * (d // 32) + c // 32) * 4 + t // 16)
+    r, w = c // (d // 16), c % (d // 16)
+    v = value(32 * d + (((t // 4) * 16 + r) * 4 + t % 4) * (d // 32) + w // 2,
+              66 * d + (((c // 32) * 4 + t % 16 // 4) * 4 + t // 16) * 4 + t % 4)
+    return k, v
+
+
+def exact(case, seed):
+    if case["kind"] == "select":                    # whole numbers only
+        return None
+    state = prepare(case, seed)
+    h, d = case["kv_heads"], case["dim"]
+    if case["kind"] == "write":
+        return {"k": _exact_quantised(state["k"]), "v": _exact_quantised(state["v"])}
+    if case["kind"] == "read":
+        s = state["slots"]
+        both = [_exact_tokens(state["cache"], i, s // PAGE, s % PAGE, d) for i in range(h)]
+        return {"k": torch.stack([k for k, _ in both], 1), "v": torch.stack([v for _, v in both], 1)}
+    lengths, queries = _lengths(case)
+    g, q = case["heads"] // h, state["q"].double()
+    out = torch.zeros(q.shape, dtype=torch.float64, device=DEVICE)
+    lse = torch.zeros(q.shape[:2], dtype=torch.float64, device=DEVICE)
+    at = 0
+    for b, (n, nq) in enumerate(zip(lengths, queries)):
+        j = torch.arange(n, device=DEVICE)
+        position = n - nq + torch.arange(nq, device=DEVICE)[:, None]
+        seen = j <= position if case["causal"] else (j < n).expand(nq, n)
+        if case["window"]:
+            seen = seen & (j > position - case["window"])
+        for i in range(h):
+            k, v = _exact_tokens(state["cache"], i, state["table"][b].long()[j // PAGE], j % PAGE, d)
+            mask = seen
+            if case["count"]:
+                mine = state["pages"][at:at + nq, i].long()
+                has = (mine[..., None] == torch.arange(_pages(n), device=DEVICE)).any(1)
+                mask = seen & has[:, j // PAGE]
+            for r in range(i * g, (i + 1) * g):
+                s = (q[at:at + nq, r] @ k.T.contiguous()) / math.sqrt(d)
+                s = torch.where(mask, s, -math.inf)
+                lse[at:at + nq, r] = torch.logsumexp(s, -1)
+                out[at:at + nq, r] = torch.softmax(s, -1) @ v
+        at += nq
+    return {"out": out, "lse": lse}
