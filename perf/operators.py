@@ -281,8 +281,7 @@ def prepare(case, seed):
     if own:
         import paper_2011_09398_amd as lce
         state["handle"] = _handle(case, state["cache"])
-        state["workspace"] = lce.kv4_workspace(state["handle"], state["q"], state["table"],
-                                               max_len=state["longest"])
+        state["workspace"] = lce.kv4_workspace(state["handle"], state["q"], state["table"])
     return state
 
 
