@@ -335,6 +335,161 @@ lce_status lce_bmaxpool2d(const lce_bmaxpool2d_desc *desc, const int32_t *x_pack
 lce_status lce_dequantize(const int32_t *x_packed, float *out, int64_t rows, int32_t channels,
                           hipStream_t stream);
 
+/* ---- 4-bit key/value cache ----------------------------------------------
+ *
+ * The state of a transformer held the way this library holds activations:
+ * quantized as it is written, multiplied in its packed form, and read back on
+ * request.  Keys and values of past tokens are 4-bit floats (e2m1: 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and a sign) that share one power of two per 32 channels, the
+ * format gfx950's matrix cores multiply directly, and every key also leaves
+ * its 1-bit signs (lce_bitpack's: 1 iff x < 0), from which lce_kv4_select
+ * scores pages.
+ *
+ * Quantization of 32 channels x of one token and head:
+ *     e = max(floor(log2(max |x|)) - 2, -127)
+ *     code = x / 2^e rounded to the nearest e2m1 value, ties to the even code,
+ *            |x| / 2^e > 6 to 6;  the value held is code * 2^e
+ * (the shared-scale 4-bit format of the OCP Microscaling specification).  A
+ * group that holds an infinity or a NaN gets codes 0 and the scale NaN (255),
+ * and a token with such a group in its key or its value gets key codes 0 and
+ * key scales NaN: every row that attends to it is NaN, and no other row.
+ *
+ * The cache is one device buffer of pages of LCE_KV4_PAGE = 64 tokens, each
+ * page holding a record of 76*D bytes per head (D = head_dim, G = D/32), with
+ * token t of the page at
+ *     key codes    byte  t*D/2 + c/2                           (channel c, low
+ *     value codes  byte  32*D + ((t/4*16 + r)*4 + t%4)*G + w/2  nibble first;
+ *                        r = c / (D/16), w = c % (D/16))
+ *     key scales   byte  64*D + (t%16*G + c/32)*4 + t/16       (2^(byte-127))
+ *     value scales byte  66*D + (c/32)*64 + t%16/4*16 + t/16*4 + t%4
+ *     key signs    byte  68*D + t*D/8 + c/8, bit c%8
+ * The order of the value codes is that of the matrix cores' operand: a lane
+ * finds D/16 channels of four consecutive tokens in 4*G consecutive bytes.
+ * Tokens are addressed by slot = page*64 + t.  A sequence is a row of page
+ * numbers (its table) and a length; its token j is in slot
+ * table[j/64]*64 + j%64. */
+#define LCE_KV4_PAGE 64
+
+typedef enum { LCE_FLOAT32 = 0, LCE_FLOAT16 = 1, LCE_BFLOAT16 = 2 } lce_float_type;
+
+typedef struct {
+    int32_t pages;       /* pages of the buffer, >= 1                        */
+    int32_t kv_heads;    /* heads of keys and values, >= 1                   */
+    int32_t head_dim;    /* channels of a head: 64, 128 or 256               */
+} lce_kv4_cache_desc;
+
+/* Bytes of the cache buffer of `desc`: pages * kv_heads * 76 * head_dim.  Its
+ * contents need no initialization: slots that were never written may hold
+ * anything as long as no length covers them.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim). */
+lce_status lce_kv4_cache_size(const lce_kv4_cache_desc *desc, int64_t *bytes);
+
+/* Quantize `tokens` keys and values into the cache.
+ *   cache  buffer of lce_kv4_cache_size bytes             (device, 16-byte aligned)
+ *   k, v   [tokens][kv_heads][head_dim] of `type`         (device, 16-byte aligned),
+ *          channels contiguous; token and head strides in elements, each a
+ *          multiple of 16 bytes
+ *   slots  int64 [tokens], where each goes (device, 8-byte aligned); a slot
+ *          outside [0, 64*pages) drops its token.  A slot must not be named
+ *          twice in one call.
+ * tokens == 0 is a no-op (pointers may then be NULL).
+ * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0 or >= 2^31),
+ *         LCE_EUNSUPPORTED (head_dim, kv_heads > 65535), LCE_EALIGN (pointer
+ *         or stride), LCE_EHIP. */
+lce_status lce_kv4_append(const lce_kv4_cache_desc *desc, void *cache, int32_t type,
+                          const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                          const int64_t *slots, int64_t tokens, hipStream_t stream);
+
+/* Read tokens back: k and v [tokens][kv_heads][head_dim] of `type`, contiguous
+ * (device, 16-byte aligned), get the values that the cache holds for `slots`,
+ * zeros for a slot outside the cache.  float32 and bfloat16 hold every value
+ * exactly; float16 rounds to nearest those below 2^-24 and has infinities for
+ * those of 65536 and more.
+ * Errors: as lce_kv4_append. */
+lce_status lce_kv4_read(const lce_kv4_cache_desc *desc, const void *cache, const int64_t *slots,
+                        int64_t tokens, int32_t type, void *k, void *v, hipStream_t stream);
+
+/* New tokens that attend over cached sequences: `tokens` query rows, those of
+ * sequence b at q_start[b] .. q_start[b+1]-1, which are the sequence's last
+ * ones: with n of them, number i stands at position p = lengths[b] - n + i
+ * (the cache already holds their own keys and values). */
+typedef struct {
+    int32_t tokens;        /* query tokens over all sequences, >= 0                    */
+    int32_t q_heads;       /* a multiple of kv_heads; head hq reads cache head
+                              hq / (q_heads / kv_heads)                                */
+    int32_t seqs;          /* sequences, >= 1                                          */
+    int32_t table_width;   /* page numbers per row of the table, >= 1                  */
+    int32_t type;          /* LCE_FLOAT16 or LCE_BFLOAT16: q and out                   */
+    int32_t causal;        /* 1: position p sees tokens j <= p; 0: all of the sequence */
+    int32_t window;        /* > 0: only tokens j > p - window; 0: no such bound        */
+    int32_t list;          /* > 0: page numbers per token and head in `pages`          */
+    int32_t max_q;         /* hints for the split of the work, 0 = unknown: the most   */
+    int32_t max_len;       /* new tokens, the longest length.  Wrong ones cost speed.  */
+    float scale;           /* of the scores, finite and > 0                            */
+    int64_t q_token_stride, q_head_stride;   /* elements, multiples of 8               */
+} lce_kv4_query_desc;
+
+/* Bytes of workspace that every lce_kv4_attention and lce_kv4_select call with
+ * these tokens, q_heads, seqs and table_width can need (the other fields do not
+ * matter).  The workspace is 16-byte aligned device memory whose first
+ * LCE_KV4_WORKSPACE_ZERO bytes are zero before its first use; each call leaves
+ * them zero.  Calls that may run at the same time need one each.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim). */
+#define LCE_KV4_WORKSPACE_ZERO 16384
+lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_query_desc *query,
+                                  int64_t *bytes);
+
+/* Attention of new tokens over the cache: per token and query head
+ *     s_j = scale * (q . k_j) over the visible tokens j,
+ *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)
+ * with k and v as the cache holds them.  Products are exact and sums, the
+ * running maximum and the running sum are float32; softmax weights are rounded
+ * to `type` where they multiply the values, and out is rounded to it once.
+ * A row that sees nothing is 0 with lse -infinity.
+ *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
+ *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a
+ *           length are not read; tokens on a page outside the cache are hidden
+ *   q_start int32 [seqs+1], lengths int32 [seqs] (device); values outside
+ *           [0, tokens] and [0, 64*table_width] are taken as the nearest bound
+ *   pages   with query->list > 0, int32 [tokens][kv_heads][list] (device): only
+ *           tokens j on the pages j/64 named here are visible; numbers that
+ *           are negative or past the length name nothing; naming a page twice
+ *           counts it twice.  Otherwise ignored
+ *   out     [tokens][q_heads][head_dim] of query->type, contiguous (device,
+ *           16-byte aligned); rows of no sequence are left as they are
+ *   lse     float32 [tokens][q_heads] or NULL
+ *   workspace, workspace_bytes: see lce_kv4_workspace_size
+ * A query row that holds an infinity or a NaN gives NaN.  With LCE_FLOAT16,
+ * cached values of 65536 and more count as infinities, as in lce_kv4_read.
+ * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
+ *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
+ *         grid past the device's limits), LCE_EALIGN, LCE_EHIP. */
+lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
+                             const lce_kv4_query_desc *query, const void *q, const int32_t *table,
+                             const int32_t *q_start, const int32_t *lengths, const int32_t *pages,
+                             void *out, float *lse, void *workspace, int64_t workspace_bytes,
+                             hipStream_t stream);
+
+/* Choose query->list pages for each new token and cache head, by the signs of
+ * queries and keys.  A page scores
+ *     max over its visible tokens j of  sum over the query heads g of the
+ *     cache head, and the channels c, of  sgn(q_gc) * sgn(k_jc)
+ * (an XOR and a population count; sgn = -1 iff x < 0).  With n pages up to the
+ * last visible token, the pages below keep_first and those from n - keep_last
+ * on rank before all others; then higher scores, and lower page numbers among
+ * equal ones.  pages int32 [tokens][kv_heads][list] (device) gets the chosen
+ * page numbers in ascending order, then -1.  Pages on which the window leaves
+ * nothing, or that the table names outside the cache, are not chosen.
+ * The other arguments as for lce_kv4_attention.
+ * Errors: as lce_kv4_attention, plus LCE_EINVAL (list < 1, keep < 0) and
+ *         LCE_EUNSUPPORTED (q_heads / kv_heads * head_dim > 65280). */
+lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
+                          const lce_kv4_query_desc *query, const void *q, const int32_t *table,
+                          const int32_t *q_start, const int32_t *lengths, int32_t keep_first,
+                          int32_t keep_last, int32_t *pages, void *workspace,
+                          int64_t workspace_bytes, hipStream_t stream);
+
 /* ---- Schedule overrides, for tests and tuning ----------------------------
  *
  * Every convolution picks its work split by itself.  These process-wide
@@ -367,7 +522,10 @@ typedef enum {
     LCE_TUNE_XOR_STREAM = 11,     /* lce_bconv2d, filter shapes without a specialized XOR
                                      instance: 1 the streaming schedule (where a tile
                                      fits; tile and grid keys as above), -1 the XOR kernel */
-    LCE_TUNE_COUNT = 12
+    LCE_TUNE_KV4_CHUNK = 12,      /* lce_kv4_attention, lce_kv4_select: pages per
+                                     workgroup, >= 1 (raised where the workspace has no
+                                     room for that many workgroups)                     */
+    LCE_TUNE_COUNT = 13
 } lce_tuning_key;
 
 /* Set override `key` to `value` (0 = automatic).

@@ -13,6 +13,15 @@ If the library is not built this module raises; there is no CPU fallback.
     bconv2d_mfma(x_packed, w_fp4, ..) LceBConv2d on the matrix cores (same result)
     bmaxpool2d(x_packed, channels)    LceBMaxPool2d: AND over each window of packed words
     dequantize(x_packed, channels)    LceDequantize: packed bits -> +-1.0 float32
+
+A transformer's key/value cache in 4 bits:
+
+    KV4Cache(kv_heads, head_dim, ..)  the cache's memory: pages of 64 tokens
+    kv4_append(cache, k, v, slots)    quantize keys and values as they are written
+    kv4_read(cache, slots)            read tokens back as floats
+    kv4_attention(cache, q, table, q_start, lengths)  attention over cached sequences
+    kv4_select(cache, q, table, q_start, lengths, n)  the n pages whose key signs fit best
+    kv4_workspace(cache, q, table)    memory that the last two keep between calls
 """
 from __future__ import annotations
 
@@ -37,13 +46,15 @@ EXPORTS = ("lce_packed_words", "lce_bconv2d_out_shape", "lce_bitpack", "lce_bcon
            "lce_fold_thresholds", "lce_bmaxpool2d_out_shape", "lce_bmaxpool2d",
            "lce_dequantize", "lce_bconv2d_mfma_weights_size", "lce_bconv2d_mfma_weights",
            "lce_bconv2d_mfma", "lce_quantize_bconv2d", "lce_quantize_bconv2d_mfma",
+           "lce_kv4_cache_size", "lce_kv4_append", "lce_kv4_read", "lce_kv4_workspace_size",
+           "lce_kv4_attention", "lce_kv4_select",
            "lce_set_tuning", "lce_get_tuning",
            "lce_last_error", "lce_last_schedule")
 
 # lce_tuning_key values, by the names tuning() takes.
 TUNING_KEYS = {"xor_nb": 0, "xor_ks": 1, "mfma_schedule": 2, "mfma_fs_ks": 3, "mfma_fs_s": 4,
                "mfma_fs_wpc": 5, "mfma_fs_pad": 6, "mfma_packed": 7, "mfma_tile_m": 8,
-               "mfma_tile_n": 9, "mfma_fs_window": 10, "xor_stream": 11}
+               "mfma_tile_n": 9, "mfma_fs_window": 10, "xor_stream": 11, "kv4_chunk": 12}
 MFMA_SCHEDULES = {"auto": 0, "fs": 1, "ksplit": 2, "pixel": 3, "stream": 4}
 
 
@@ -58,6 +69,19 @@ class PoolDesc(ctypes.Structure):
     """lce_bmaxpool2d_desc: nine int32 fields, in header order."""
     _fields_ = [(name, ctypes.c_int32) for name in (
         "n", "h", "w", "channels", "kh", "kw", "stride_h", "stride_w", "padding")]
+
+
+class KV4CacheDesc(ctypes.Structure):
+    """lce_kv4_cache_desc: three int32 fields, in header order."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("pages", "kv_heads", "head_dim")]
+
+
+class KV4QueryDesc(ctypes.Structure):
+    """lce_kv4_query_desc: ten int32 fields, a float and two int64, in header order."""
+    _fields_ = [(name, ctypes.c_int32) for name in (
+        "tokens", "q_heads", "seqs", "table_width", "type", "causal", "window", "list", "max_q",
+        "max_len")] + [("scale", ctypes.c_float), ("q_token_stride", ctypes.c_int64),
+                       ("q_head_stride", ctypes.c_int64)]
 
 
 class LceError(RuntimeError):
@@ -111,6 +135,19 @@ def lib() -> ctypes.CDLL:
         L.lce_quantize_bconv2d_mfma.argtypes = [ctypes.POINTER(Desc), vp, vp, vp, vp, vp, vp,
                                                 vp, vp]
         L.lce_quantize_bconv2d_mfma.restype = ctypes.c_int
+        cd, qd = ctypes.POINTER(KV4CacheDesc), ctypes.POINTER(KV4QueryDesc)
+        L.lce_kv4_cache_size.argtypes = [cd, ctypes.POINTER(i64)]
+        L.lce_kv4_cache_size.restype = ctypes.c_int
+        L.lce_kv4_append.argtypes = [cd, vp, i32, vp, i64, i64, vp, i64, i64, vp, i64, vp]
+        L.lce_kv4_append.restype = ctypes.c_int
+        L.lce_kv4_read.argtypes = [cd, vp, vp, i64, i32, vp, vp, vp]
+        L.lce_kv4_read.restype = ctypes.c_int
+        L.lce_kv4_workspace_size.argtypes = [cd, qd, ctypes.POINTER(i64)]
+        L.lce_kv4_workspace_size.restype = ctypes.c_int
+        L.lce_kv4_attention.argtypes = [cd, vp, qd, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.lce_kv4_attention.restype = ctypes.c_int
+        L.lce_kv4_select.argtypes = [cd, vp, qd, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp]
+        L.lce_kv4_select.restype = ctypes.c_int
         L.lce_set_tuning.argtypes = [i32, i32]
         L.lce_set_tuning.restype = ctypes.c_int
         L.lce_get_tuning.argtypes = [i32]
@@ -661,6 +698,239 @@ class PreparedQuantBConv2d:
         st = self._fn(self._desc_ref, *self.args, _current_stream() if stream is None else stream)
         if st != LCE_OK:
             raise LceError(st, last_error())
+
+
+KV4_PAGE = 64
+KV4_WORKSPACE_ZERO = 16384
+FLOAT_TYPE = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
+_float_types = {}      # torch dtype -> lce_float_type, filled at first use
+
+
+def _float_type(dtype, name):
+    code = _float_types.get(dtype)
+    if code is None:
+        code = FLOAT_TYPE.get(str(dtype))
+        if code is None:
+            raise TypeError(f"{name} must be float32, float16 or bfloat16, got {dtype}")
+        _float_types[dtype] = code
+    return code
+
+
+class KV4Cache:
+    """A 4-bit key/value cache: pages of 64 tokens in one device buffer.
+
+    KV4Cache(kv_heads, head_dim, pages=n) allocates uint8 [n, kv_heads,
+    76*head_dim] on `device`; data=t takes an existing buffer of that kind.
+    Tokens are addressed by slot = page*64 + place; which pages make up a
+    sequence is the caller's table.  head_dim is 64, 128 or 256."""
+
+    def __init__(self, kv_heads: int, head_dim: int, pages: Optional[int] = None, *, data=None,
+                 device="cuda"):
+        import torch
+        if (pages is None) == (data is None):
+            raise ValueError("give either pages or data")
+        if data is not None:
+            _require(data, torch.uint8, "data")
+            if data.dim() != 3 or data.shape[1] != kv_heads or data.shape[2] != 76 * head_dim:
+                raise ValueError(f"data must be [pages, {kv_heads}, {76 * head_dim}], got "
+                                 f"{list(data.shape)}")
+            pages = data.shape[0]
+        self.desc = KV4CacheDesc(pages, kv_heads, head_dim)
+        n = ctypes.c_int64()
+        _check(lib().lce_kv4_cache_size(ctypes.byref(self.desc), ctypes.byref(n)))
+        if data is None:
+            data = torch.empty((pages, kv_heads, 76 * head_dim), dtype=torch.uint8, device=device)
+        self.data, self.pages, self.kv_heads, self.head_dim = data, pages, kv_heads, head_dim
+        self._ref = ctypes.byref(self.desc)
+        self._ptr = data.data_ptr()
+
+
+def _require_like(t, dtype, device, name):
+    """An index tensor of a call on `device`."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _require_cache(cache):
+    if not isinstance(cache, KV4Cache):
+        raise TypeError("cache must be a KV4Cache")
+
+
+def _require_heads(t, cache, name):
+    """A [tokens, heads, head_dim] float tensor with contiguous channels."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != cache.data.device:
+        raise ValueError(f"{name} must be on {cache.data.device}, got {t.device}")
+    if t.dim() != 3 or t.shape[2] != cache.head_dim:
+        raise ValueError(f"{name} must be [tokens, heads, {cache.head_dim}], got {list(t.shape)}")
+    if t.stride(2) != 1 and t.numel():
+        raise ValueError(f"{name}'s channels must be contiguous")
+
+
+def kv4_append(cache: KV4Cache, k, v, slots) -> None:
+    """Quantize k and v [tokens, kv_heads, head_dim] (float32, float16 or bfloat16; any
+    token and head strides that are multiples of 16 bytes) into the cache's `slots`
+    (int64 [tokens]; a slot outside the cache drops its token)."""
+    import torch
+    _require_cache(cache)
+    _require_heads(k, cache, "k")
+    _require_heads(v, cache, "v")
+    n = k.shape[0]
+    if k.shape != v.shape or k.shape[1] != cache.kv_heads:
+        raise ValueError(f"k and v must be [tokens, {cache.kv_heads}, {cache.head_dim}], got "
+                         f"{list(k.shape)} and {list(v.shape)}")
+    if k.dtype != v.dtype:
+        raise TypeError(f"k and v must have one dtype, got {k.dtype} and {v.dtype}")
+    _require_like(slots, torch.int64, cache.data.device, "slots")
+    if slots.shape != (n,):
+        raise ValueError(f"slots must have {n} elements")
+    _check(lib().lce_kv4_append(cache._ref, cache._ptr, _float_type(k.dtype, "k"), k.data_ptr(),
+                                k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                                slots.data_ptr(), n, _stream_handle(k)))
+
+
+def kv4_read(cache: KV4Cache, slots, *, dtype=None, out=None):
+    """The values that the cache holds for `slots` (int64 [tokens]): a pair k, v
+    [tokens, kv_heads, head_dim] of `dtype` (default bfloat16), or into the pair
+    `out`.  Slots outside the cache read as zeros."""
+    import torch
+    _require_cache(cache)
+    _require_like(slots, torch.int64, cache.data.device, "slots")
+    if slots.dim() != 1:
+        raise ValueError("slots must have one dimension")
+    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    if out is None:
+        if dtype is None:
+            dtype = torch.bfloat16
+        code = _float_type(dtype, "dtype")
+        k = torch.empty(shape, dtype=dtype, device=slots.device)
+        v = torch.empty(shape, dtype=dtype, device=slots.device)
+    else:
+        k, v = out
+        for t, name in ((k, "out[0]"), (v, "out[1]")):
+            _require_like(t, k.dtype if dtype is None else dtype, slots.device, name)
+            if t.shape != shape:
+                raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        code = _float_type(k.dtype, "out")
+    _check(lib().lce_kv4_read(cache._ref, cache._ptr, slots.data_ptr(), shape[0], code,
+                              k.data_ptr(), v.data_ptr(), _stream_handle(slots)))
+    return k, v
+
+
+def _kv4_query(cache, q, table, q_start, lengths, *, causal, window, count, max_q, max_len, scale):
+    """Checks the arguments that attention and selection share; their descriptor."""
+    import torch
+    _require_cache(cache)
+    _require_heads(q, cache, "q")
+    device = cache.data.device
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences, pages]")
+    seqs, width = table.shape
+    for t, name, shape in ((table, "table", table.shape), (q_start, "q_start", (seqs + 1,)),
+                           (lengths, "lengths", (seqs,))):
+        _require_like(t, torch.int32, device, name)
+        if t.shape != shape:
+            raise ValueError(f"{name} must have {shape[0]} elements, got {list(t.shape)}")
+    if q.dtype == torch.float32:
+        raise TypeError("q must be float16 or bfloat16, got torch.float32")
+    return KV4QueryDesc(q.shape[0], q.shape[1], seqs, width, _float_type(q.dtype, "q"),
+                        1 if causal else 0, window, count, max_q or 0, max_len or 0, scale,
+                        q.stride(0), q.stride(1))
+
+
+def kv4_workspace(cache: KV4Cache, q, table):
+    """Workspace (uint8, zeroed) for kv4_attention and kv4_select calls with q's and
+    table's shapes, or with fewer tokens.  Calls that may overlap need one each."""
+    import torch
+    _require_cache(cache)
+    _require_heads(q, cache, "q")
+    d = KV4QueryDesc(q.shape[0], q.shape[1], table.shape[0], table.shape[1])
+    n = ctypes.c_int64()
+    _check(lib().lce_kv4_workspace_size(cache._ref, ctypes.byref(d), ctypes.byref(n)))
+    ws = torch.empty(n.value, dtype=torch.uint8, device=cache.data.device)
+    ws[:KV4_WORKSPACE_ZERO].zero_()
+    return ws
+
+
+def _workspace(workspace, cache, q, table):
+    import torch
+    if workspace is None:
+        return kv4_workspace(cache, q, table)
+    _require_like(workspace, torch.uint8, cache.data.device, "workspace")
+    return workspace
+
+
+def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optional[float] = None,
+                  causal: bool = True, window: int = 0, pages=None, max_q: Optional[int] = None,
+                  max_len: Optional[int] = None, out=None, return_lse: bool = False,
+                  workspace=None):
+    """Attention of new tokens over cached sequences (lce_kv4_attention).
+
+    q [tokens, q_heads, head_dim], float16 or bfloat16: the tokens of sequence b are rows
+    q_start[b]:q_start[b+1] and stand at its end; table int32 [seqs, pages], lengths int32
+    [seqs] (cached tokens, the new ones included).  window > 0 hides tokens further back;
+    pages int32 [tokens, kv_heads, n] restricts every token and cache head to the pages
+    listed (negative: none).  max_q and max_len, the most new tokens and the longest
+    length, help to split the work.  Returns out, or (out, lse float32 [tokens, q_heads]).
+    """
+    import torch
+    count = 0
+    if pages is not None:
+        _require_like(pages, torch.int32, cache.data.device, "pages")
+        if pages.dim() != 3 or pages.shape[:2] != (q.shape[0], cache.kv_heads) or not pages.shape[2]:
+            raise ValueError(f"pages must be [{q.shape[0]}, {cache.kv_heads}, n], got "
+                             f"{list(pages.shape)}")
+        count = pages.shape[2]
+    d = _kv4_query(cache, q, table, q_start, lengths, causal=causal, window=window, count=count,
+                   max_q=max_q, max_len=max_len,
+                   scale=cache.head_dim ** -0.5 if scale is None else scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    else:
+        _require_like(out, q.dtype, q.device, "out")
+        if out.shape != q.shape:
+            raise ValueError(f"out must be {list(q.shape)}, got {list(out.shape)}")
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
+    ws = _workspace(workspace, cache, q, table)
+    _check(lib().lce_kv4_attention(
+        cache._ref, cache._ptr, ctypes.byref(d), q.data_ptr(), table.data_ptr(),
+        q_start.data_ptr(), lengths.data_ptr(), None if pages is None else pages.data_ptr(),
+        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(),
+        _stream_handle(q)))
+    return (out, lse) if return_lse else out
+
+
+def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_first: int = 1,
+               keep_last: int = 1, causal: bool = True, window: int = 0,
+               max_len: Optional[int] = None, out=None, workspace=None):
+    """The `count` pages of each token and cache head whose key signs agree best with the
+    query signs (lce_kv4_select): int32 [tokens, kv_heads, count], ascending, then -1.
+    The first keep_first and the last keep_last pages are always among them."""
+    import torch
+    d = _kv4_query(cache, q, table, q_start, lengths, causal=causal, window=window, count=count,
+                   max_q=None, max_len=max_len, scale=1.0)
+    shape = (q.shape[0], cache.kv_heads, count)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.int32, device=q.device)
+    else:
+        _require_like(out, torch.int32, q.device, "out")
+        if out.shape != shape:
+            raise ValueError(f"out must be {list(shape)}, got {list(out.shape)}")
+    ws = _workspace(workspace, cache, q, table)
+    _check(lib().lce_kv4_select(
+        cache._ref, cache._ptr, ctypes.byref(d), q.data_ptr(), table.data_ptr(),
+        q_start.data_ptr(), lengths.data_ptr(), keep_first, keep_last, out.data_ptr(),
+        ws.data_ptr(), ws.numel(), _stream_handle(q)))
+    return out
 
 
 class PreparedBitpack:

@@ -1,0 +1,269 @@
+// C ABI of the 4-bit key/value cache (declared in lce.h): host-side checks and
+// the split of the work.  No allocation, no synchronization.
+#include <algorithm>
+#include <cmath>
+
+#include "kv4_launch.hpp"
+#include "status.hpp"
+
+namespace {
+
+using lce::aligned;
+using lce::check_launch;
+using lce::fail;
+using lce::ok;
+using lce::tuning;
+using lce::kv4::kPage;
+
+lce_status validate_cache(const lce_kv4_cache_desc *d) {
+    if (!d) return fail(LCE_EINVAL, "desc is NULL");
+    if (d->pages < 1 || d->kv_heads < 1)
+        return fail(LCE_EINVAL, "pages %d and kv_heads %d must be >= 1", d->pages, d->kv_heads);
+    if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256)
+        return fail(LCE_EUNSUPPORTED, "head_dim %d is not 64, 128 or 256", d->head_dim);
+    if (d->kv_heads > 65535)
+        return fail(LCE_EUNSUPPORTED, "kv_heads %d exceeds 65535", d->kv_heads);
+    return LCE_OK;
+}
+
+lce_status validate_tokens(const lce_kv4_cache_desc *d, int32_t type, int64_t tokens) {
+    if (const lce_status st = validate_cache(d)) return st;
+    if (type != LCE_FLOAT32 && type != LCE_FLOAT16 && type != LCE_BFLOAT16)
+        return fail(LCE_EINVAL, "unknown type %d", type);
+    if (tokens < 0 || tokens > INT32_MAX)
+        return fail(LCE_EINVAL, "tokens %lld outside [0, 2^31)", (long long)tokens);
+    // workgroups of at least 8 tokens of one head
+    if ((tokens / 8 + 1) * d->kv_heads > INT32_MAX)
+        return fail(LCE_EUNSUPPORTED, "%lld tokens of %d heads: too many for one call",
+                    (long long)tokens, d->kv_heads);
+    return LCE_OK;
+}
+
+lce_status validate_query(const lce_kv4_cache_desc *d, const lce_kv4_query_desc *q) {
+    if (const lce_status st = validate_cache(d)) return st;
+    if (!q) return fail(LCE_EINVAL, "query is NULL");
+    if (q->tokens < 0 || q->seqs < 1 || q->table_width < 1)
+        return fail(LCE_EINVAL, "tokens %d must be >= 0, seqs %d and table_width %d >= 1",
+                    q->tokens, q->seqs, q->table_width);
+    if (q->q_heads < 1 || q->q_heads % d->kv_heads)
+        return fail(LCE_EINVAL, "q_heads %d is not a multiple of kv_heads %d", q->q_heads,
+                    d->kv_heads);
+    if (q->table_width > INT32_MAX / kPage)
+        return fail(LCE_EUNSUPPORTED, "table_width %d: sequences of 2^31 tokens or more",
+                    q->table_width);
+    // rows and workgroups are counted in 32 bits
+    if (((int64_t)q->tokens + q->seqs) * q->q_heads > INT32_MAX)
+        return fail(LCE_EUNSUPPORTED, "%d tokens of %d heads in %d sequences: too many for one call",
+                    q->tokens, q->q_heads, q->seqs);
+    return LCE_OK;
+}
+
+lce_status validate_call(const lce_kv4_cache_desc *d, const lce_kv4_query_desc *q) {
+    if (const lce_status st = validate_query(d, q)) return st;
+    if (q->type != LCE_FLOAT16 && q->type != LCE_BFLOAT16)
+        return fail(q->type == LCE_FLOAT32 ? LCE_EUNSUPPORTED : LCE_EINVAL,
+                    "query type %d is not float16 or bfloat16", q->type);
+    if (q->causal != 0 && q->causal != 1) return fail(LCE_EINVAL, "causal %d is not 0 or 1", q->causal);
+    if (q->window < 0 || q->list < 0 || q->max_q < 0 || q->max_len < 0)
+        return fail(LCE_EINVAL, "window %d, list %d, max_q %d and max_len %d must be >= 0",
+                    q->window, q->list, q->max_q, q->max_len);
+    return LCE_OK;
+}
+
+// What the workspace has room for: states of this many tiles of 16 rows.  More
+// workgroups than this would not run at the same time anyway.
+constexpr int64_t kMostParts = 4096;
+
+int64_t tiles16(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q, bool list) {
+    const int64_t group = q.q_heads / d.kv_heads;
+    return list ? q.tokens * ((group + 15) / 16) : q.tokens * group / 16 + q.seqs;
+}
+
+// Pages that a unit of work can have before it, as far as the call says.
+int64_t most_pages(const lce_kv4_query_desc &q) {
+    int64_t n = q.table_width;
+    if (q.max_len > 0) n = std::min<int64_t>(n, (q.max_len + (int64_t)kPage - 1) / kPage);
+    if (q.window > 0) n = std::min<int64_t>(n, ((int64_t)q.window + std::max(q.max_q, 1)) / kPage + 2);
+    return n;
+}
+
+struct Split {
+    int chunk;    // pages per workgroup
+    int splits;   // workgroups that share a unit, at most
+};
+
+// Divides `pages` pages of each of `units` units of work so that about `target`
+// workgroups run, of at least `least` pages each.
+Split split_pages(int64_t units, int64_t pages, int64_t target, int64_t least) {
+    const int64_t room = std::max<int64_t>(kMostParts / std::max<int64_t>(units, 1), 1);
+    int64_t z = std::min(std::max<int64_t>(target / std::max<int64_t>(units, 1), 1), room);
+    int64_t chunk = std::max((pages + z - 1) / z, least);
+    if (const int t = tuning(LCE_TUNE_KV4_CHUNK))
+        chunk = std::max<int64_t>(t > 0 ? t : 1, (pages + room - 1) / room);
+    Split s;
+    s.chunk = (int)chunk;
+    s.splits = (int)((pages + chunk - 1) / chunk);
+    return s;
+}
+
+void fill_query(lce::kv4::QueryParams &p, const lce_kv4_cache_desc &d, const void *cache,
+                const lce_kv4_query_desc &q, const void *qp, const int32_t *table,
+                const int32_t *q_start, const int32_t *lengths, const Split &s, void *workspace) {
+    p.cache = static_cast<const uint8_t *>(cache);
+    p.q = qp;
+    p.table = table, p.q_start = q_start, p.lengths = lengths;
+    p.q_token = q.q_token_stride, p.q_head = q.q_head_stride;
+    p.pages = d.pages, p.kv_heads = d.kv_heads, p.group = q.q_heads / d.kv_heads;
+    p.tokens = q.tokens, p.seqs = q.seqs, p.width = q.table_width;
+    p.causal = q.causal, p.window = q.window, p.list = q.list;
+    p.chunk = s.chunk;
+    p.tickets = static_cast<int32_t *>(workspace);
+}
+
+}  // namespace
+
+extern "C" {
+
+lce_status lce_kv4_cache_size(const lce_kv4_cache_desc *desc, int64_t *bytes) {
+    if (!bytes) return fail(LCE_EINVAL, "bytes output pointer is NULL");
+    if (const lce_status st = validate_cache(desc)) return st;
+    *bytes = (int64_t)desc->pages * desc->kv_heads * 76 * desc->head_dim;
+    return ok();
+}
+
+lce_status lce_kv4_append(const lce_kv4_cache_desc *desc, void *cache, int32_t type,
+                          const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                          const int64_t *slots, int64_t tokens, hipStream_t stream) {
+    if (const lce_status st = validate_tokens(desc, type, tokens)) return st;
+    if (tokens == 0) return ok();
+    if (!cache || !k || !v || !slots) return fail(LCE_EINVAL, "cache/k/v/slots is NULL");
+    if (!aligned(cache, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8))
+        return fail(LCE_EALIGN, "cache, k and v must be 16-byte aligned, slots 8-byte");
+    const int64_t unit = type == LCE_FLOAT32 ? 4 : 8;
+    if (k_token_stride % unit || k_head_stride % unit || v_token_stride % unit ||
+        v_head_stride % unit)
+        return fail(LCE_EALIGN, "strides must be multiples of 16 bytes (%lld elements)",
+                    (long long)unit);
+    lce::kv4::AppendParams p;
+    p.cache = static_cast<uint8_t *>(cache);
+    p.k = k, p.v = v, p.slots = slots, p.tokens = tokens;
+    p.k_token = k_token_stride, p.k_head = k_head_stride;
+    p.v_token = v_token_stride, p.v_head = v_head_stride;
+    p.pages = desc->pages, p.kv_heads = desc->kv_heads;
+    lce::kv4::launch_append(p, type, desc->head_dim, stream);
+    return check_launch("lce_kv4_append launch");
+}
+
+lce_status lce_kv4_read(const lce_kv4_cache_desc *desc, const void *cache, const int64_t *slots,
+                        int64_t tokens, int32_t type, void *k, void *v, hipStream_t stream) {
+    if (const lce_status st = validate_tokens(desc, type, tokens)) return st;
+    if (tokens == 0) return ok();
+    if (!cache || !k || !v || !slots) return fail(LCE_EINVAL, "cache/k/v/slots is NULL");
+    if (!aligned(cache, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8))
+        return fail(LCE_EALIGN, "cache, k and v must be 16-byte aligned, slots 8-byte");
+    lce::kv4::ReadParams p;
+    p.cache = static_cast<const uint8_t *>(cache);
+    p.slots = slots, p.k = k, p.v = v, p.tokens = tokens;
+    p.pages = desc->pages, p.kv_heads = desc->kv_heads;
+    lce::kv4::launch_read(p, type, desc->head_dim, stream);
+    return check_launch("lce_kv4_read launch");
+}
+
+lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_query_desc *query,
+                                  int64_t *bytes) {
+    if (!bytes) return fail(LCE_EINVAL, "bytes output pointer is NULL");
+    if (const lce_status st = validate_query(desc, query)) return st;
+    const int64_t heads = desc->kv_heads, width = query->table_width;
+    const int64_t units = std::max(tiles16(*desc, *query, false), tiles16(*desc, *query, true)) *
+                          heads;
+    // a list may be longer than the table, so its splits are bounded by the room
+    const int64_t parts = kMostParts * 16 * (desc->head_dim + 2) * 4;
+    const int64_t ranks = query->tokens * heads * width * 2;
+    *bytes = LCE_KV4_WORKSPACE_ZERO + std::max(units ? parts : 0, ranks);
+    return ok();
+}
+
+lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
+                             const lce_kv4_query_desc *query, const void *q, const int32_t *table,
+                             const int32_t *q_start, const int32_t *lengths, const int32_t *pages,
+                             void *out, float *lse, void *workspace, int64_t workspace_bytes,
+                             hipStream_t stream) {
+    if (const lce_status st = validate_call(desc, query)) return st;
+    if (!(query->scale > 0.0f) || !std::isfinite(query->scale))
+        return fail(LCE_EINVAL, "scale %g is not a finite number > 0", query->scale);
+    if (query->tokens == 0) return ok();
+    if (!cache || !q || !table || !q_start || !lengths || !out || !workspace)
+        return fail(LCE_EINVAL, "cache/q/table/q_start/lengths/out/workspace is NULL");
+    if (query->list > 0 && !pages) return fail(LCE_EINVAL, "list %d needs pages", query->list);
+    if (!aligned(cache, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16))
+        return fail(LCE_EALIGN, "cache, q, out and workspace must be 16-byte aligned");
+    if (!aligned(table, 4) || !aligned(q_start, 4) || !aligned(lengths, 4) || !aligned(pages, 4) ||
+        !aligned(lse, 4))
+        return fail(LCE_EALIGN, "table, q_start, lengths, pages and lse must be 4-byte aligned");
+    if (query->q_token_stride % 8 || query->q_head_stride % 8)
+        return fail(LCE_EALIGN, "q strides must be multiples of 8 elements");
+    int64_t need = 0;
+    if (const lce_status st = lce_kv4_workspace_size(desc, query, &need)) return st;
+    if (workspace_bytes < need)
+        return fail(LCE_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
+                    (long long)need);
+
+    const bool list = query->list > 0;
+    const int64_t units = tiles16(*desc, *query, list) * desc->kv_heads;
+    const Split s = split_pages(units, list ? query->list : most_pages(*query), 1024, 4);
+    lce::kv4::AttendParams p;
+    fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
+    p.named = list ? pages : nullptr;
+    p.out = out;
+    p.lse = lse;
+    p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + LCE_KV4_WORKSPACE_ZERO);
+    p.scale_log2 = query->scale * 1.44269504088896341f;
+    lce::kv4::launch_attend16(p, query->type, desc->head_dim,
+                              dim3((unsigned)units, (unsigned)s.splits), stream);
+    return check_launch("lce_kv4_attention launch");
+}
+
+lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
+                          const lce_kv4_query_desc *query, const void *q, const int32_t *table,
+                          const int32_t *q_start, const int32_t *lengths, int32_t keep_first,
+                          int32_t keep_last, int32_t *pages, void *workspace,
+                          int64_t workspace_bytes, hipStream_t stream) {
+    if (const lce_status st = validate_call(desc, query)) return st;
+    if (query->list < 1 || keep_first < 0 || keep_last < 0)
+        return fail(LCE_EINVAL, "list %d must be >= 1, keep_first %d and keep_last %d >= 0",
+                    query->list, keep_first, keep_last);
+    if ((int64_t)query->q_heads / desc->kv_heads * desc->head_dim > 65280)
+        return fail(LCE_EUNSUPPORTED, "%d query heads of %d channels a cache head: past 65280",
+                    query->q_heads / desc->kv_heads, desc->head_dim);
+    if (query->tokens == 0) return ok();
+    if (!cache || !q || !table || !q_start || !lengths || !pages || !workspace)
+        return fail(LCE_EINVAL, "cache/q/table/q_start/lengths/pages/workspace is NULL");
+    if (!aligned(cache, 16) || !aligned(q, 16) || !aligned(workspace, 16))
+        return fail(LCE_EALIGN, "cache, q and workspace must be 16-byte aligned");
+    if (!aligned(table, 4) || !aligned(q_start, 4) || !aligned(lengths, 4) || !aligned(pages, 4))
+        return fail(LCE_EALIGN, "table, q_start, lengths and pages must be 4-byte aligned");
+    if (query->q_token_stride % 8 || query->q_head_stride % 8)
+        return fail(LCE_EALIGN, "q strides must be multiples of 8 elements");
+    int64_t need = 0;
+    if (const lce_status st = lce_kv4_workspace_size(desc, query, &need)) return st;
+    if (workspace_bytes < need)
+        return fail(LCE_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
+                    (long long)need);
+
+    const int64_t units = (int64_t)query->tokens * desc->kv_heads;
+    // a window hides pages but does not renumber them: all up to the last count
+    lce_kv4_query_desc all = *query;
+    all.window = 0;
+    const Split s = split_pages(units, most_pages(all), 1024, 8);
+    lce::kv4::SelectParams p;
+    fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
+    p.keep_first = keep_first, p.keep_last = keep_last;
+    p.chosen = pages;
+    p.ranks = reinterpret_cast<uint16_t *>(static_cast<char *>(workspace) + LCE_KV4_WORKSPACE_ZERO);
+    lce::kv4::launch_select(p, query->type, desc->head_dim,
+                            dim3((unsigned)units, (unsigned)s.splits), stream);
+    return check_launch("lce_kv4_select launch");
+}
+
+}  // extern "C"

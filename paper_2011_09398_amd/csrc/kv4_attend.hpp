@@ -1,0 +1,88 @@
+// What the attention kernels over the 4-bit cache share: query operands,
+// element types, and the joining of a row's splits.
+#pragma once
+
+#include "kv4_launch.hpp"
+
+namespace lce {
+namespace kv4 {
+
+// Element type of queries, softmax weights and outputs, and its products.
+struct Bf16 {
+    typedef __bf16 T;
+    typedef bf16x2 T2;
+    typedef bf16x8 T8;
+    // pieces of 4 significant bits (and a sign each) that hold any bfloat16
+    static constexpr int kPieces = 2;
+    // the largest scale byte a finite value can have, for tokens that a row
+    // does not see (their weight is 0, and 0 times what the bytes decode to has
+    // to be 0): 6 * 2^125 is finite in bfloat16
+    static constexpr uint32_t kMaxScale = 252;
+    static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
+    }
+};
+
+struct F16 {
+    typedef _Float16 T;
+    typedef f16x2 T2;
+    typedef f16x8 T8;
+    static constexpr int kPieces = 3;
+    static constexpr uint32_t kMaxScale = 140;   // 6 * 2^13 is finite in float16
+    static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
+    }
+};
+
+// Two codes (byte BYTE of c) as a packed pair of E::T, times a power of two.
+template <typename E, int BYTE>
+__device__ __forceinline__ uint32_t decode_pair(uint32_t c, float s) {
+    if constexpr (__is_same(typename E::T, __bf16))
+        return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, BYTE));
+    else
+        return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, BYTE));
+}
+
+template <typename E>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+    typename E::T2 v = {(typename E::T)a, (typename E::T)b};
+    return bits_as<uint32_t>(v);
+}
+
+// A row's scale and the next piece of its values: a query row is multiplied in
+// 8-bit floats (e4m3) against the 4-bit keys.  With E = floor(log2 max|q|) the
+// first piece is q * 2^(7-E) rounded to 4 significant bits, the next ones what
+// is left, times 16 each: two hold a bfloat16's 8 bits exactly, three a
+// float16's 11 (of a row's small values, to 2^-21 and 2^-25 of its largest).
+// The matrix cores multiply the pieces' products by the pieces' scales and the
+// key groups' own, so that every product is exact.
+struct RowScale {
+    float up;         // 2^(7-E)
+    uint32_t byte;    // biased exponent of 2^(E-7); 255 (NaN) for a row that is not finite
+};
+
+__device__ __forceinline__ RowScale row_scale(float top) {
+    const uint32_t t = bits_as<uint32_t>(top);
+    RowScale r;
+    // rows below 2^-100 are scaled as if they reached it
+    const int e = max((int)(t >> 23), 27);   // biased E
+    r.up = bits_as<float>((uint32_t)(254 + 7 - e) << 23);
+    r.byte = t >= 0x7F800000u ? 255u : (uint32_t)(e - 7);
+    return r;
+}
+
+// Four values -> four e4m3 bytes, and what the rounding left of them, times 16.
+__device__ __forceinline__ uint32_t next_piece(float (&x)[4]) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+    const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    x[0] = (x[0] - lo[0]) * 16.0f;
+    x[1] = (x[1] - lo[1]) * 16.0f;
+    x[2] = (x[2] - hi[0]) * 16.0f;
+    x[3] = (x[3] - hi[1]) * 16.0f;
+    return (uint32_t)w;
+}
+
+}  // namespace kv4
+}  // namespace lce

@@ -7,13 +7,11 @@
 #include <atomic>
 #include <climits>
 #include <cmath>
-#include <cstdarg>
 #include <cstdlib>
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
 #include <numeric>
-#include <string>
 
 #include "lce.h"
 #include "bitpack.hpp"
@@ -21,6 +19,7 @@
 #include "pool.hpp"
 #include "bconv_mfma.hpp"
 #include "launch.hpp"
+#include "status.hpp"
 
 // Kernels that run once per filter tensor (not on the timed path).
 namespace lce {
@@ -96,31 +95,13 @@ __global__ __launch_bounds__(256) void mfma_expand_weights_kernel(const uint32_t
 
 namespace {
 
-thread_local std::string g_last_error;
 thread_local const char *g_last_schedule = "";   // of the last convolution launched
 
-lce_status fail(lce_status st, const char *fmt, ...) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    g_last_error = buf;
-    return st;
-}
-
-lce_status ok() {
-    g_last_error.clear();
-    return LCE_OK;
-}
-
-lce_status check_launch(const char *what) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return fail(LCE_EHIP, "%s: %s", what, hipGetErrorString(e));
-    return ok();
-}
-
-bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+using lce::aligned;
+using lce::check_launch;
+using lce::fail;
+using lce::ok;
+using lce::tuning;
 
 int packed_words(int channels) { return (channels + 31) / 32; }
 
@@ -361,14 +342,6 @@ void dispatch(const BconvParams &p, dim3 grid, hipStream_t s, int vec, bool padz
     else
         dispatch<OUT, false>(p, grid, s, vec);
 }
-
-// Schedule overrides (lce_set_tuning): 0 = the library's own choice.  Each
-// launch reads every value it uses once, with a relaxed atomic load, so a
-// concurrent lce_set_tuning is never a data race (a launch sees the old or
-// the new value).
-std::atomic<int32_t> g_tuning[LCE_TUNE_COUNT];
-
-int tuning(lce_tuning_key key) { return g_tuning[key].load(std::memory_order_relaxed); }
 
 // A device attribute, cached per device.  The cache entries are atomics: two
 // threads making their first launch together both query the attribute and
@@ -1894,16 +1867,16 @@ lce_status lce_quantize_bconv2d_mfma(const lce_bconv2d_desc *desc, const float *
 
 lce_status lce_set_tuning(int32_t key, int32_t value) {
     if (key < 0 || key >= LCE_TUNE_COUNT) return fail(LCE_EINVAL, "unknown tuning key %d", key);
-    g_tuning[key].store(value, std::memory_order_relaxed);
+    lce::g_tuning[key].store(value, std::memory_order_relaxed);
     return ok();
 }
 
 int32_t lce_get_tuning(int32_t key) {
     if (key < 0 || key >= LCE_TUNE_COUNT) return 0;
-    return g_tuning[key].load(std::memory_order_relaxed);
+    return lce::g_tuning[key].load(std::memory_order_relaxed);
 }
 
-const char *lce_last_error(void) { return g_last_error.c_str(); }
+const char *lce_last_error(void) { return lce::last_error_text(); }
 
 const char *lce_last_schedule(void) { return g_last_schedule; }
 
