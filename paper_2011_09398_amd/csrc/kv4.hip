@@ -3,7 +3,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kv4_launch.hpp"
+#include "kv4_attend.hpp"
 #include "status.hpp"
 
 namespace {
@@ -95,7 +95,8 @@ struct Split {
 // Divides `pages` pages of each of `units` units of work so that about `target`
 // workgroups run, of at least `least` pages each.
 Split split_pages(int64_t units, int64_t pages, int64_t target, int64_t least) {
-    const int64_t room = std::max<int64_t>(kMostParts / std::max<int64_t>(units, 1), 1);
+    const int64_t room = std::min<int64_t>(
+        std::max<int64_t>(kMostParts / std::max<int64_t>(units, 1), 1), lce::kv4::kMostSplits);
     int64_t z = std::min(std::max<int64_t>(target / std::max<int64_t>(units, 1), 1), room);
     int64_t chunk = std::max((pages + z - 1) / z, least);
     if (const int t = tuning(LCE_TUNE_KV4_CHUNK))

@@ -77,21 +77,26 @@ __device__ __forceinline__ Sequence find_sequence(const int32_t *q_start, const 
                                                   int seqs, int tokens, int width, int64_t item,
                                                   First first) {
     const int lane = threadIdx.x & 63;
-    int found = -1;
+    Sequence s;
+    s.index = -1;
+    s.start = s.queries = s.length = 0;
     for (int base = 0; base < seqs; base += 64) {
-        const int b = base + lane;
-        const bool at = b < seqs && first(clampi(q_start[min(b, seqs - 1)], 0, tokens), b) <= item;
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(at);
-        found += __builtin_popcountll(mask);
+        // everything a sequence has, one a lane, in one round trip to memory
+        const int b = min(base + lane, seqs - 1);
+        const int start = clampi(q_start[b], 0, tokens), end = clampi(q_start[b + 1], 0, tokens);
+        const int length = lengths[b];
+        const uint64_t mask =
+            __builtin_amdgcn_ballot_w64(base + lane < seqs && first(start, b) <= item);
+        if (mask) {
+            const int at = 63 - __builtin_clzll(mask);
+            s.index = base + at;
+            s.start = __builtin_amdgcn_readlane(start, at);
+            s.queries = max(__builtin_amdgcn_readlane(end, at) - s.start, 0);
+            s.length = (int)min(max((int64_t)__builtin_amdgcn_readlane(length, at), (int64_t)0),
+                                (int64_t)kPage * width);
+        }
         if (mask != ~0ull) break;
     }
-    Sequence s;
-    s.index = __builtin_amdgcn_readfirstlane(found);
-    s.start = s.queries = s.length = 0;
-    if (s.index < 0) return s;
-    s.start = clampi(q_start[s.index], 0, tokens);
-    s.queries = max(clampi(q_start[s.index + 1], 0, tokens) - s.start, 0);
-    s.length = (int)min(max((int64_t)lengths[s.index], (int64_t)0), (int64_t)kPage * width);
     return s;
 }
 

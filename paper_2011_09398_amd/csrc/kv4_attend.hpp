@@ -84,5 +84,43 @@ __device__ __forceinline__ uint32_t next_piece(float (&x)[4]) {
     return (uint32_t)w;
 }
 
+// What workgroups on different XCDs tell each other within a launch goes through
+// relaxed atomics of device scope: written through and read past the caches that
+// are not coherent, so that neither side has to write back or invalidate a whole
+// L2 (a release fence per workgroup measured 64 ns of the launch each, one after
+// the other: 160 us for 2500 of them, against 18).  What remains of the order is
+// that the stores are done before the ticket is drawn.
+__device__ __forceinline__ void put(float *p, float a, float b) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), bits_as<uint64_t>(f32x2{a, b}),
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ f32x2 get(const float *p) {
+    return bits_as<f32x2>(__hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// Draws a ticket after this wave's stores; true for the last of `all`, which
+// also puts the count back to 0 for the next call.
+__device__ __forceinline__ bool last_of(int32_t *ticket, int all) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const int32_t before =
+        __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before != all - 1) return false;
+    __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
+constexpr int kMostSplits = 256;   // of one unit: what joining them has LDS for
+
+// States of a tile's splits in the workspace, kRows rows each: (m, l) per row,
+// then the sums of weighted values.
+template <int D, int ROWS>
+struct Part {
+    static constexpr int kFloats = ROWS * (D + 2);
+    static __device__ __forceinline__ int state(int row) { return 2 * row; }
+    static __device__ __forceinline__ int sums(int row) { return 2 * ROWS + row * D; }
+};
+
 }  // namespace kv4
 }  // namespace lce

@@ -15,56 +15,61 @@ constexpr int kRows = 16;
 // and the value codes of tokens 16t + 4g + i for the D/16 channels from
 // D/16 * n on.
 template <int D>
-struct PageRegs {
+struct Keys {
     static constexpr int kChunks = D < 128 ? 1 : D / 128;
     u32x4 k[4][kChunks];
-    uint32_t v[4][D / 32];
-    uint32_t ks[kChunks];   // byte t: scale of tokens 16t + n
-    u32x4 vs;               // byte i of word t: scale of token 16t + 4g + i
+    uint32_t scale[kChunks];   // byte t: scale of tokens 16t + n
+
+    __device__ __forceinline__ void load(const uint8_t *rec, int n, int g) {
+        // a head of 64 channels fills half of the product's 128: the other half
+        // repeats them, against another piece of the queries
+        const int kg = D < 128 ? g % 2 : g;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+                k[t][c] = *reinterpret_cast<const u32x4 *>(rec + (16 * t + n) * (D / 2) + 64 * c +
+                                                           16 * kg);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+            scale[c] = *reinterpret_cast<const uint32_t *>(rec + Record<D>::kKeyScale +
+                                                           (n * (D / 32) + 4 * c + kg) * 4);
+    }
 };
 
 template <int D>
-__device__ __forceinline__ void load_page(PageRegs<D> &r, const uint8_t *rec, int n, int g) {
-    typedef PageRegs<D> P;
-    // a head of 64 channels fills half of the product's 128: the other half
-    // repeats them, against another piece of the queries
-    const int kg = D < 128 ? g % 2 : g;
+struct Values {
+    uint32_t v[4][D / 32];
+    u32x4 scale;               // byte i of word t: scale of token 16t + 4g + i
+
+    __device__ __forceinline__ void load(const uint8_t *rec, int n, int g) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+            const uint8_t *at = rec + Record<D>::kValue + ((4 * t + g) * 16 + n) * (D / 8);
+            if constexpr (D == 64) {
+                const u32x2 w = *reinterpret_cast<const u32x2 *>(at);
+                v[t][0] = w[0], v[t][1] = w[1];
+            } else {
 #pragma unroll
-        for (int c = 0; c < P::kChunks; ++c)
-            r.k[t][c] = *reinterpret_cast<const u32x4 *>(rec + (16 * t + n) * (D / 2) + 64 * c +
-                                                         16 * kg);
+                for (int j = 0; j < D / 128; ++j) {
+                    const u32x4 w = reinterpret_cast<const u32x4 *>(at)[j];
 #pragma unroll
-    for (int c = 0; c < P::kChunks; ++c)
-        r.ks[c] = *reinterpret_cast<const uint32_t *>(rec + Record<D>::kKeyScale +
-                                                      (n * (D / 32) + 4 * c + kg) * 4);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const uint8_t *at = rec + Record<D>::kValue + ((4 * t + g) * 16 + n) * (D / 8);
-        if constexpr (D == 64) {
-            const u32x2 w = *reinterpret_cast<const u32x2 *>(at);
-            r.v[t][0] = w[0], r.v[t][1] = w[1];
-        } else {
-#pragma unroll
-            for (int j = 0; j < D / 128; ++j) {
-                const u32x4 w = reinterpret_cast<const u32x4 *>(at)[j];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) r.v[t][4 * j + i] = w[i];
+                    for (int i = 0; i < 4; ++i) v[t][4 * j + i] = w[i];
+                }
             }
         }
+        // channels D/16 * n lie in group n * D / 512
+        scale = *reinterpret_cast<const u32x4 *>(rec + Record<D>::kValueScale +
+                                                 (n * D / 512) * 64 + 16 * g);
     }
-    // channels D/16 * n lie in group n * D / 512
-    r.vs = *reinterpret_cast<const u32x4 *>(rec + Record<D>::kValueScale + (n * D / 512) * 64 +
-                                            16 * g);
-}
+};
 
 // Queries of 16 rows as second operands: lane (n, g) holds, of row n, channels
 // 16g .. +15 and 64 + 16g .. +15 of each 128 (the order of an 8-bit operand),
 // in pieces.
 template <typename E, int D>
 struct Queries {
-    static constexpr int kChunks = PageRegs<D>::kChunks;
+    static constexpr int kChunks = Keys<D>::kChunks;
     // products per 128 channels (per head where D = 64: there one product takes
     // two pieces, in its two halves)
     static constexpr int kSteps = D < 128 ? (E::kPieces + 1) / 2 : E::kPieces;
@@ -75,7 +80,7 @@ struct Queries {
 template <typename E, int D>
 __device__ __forceinline__ void load_queries(Queries<E, D> &q, const typename E::T *row, bool valid,
                                              int g) {
-    constexpr int kChunks = PageRegs<D>::kChunks, kHalves = D < 128 ? 1 : 2;
+    constexpr int kChunks = Keys<D>::kChunks, kHalves = D < 128 ? 1 : 2;
     float x[kChunks][kHalves][16];
     float top = 0.0f;
     bool odd = false;
@@ -144,16 +149,16 @@ __device__ __forceinline__ void load_queries(Queries<E, D> &q, const typename E:
 
 // Scores of a page: s[t][i] of lane (n, g) is row n against token 16t + 4g + i.
 template <typename E, int D, int T>
-__device__ __forceinline__ f32x4 scores(const PageRegs<D> &r, const Queries<E, D> &q) {
+__device__ __forceinline__ f32x4 scores(const Keys<D> &r, const Queries<E, D> &q) {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int c = 0; c < PageRegs<D>::kChunks; ++c) {
+    for (int c = 0; c < Keys<D>::kChunks; ++c) {
         const u32x4 k = r.k[T][c];
         const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
 #pragma unroll
         for (int st = 0; st < Queries<E, D>::kSteps; ++st)
             s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.piece[st][c], s, 4, 0, T,
-                                                                 (int)r.ks[c], 0, (int)q.scale[st]);
+                                                                 (int)r.scale[c], 0, (int)q.scale[st]);
     }
     return s;
 }
@@ -170,56 +175,65 @@ struct RowState {
 // The values of token pairs: byte B of a token's codes holds its channels 2B
 // and 2B+1; a product wants two tokens of one channel side by side.
 template <typename E, int D, int TAU, int B>
-__device__ __forceinline__ void decode_values(const PageRegs<D> &r, const float (&scale)[4],
-                                              uint32_t (&even)[2], uint32_t (&odd)[2]) {
+__device__ __forceinline__ void decode_values(const Values<D> &r, uint32_t (&even)[2],
+                                              uint32_t (&odd)[2]) {
     constexpr int G = D / 32;
-    uint32_t x[4];
-#define LCE_KV4_TOKEN(I) \
-    x[I] = decode_pair<E, (I * G + B) % 4>(r.v[TAU][(I * G + B) / 4], scale[I])
-    LCE_KV4_TOKEN(0);
-    LCE_KV4_TOKEN(1);
-    LCE_KV4_TOKEN(2);
-    LCE_KV4_TOKEN(3);
-#undef LCE_KV4_TOKEN
-    even[0] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
-    odd[0] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
-    even[1] = __builtin_amdgcn_perm(x[3], x[2], 0x05040100u);
-    odd[1] = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
+    // the bits beside the exponent's do not count: a shift makes a scale's byte one
+    const uint32_t w = r.scale[TAU];
+    const uint32_t x0 = decode_pair<E, B % 4>(r.v[TAU][B / 4], bits_as<float>(w << 23));
+    const uint32_t x1 =
+        decode_pair<E, (G + B) % 4>(r.v[TAU][(G + B) / 4], bits_as<float>(w << 15));
+    const uint32_t x2 =
+        decode_pair<E, (2 * G + B) % 4>(r.v[TAU][(2 * G + B) / 4], bits_as<float>(w << 7));
+    const uint32_t x3 =
+        decode_pair<E, (3 * G + B) % 4>(r.v[TAU][(3 * G + B) / 4], bits_as<float>(w >> 1));
+    even[0] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+    odd[0] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+    even[1] = __builtin_amdgcn_perm(x3, x2, 0x05040100u);
+    odd[1] = __builtin_amdgcn_perm(x3, x2, 0x07060302u);
 }
 
 template <typename E, int D, int U, int B>
-__device__ __forceinline__ void add_values(RowState<D> &st, const PageRegs<D> &r,
-                                           const float (&s0)[4], const float (&s1)[4],
-                                           const u32x4 &p) {
+__device__ __forceinline__ void add_values(RowState<D> &st, const Values<D> &r, const u32x4 &p) {
     if constexpr (B < D / 32) {
         uint32_t e0[2], o0[2], e1[2], o1[2];
-        decode_values<E, D, 2 * U, B>(r, s0, e0, o0);
-        decode_values<E, D, 2 * U + 1, B>(r, s1, e1, o1);
+        decode_values<E, D, 2 * U, B>(r, e0, o0);
+        decode_values<E, D, 2 * U + 1, B>(r, e1, o1);
         st.o[2 * B] = E::mfma16(u32x4{e0[0], e0[1], e1[0], e1[1]}, p, st.o[2 * B]);
         st.o[2 * B + 1] = E::mfma16(u32x4{o0[0], o0[1], o1[0], o1[1]}, p, st.o[2 * B + 1]);
-        add_values<E, D, U, B + 1>(st, r, s0, s1, p);
+        add_values<E, D, U, B + 1>(st, r, p);
     }
 }
 
-// One page into the rows' state.  MASK: some row does not see some token (lo,
-// hi: this row's visible tokens, counted from the page's first).
-template <typename E, int D, bool MASK>
-__device__ __forceinline__ void attend_page(RowState<D> &st, const PageRegs<D> &r,
-                                            const Queries<E, D> &q, float c, int lo, int hi,
-                                            int g) {
-    f32x4 s[4] = {scores<E, D, 0>(r, q), scores<E, D, 1>(r, q), scores<E, D, 2>(r, q),
-                  scores<E, D, 3>(r, q)};
-    float top = -__builtin_inff();
+// Hides the tokens outside [lo, hi) (this row's visible ones, counted from the
+// page's first) and makes what the scales of tokens stand for finite: a hidden
+// token's weight is 0, and 0 times its values has to be 0 whatever the page's
+// unwritten bytes are.
+template <typename E, int D>
+__device__ __forceinline__ void hide(f32x4 (&s)[4], Values<D> &r, int lo, int hi, int g) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = 16 * t + 4 * g + i;
+            s[t][i] = j >= lo && j < hi ? s[t][i] : -__builtin_inff();
+            w |= min(r.scale[t] >> (8 * i) & 255u, E::kMaxScale) << (8 * i);
+        }
+        r.scale[t] = w;
+    }
+}
+
+// A page's scores into the rows' maximum and sum; its weights, ready to be
+// multiplied.
+template <typename E, int D>
+__device__ __forceinline__ void weigh(RowState<D> &st, const f32x4 (&s)[4], u32x4 (&p)[2],
+                                      float c) {
+    float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (MASK) {
-                const int j = 16 * t + 4 * g + i;
-                s[t][i] = j >= lo && j < hi ? s[t][i] : -__builtin_inff();
-            }
-            top = fmaxf(top, s[t][i]);
-        }
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
     top *= c;
     // The maximum that weights are taken against follows the true one only when
     // that has passed it by 2^8: weights up to 256 cost no precision, and most
@@ -233,7 +247,6 @@ __device__ __forceinline__ void attend_page(RowState<D> &st, const PageRegs<D> &
 #pragma unroll
         for (int m = 0; m < D / 16; ++m) st.o[m] *= f;
     }
-    u32x4 p[2];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         float w[4];
@@ -245,18 +258,13 @@ __device__ __forceinline__ void attend_page(RowState<D> &st, const PageRegs<D> &
         p[t / 2][t % 2 * 2] = pack_pair<E>(w[0], w[1]);
         p[t / 2][t % 2 * 2 + 1] = pack_pair<E>(w[2], w[3]);
     }
-    float scale[4][4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (MASK)
-                scale[t][i] = scale_of(min(r.vs[t] >> (8 * i) & 255u, E::kMaxScale));
-            else   // the bits beside the exponent's do not count
-                scale[t][i] = bits_as<float>(i < 3 ? r.vs[t] << (23 - 8 * i) : r.vs[t] >> 1);
-        }
-    add_values<E, D, 0, 0>(st, r, scale[0], scale[1], p[0]);
-    add_values<E, D, 1, 0>(st, r, scale[2], scale[3], p[1]);
+}
+
+template <typename E, int D>
+__device__ __forceinline__ void add_page(RowState<D> &st, const Values<D> &r,
+                                         const u32x4 (&p)[2]) {
+    add_values<E, D, 0, 0>(st, r, p[0]);
+    add_values<E, D, 1, 0>(st, r, p[1]);
 }
 
 // Joins another state of the same rows into this one.
@@ -270,11 +278,17 @@ __device__ __forceinline__ void join(RowState<D> &a, float m, float l, const f32
     for (int i = 0; i < D / 16; ++i) a.o[i] = a.o[i] * fa + o[i] * fb;
 }
 
-template <typename E, int D>
-struct Shared {
-    float o[2][D / 16 * 4][64];
-    float m[2][64], l[2][64];
-    int last;
+template <int D>
+union Shared {
+    struct {
+        float o[2][D / 16 * 4][64];
+        float m[2][64], l[2][64];
+    } waves;
+    struct {
+        float weight[kMostSplits][kRows];   // of each split in each row
+        float l[kRows], m[kRows];
+        int last;
+    } join;
 };
 
 }  // namespace
@@ -290,8 +304,8 @@ struct Shared {
 // belong to one row and the weights leave the softmax as the second operand of
 // the product with the values; no weight and no score crosses lanes.
 template <typename E, int D, bool LIST>
-__global__ __launch_bounds__(kThreads, 2) void attend16_kernel(AttendParams p) {
-    __shared__ Shared<E, D> sh;
+__global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(AttendParams p) {
+    __shared__ Shared<D> sh;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % p.kv_heads, slot = blockIdx.x / p.kv_heads, split = blockIdx.y;
@@ -335,12 +349,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend16_kernel(AttendParams p) {
     const int begin = split * p.chunk;
     const int end = split == splits - 1 ? count : begin + p.chunk;
 
-    Queries<E, D> q;
-    load_queries<E, D>(q,
-                       (const typename E::T *)p.q + (int64_t)(seq.start + i) * p.q_token +
-                           (int64_t)hq * p.q_head,
-                       mine, g);
-
     RowState<D> st;
     st.m = -1e30f;   // finite: a row that has seen nothing weighs exp2(-inf) = 0
     st.l = 0.0f;
@@ -355,40 +363,65 @@ __global__ __launch_bounds__(kThreads, 2) void attend16_kernel(AttendParams p) {
     const uint8_t *cache = p.cache + (int64_t)head * Record<D>::kBytes;
     const int last_page = (z.hi + kPage - 1) / kPage;
 
-    for (int from = begin + wave; from < end; from += kWaves * 64) {
-        // 64 of this wave's pages at a time, one a lane
-        const int e = from + kWaves * lane;
-        int page = -1, phys = -1;
-        if (e < end) {
-            page = LIST ? named[e] : page0 + e;
-            if (page >= 0 && page < last_page) phys = table[page];
-        }
-        uint64_t todo = __builtin_amdgcn_ballot_w64(phys >= 0 && phys < p.pages);
-        if (!todo) continue;
-        PageRegs<D> cur;
-        int at = __builtin_ctzll(todo);
-        todo &= todo - 1;
-        int number = __builtin_amdgcn_readlane(page, at);
-        load_page<D>(cur, cache + (int64_t)__builtin_amdgcn_readlane(phys, at) * stride, n, g);
-        while (true) {
-            PageRegs<D> next;
-            int next_number = -1;
-            if (todo) {
-                at = __builtin_ctzll(todo);
-                todo &= todo - 1;
-                next_number = __builtin_amdgcn_readlane(page, at);
-                load_page<D>(next, cache + (int64_t)__builtin_amdgcn_readlane(phys, at) * stride, n,
-                             g);
+    // 64 of this wave's pages at a time, one a lane: their numbers in the
+    // sequence and in the cache, and which are there
+    int from = begin + wave, page = -1, phys = -1;
+    uint64_t todo = 0;
+    const auto fetch = [&]() {
+        while (!todo && from < end) {
+            const int e = from + kWaves * lane;
+            from += kWaves * 64;
+            page = phys = -1;
+            if (e < end) {
+                page = LIST ? named[e] : page0 + e;
+                if (page >= 0 && page < last_page) phys = table[page];
             }
-            const int t0 = number * kPage;
-            if (t0 < z.lo || t0 + kPage > a.hi)
-                attend_page<E, D, true>(st, cur, q, p.scale_log2, span.lo - t0, span.hi - t0, g);
-            else
-                attend_page<E, D, false>(st, cur, q, p.scale_log2, 0, kPage, g);
-            if (next_number < 0) break;
-            cur = next;
-            number = next_number;
+            todo = __builtin_amdgcn_ballot_w64(phys >= 0 && phys < p.pages);
         }
+    };
+    const auto next = [&](int &number) {
+        const int at = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        number = __builtin_amdgcn_readlane(page, at);
+        return cache + (int64_t)__builtin_amdgcn_readlane(phys, at) * stride;
+    };
+
+    // Keys and values of one page are in registers at a time: the next page's
+    // keys are on their way once this page's scores are there, its values once
+    // this page's are added.
+    fetch();
+    Keys<D> keys;
+    Values<D> values;
+    int number = 0;
+    const bool any = todo != 0;
+    if (any) {
+        const uint8_t *rec = next(number);
+        keys.load(rec, n, g);
+        values.load(rec, n, g);
+    }
+    Queries<E, D> q;
+    load_queries<E, D>(q,
+                       (const typename E::T *)p.q + (int64_t)(seq.start + i) * p.q_token +
+                           (int64_t)hq * p.q_head,
+                       mine, g);
+    bool more = any;
+    while (more) {
+        const int t0 = number * kPage;
+        const bool masked = t0 < z.lo || t0 + kPage > a.hi;
+        f32x4 s[4] = {scores<E, D, 0>(keys, q), scores<E, D, 1>(keys, q),
+                      scores<E, D, 2>(keys, q), scores<E, D, 3>(keys, q)};
+        fetch();
+        more = todo != 0;
+        const uint8_t *rec = nullptr;
+        if (more) {
+            rec = next(number);
+            keys.load(rec, n, g);
+        }
+        if (masked) hide<E, D>(s, values, span.lo - t0, span.hi - t0, g);
+        u32x4 w[2];
+        weigh<E, D>(st, s, w, p.scale_log2);
+        add_page<E, D>(st, values, w);
+        if (more) values.load(rec, n, g);
     }
     st.l = across_rows(st.l, [](float x, float y) { return x + y; });
 
@@ -396,12 +429,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend16_kernel(AttendParams p) {
 #pragma unroll
     for (int half = kWaves / 2; half > 0; half /= 2) {
         if (wave >= half && wave < 2 * half) {
-            sh.m[wave - half][lane] = st.m;
-            sh.l[wave - half][lane] = st.l;
+            sh.waves.m[wave - half][lane] = st.m;
+            sh.waves.l[wave - half][lane] = st.l;
 #pragma unroll
             for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sh.o[wave - half][4 * m + j][lane] = st.o[m][j];
+                for (int j = 0; j < 4; ++j) sh.waves.o[wave - half][4 * m + j][lane] = st.o[m][j];
         }
         __syncthreads();
         if (wave < half) {
@@ -409,14 +442,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend16_kernel(AttendParams p) {
 #pragma unroll
             for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[m][j] = sh.o[wave][4 * m + j][lane];
-            join<D>(st, sh.m[wave][lane], sh.l[wave][lane], o);
+                for (int j = 0; j < 4; ++j) o[m][j] = sh.waves.o[wave][4 * m + j][lane];
+            join<D>(st, sh.waves.m[wave][lane], sh.waves.l[wave][lane], o);
         }
         __syncthreads();
     }
 
-    const int unit = blockIdx.x;
-    constexpr int kPart = kRows * (D + 2);   // floats of a split: m[16], l[16], o[16][D]
     if (splits == 1) {
         if (wave == 0 && mine) {
             const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
@@ -437,51 +468,87 @@ __global__ __launch_bounds__(kThreads, 2) void attend16_kernel(AttendParams p) {
 
     // several splits: leave this one's state in the workspace; the last to get
     // here joins them
-    float *part = p.part + ((int64_t)unit * gridDim.y) * kPart;
+    typedef Part<D, kRows> P;
+    float *part = p.part + (int64_t)blockIdx.x * gridDim.y * P::kFloats;
     if (wave == 0) {
-        float *my = part + (int64_t)split * kPart;
+        float *my = part + (int64_t)split * P::kFloats;
         if (mine) {
-            if (g == 0) {
-                my[n] = st.m;
-                my[kRows + n] = st.l;
-            }
+            if (g == 0) put(my + P::state(n), st.m, st.l);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int m = 0; m < D / 16; m += 4)
-                    *reinterpret_cast<f32x4 *>(my + 2 * kRows + n * D + D / 16 * (4 * g + j) + m) =
-                        f32x4{st.o[m][j], st.o[m + 1][j], st.o[m + 2][j], st.o[m + 3][j]};
+                for (int m = 0; m < D / 16; m += 2)
+                    put(my + P::sums(n) + D / 16 * (4 * g + j) + m, st.o[m][j], st.o[m + 1][j]);
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-        if (lane == 0)
-            sh.last = __hip_atomic_fetch_add(p.tickets + unit, 1, __ATOMIC_RELAXED,
-                                             __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
+        if (lane == 0) sh.join.last = last_of(p.tickets + blockIdx.x, splits);
     }
     __syncthreads();
-    if (!sh.last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    if (threadIdx.x == 0) p.tickets[unit] = 0;   // for the next call
-    for (int x = threadIdx.x; x < valid * (D / 4); x += kThreads) {
-        const int r = x / (D / 4), c = x % (D / 4) * 4;
-        float top = -1e30f;
-        for (int s = 0; s < splits; ++s) top = fmaxf(top, part[(int64_t)s * kPart + r]);
-        float l = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = 0; s < splits; ++s) {
-            const float *from = part + (int64_t)s * kPart;
-            const float f = __builtin_amdgcn_exp2f(from[r] - top);
-            l += from[kRows + r] * f;
-            o += *reinterpret_cast<const f32x4 *>(from + 2 * kRows + r * D + c) * f;
+    if (!sh.join.last) return;
+
+    // a thread for every two channels, eight splits in flight, the first of them
+    // before the weights are known
+    const int pairs = valid * (D / 2);
+    const auto from_of = [&](int x) {
+        return part + P::sums(x / (D / 2)) + x % (D / 2) * 2;
+    };
+    f32x2 y[8];
+    const auto fetch_sums = [&](const float *from, int s) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            y[k] = get(from + (int64_t)min(s + k, splits - 1) * P::kFloats);
+    };
+    fetch_sums(from_of(min((int)threadIdx.x, pairs - 1)), 0);
+    // sixteen threads a row: its maximum, the splits' weights against it, its sum
+    {
+        constexpr int kEach = kMostSplits / 16;
+        const int r = threadIdx.x / 16, k = threadIdx.x % 16;
+        if (r < valid) {
+            float top = -1e30f, l = 0.0f;
+            f32x2 ml[kEach];
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+                if (16 * u < splits)
+                    ml[u] = get(part + (int64_t)min(16 * u + k, splits - 1) * P::kFloats +
+                                P::state(r));
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+                if (16 * u < splits) top = fmaxf(top, ml[u][0]);
+#pragma unroll
+            for (int d = 1; d < 16; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+                if (16 * u + k < splits) {
+                    const float f = __builtin_amdgcn_exp2f(ml[u][0] - top);
+                    sh.join.weight[16 * u + k][r] = f;
+                    l += ml[u][1] * f;
+                }
+#pragma unroll
+            for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
+            if (k == 0) {
+                sh.join.m[r] = top;
+                sh.join.l[r] = l;
+            }
         }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < pairs; x += kThreads) {
+        const int r = x / (D / 2), c = x % (D / 2) * 2;
+        f32x2 o = {0.0f, 0.0f};
+        for (int s = 0; s < splits; s += 8) {
+            if (s > 0 || x >= kThreads) fetch_sums(from_of(x), s);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (s + k < splits) o += y[k] * sh.join.weight[s + k][r];
+        }
+        const float l = sh.join.l[r], inv = l == 0.0f ? 0.0f : 1.0f / l;
         const int rr = base + row0 + r;
         const int64_t at = (int64_t)(seq.start + rr / p.group) * (p.kv_heads * p.group) +
                            head * p.group + rr % p.group;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        u32x2 w = {pack_pair<E>(o[0] * inv, o[1] * inv), pack_pair<E>(o[2] * inv, o[3] * inv)};
-        *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + c) = w;
+        *reinterpret_cast<uint32_t *>((typename E::T *)p.out + at * D + c) =
+            pack_pair<E>(o[0] * inv, o[1] * inv);
         if (p.lse && c == 0)
             p.lse[at] = l == 0.0f ? -__builtin_inff()
-                                  : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+                                  : (sh.join.m[r] + __builtin_log2f(l)) * 0.69314718055994531f;
     }
 }
 

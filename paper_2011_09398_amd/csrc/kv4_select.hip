@@ -1,5 +1,5 @@
 // Choosing pages of the 4-bit cache by the signs of queries and keys.
-#include "kv4_launch.hpp"
+#include "kv4_attend.hpp"
 
 namespace lce {
 namespace kv4 {
@@ -124,19 +124,18 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p) {
             for (int s = 1; s < 64; s *= 2) rank = max(rank, (uint32_t)__shfl_xor((int)rank, s));
             if (rank && (page < p.keep_first || page >= pages - p.keep_last)) rank = kKept;
         }
-        if (lane == 0) ranks[page] = (uint16_t)rank;
+        if (lane == 0)
+            __hip_atomic_store(ranks + page, (uint16_t)rank, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
     }
 
     if (splits > 1) {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (threadIdx.x == 0)
-            last = __hip_atomic_fetch_add(p.tickets + blockIdx.x, 1, __ATOMIC_RELAXED,
-                                          __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
+        if (threadIdx.x == 0) last = last_of(p.tickets + blockIdx.x, splits);
         __syncthreads();
         if (!last) return;
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        if (threadIdx.x == 0) p.tickets[blockIdx.x] = 0;   // for the next call
     } else {
         __syncthreads();
     }
