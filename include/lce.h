@@ -436,7 +436,7 @@ typedef struct {
  * LCE_KV4_WORKSPACE_ZERO bytes are zero before its first use; each call leaves
  * them zero.  Calls that may run at the same time need one each.
  * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim). */
-#define LCE_KV4_WORKSPACE_ZERO 16384
+#define LCE_KV4_WORKSPACE_ZERO 131072
 lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_query_desc *query,
                                   int64_t *bytes);
 

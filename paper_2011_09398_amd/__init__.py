@@ -701,7 +701,7 @@ class PreparedQuantBConv2d:
 
 
 KV4_PAGE = 64
-KV4_WORKSPACE_ZERO = 16384
+KV4_WORKSPACE_ZERO = 131072
 FLOAT_TYPE = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2}
 _float_types = {}      # torch dtype -> lce_float_type, filled at first use
 

@@ -73,6 +73,7 @@ lce_status validate_call(const lce_kv4_cache_desc *d, const lce_kv4_query_desc *
 // What the workspace has room for: states of this many tiles of 16 rows.  More
 // workgroups than this would not run at the same time anyway.
 constexpr int64_t kMostParts = 4096;
+static_assert(kMostParts / 2 <= lce::kv4::kTickets, "a ticket for each unit that is shared");
 
 int64_t tiles16(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q, bool list) {
     const int64_t group = q.q_heads / d.kv_heads;

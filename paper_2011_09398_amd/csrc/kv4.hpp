@@ -12,7 +12,9 @@ namespace kv4 {
 
 constexpr int kPage = LCE_KV4_PAGE;
 constexpr int kThreads = 256;
-constexpr int kTickets = LCE_KV4_WORKSPACE_ZERO / 4;
+// Tickets are 64 bytes apart: draws from one line of memory wait for each other.
+constexpr int kTicketStride = 16;
+constexpr int kTickets = LCE_KV4_WORKSPACE_ZERO / (4 * kTicketStride);
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;

@@ -113,13 +113,17 @@ __device__ __forceinline__ bool last_of(int32_t *ticket, int all) {
 
 constexpr int kMostSplits = 256;   // of one unit: what joining them has LDS for
 
-// States of a tile's splits in the workspace, kRows rows each: (m, l) per row,
-// then the sums of weighted values.
+// A split's state in the workspace: (m, l) of each row, then pairs of sums in
+// the order in which a wave holds them, `rows` rows next to each other, so that
+// a store of the wave is one run of memory.
 template <int D, int ROWS>
 struct Part {
     static constexpr int kFloats = ROWS * (D + 2);
     static __device__ __forceinline__ int state(int row) { return 2 * row; }
-    static __device__ __forceinline__ int sums(int row) { return 2 * ROWS + row * D; }
+    // the pair at channels D/16 * (4g + j) + m, m + 1
+    static __device__ __forceinline__ int sums(int rows, int row, int g, int j, int m) {
+        return 2 * ROWS + 2 * (((j * (D / 32) + m / 2) * 4 + g) * rows + row);
+    }
 };
 
 }  // namespace kv4

@@ -478,9 +478,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int m = 0; m < D / 16; m += 2)
-                    put(my + P::sums(n) + D / 16 * (4 * g + j) + m, st.o[m][j], st.o[m + 1][j]);
+                    put(my + P::sums(valid, n, g, j, m), st.o[m][j], st.o[m + 1][j]);
         }
-        if (lane == 0) sh.join.last = last_of(p.tickets + blockIdx.x, splits);
+        if (lane == 0) sh.join.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
     }
     __syncthreads();
     if (!sh.join.last) return;
@@ -488,16 +488,14 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     // a thread for every two channels, eight splits in flight, the first of them
     // before the weights are known
     const int pairs = valid * (D / 2);
-    const auto from_of = [&](int x) {
-        return part + P::sums(x / (D / 2)) + x % (D / 2) * 2;
-    };
     f32x2 y[8];
-    const auto fetch_sums = [&](const float *from, int s) {
+    const auto fetch_sums = [&](int x, int s) {
+        const float *from = part + 2 * kRows + 2 * x;   // pairs as they lie in memory
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             y[k] = get(from + (int64_t)min(s + k, splits - 1) * P::kFloats);
     };
-    fetch_sums(from_of(min((int)threadIdx.x, pairs - 1)), 0);
+    fetch_sums(min((int)threadIdx.x, pairs - 1), 0);
     // sixteen threads a row: its maximum, the splits' weights against it, its sum
     {
         constexpr int kEach = kMostSplits / 16;
@@ -532,10 +530,11 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     }
     __syncthreads();
     for (int x = threadIdx.x; x < pairs; x += kThreads) {
-        const int r = x / (D / 2), c = x % (D / 2) * 2;
+        const int r = x % valid, gg = x / valid % 4, jm = x / valid / 4;
+        const int c = D / 16 * (4 * gg + jm / (D / 32)) + jm % (D / 32) * 2;
         f32x2 o = {0.0f, 0.0f};
         for (int s = 0; s < splits; s += 8) {
-            if (s > 0 || x >= kThreads) fetch_sums(from_of(x), s);
+            if (s > 0 || x >= kThreads) fetch_sums(x, s);
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (s + k < splits) o += y[k] * sh.join.weight[s + k][r];

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p) {
     if (splits > 1) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (threadIdx.x == 0) last = last_of(p.tickets + blockIdx.x, splits);
+        if (threadIdx.x == 0) last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
         __syncthreads();
         if (!last) return;
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
