@@ -93,18 +93,33 @@ struct Split {
     int splits;   // workgroups that share a unit, at most
 };
 
-// Divides `pages` pages of each of `units` units of work so that about `target`
-// workgroups run, of at least `least` pages each.
-Split split_pages(int64_t units, int64_t pages, int64_t target, int64_t least) {
-    const int64_t room = std::min<int64_t>(
-        std::max<int64_t>(kMostParts / std::max<int64_t>(units, 1), 1), lce::kv4::kMostSplits);
-    int64_t z = std::min(std::max<int64_t>(target / std::max<int64_t>(units, 1), 1), room);
-    int64_t chunk = std::max((pages + z - 1) / z, least);
-    if (const int t = tuning(LCE_TUNE_KV4_CHUNK))
+// `pages` pages of each of `units` units of work, `step` microseconds for a wave to
+// take one: how many workgroups (of four waves) share a unit.  Sharing costs
+// about `fixed` microseconds for the partial states, the ticket and the joining,
+// and 0.06 for each state joined, so a unit is divided only where its pages take
+// longer, and no further than 512 workgroups in all: two a CU keep as many loads
+// in flight as the memory answers.  Measured (us): one sequence of 20001 tokens,
+// 8 heads of 128, chunks of 8, 12, 16, 32, 64 pages 13.5, 12.2, 12.1, 14.0, 20.0;
+// lists of 64 pages, 128 units of 128, chunks of 8, 12, 16, 24, 64: 20.9, 18.5,
+// 17.6, 18.0, 21.9; lists of 24, 120 units of 256, chunks of 8, 12, 24: 20.7,
+// 19.5, 19.0; 64 sequences of up to 8192 tokens, 512 units of 128, chunks of 16,
+// 64, 128: 50.3, 49.8, 44.8.
+Split split_pages(int64_t units, int64_t pages, double step, double fixed) {
+    const int64_t some = std::max<int64_t>(units, 1);
+    const int64_t room =
+        std::min<int64_t>(std::max<int64_t>(kMostParts / some, 1), lce::kv4::kMostSplits);
+    int64_t chunk = std::max<int64_t>(pages, 1);
+    if (const int t = tuning(LCE_TUNE_KV4_CHUNK)) {
         chunk = std::max<int64_t>(t > 0 ? t : 1, (pages + room - 1) / room);
+    } else {
+        const double whole = pages * step / 4;
+        // the least of whole / z + fixed + 0.06 z
+        const int64_t z = std::min<int64_t>({room, 512 / some, (int64_t)std::sqrt(whole / 0.06)});
+        if (z > 1 && whole / z + fixed + 0.06 * z < whole) chunk = (pages + z - 1) / z;
+    }
     Split s;
     s.chunk = (int)chunk;
-    s.splits = (int)((pages + chunk - 1) / chunk);
+    s.splits = (int)std::max<int64_t>((pages + chunk - 1) / chunk, 1);
     return s;
 }
 
@@ -180,7 +195,7 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
     const int64_t units = std::max(tiles16(*desc, *query, false), tiles16(*desc, *query, true)) *
                           heads;
     // a list may be longer than the table, so its splits are bounded by the room
-    const int64_t parts = kMostParts * 16 * (desc->head_dim + 2) * 4;
+    const int64_t parts = kMostParts * 16 * (desc->head_dim + 4) * 4;
     const int64_t ranks = query->tokens * heads * width * 2;
     *bytes = LCE_KV4_WORKSPACE_ZERO + std::max(units ? parts : 0, ranks);
     return ok();
@@ -213,7 +228,8 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
 
     const bool list = query->list > 0;
     const int64_t units = tiles16(*desc, *query, list) * desc->kv_heads;
-    const Split s = split_pages(units, list ? query->list : most_pages(*query), 1024, 4);
+    const Split s = split_pages(units, list ? query->list : most_pages(*query),
+                                0.25 + 0.4 * desc->head_dim / 128, 1 + 2.5 * desc->head_dim / 128);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;
@@ -257,7 +273,7 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
     // a window hides pages but does not renumber them: all up to the last count
     lce_kv4_query_desc all = *query;
     all.window = 0;
-    const Split s = split_pages(units, most_pages(all), 1024, 8);
+    const Split s = split_pages(units, most_pages(all), 0.5, 2);
     lce::kv4::SelectParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.keep_first = keep_first, p.keep_last = keep_last;

@@ -84,20 +84,16 @@ __device__ __forceinline__ uint32_t next_piece(float (&x)[4]) {
     return (uint32_t)w;
 }
 
-// What workgroups on different XCDs tell each other within a launch goes through
-// relaxed atomics of device scope: written through and read past the caches that
-// are not coherent, so that neither side has to write back or invalidate a whole
-// L2 (a release fence per workgroup measured 64 ns of the launch each, one after
-// the other: 160 us for 2500 of them, against 18).  What remains of the order is
-// that the stores are done before the ticket is drawn.
-__device__ __forceinline__ void put(float *p, float a, float b) {
-    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), bits_as<uint64_t>(f32x2{a, b}),
+// What workgroups on different XCDs tell each other within a launch is stored
+// with relaxed atomics of device scope, which write through the caches that are
+// not coherent; a release fence would write back the XCD's whole L2 instead, one
+// workgroup after the other (64 ns each: 160 us of a launch of 2500, against 18).
+// What remains of the order is that the stores are done before the ticket is
+// drawn.  The one workgroup that reads them invalidates its caches first (an
+// acquire fence), and loads as usual.
+__device__ __forceinline__ void put(float *p, f32x2 v) {
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), bits_as<uint64_t>(v),
                        __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-__device__ __forceinline__ f32x2 get(const float *p) {
-    return bits_as<f32x2>(__hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED,
-                                            __HIP_MEMORY_SCOPE_AGENT));
 }
 
 // Draws a ticket after this wave's stores; true for the last of `all`, which
@@ -111,20 +107,71 @@ __device__ __forceinline__ bool last_of(int32_t *ticket, int all) {
     return true;
 }
 
-constexpr int kMostSplits = 256;   // of one unit: what joining them has LDS for
+constexpr int kMostSplits = 256;   // of one unit
 
-// A split's state in the workspace: (m, l) of each row, then pairs of sums in
-// the order in which a wave holds them, `rows` rows next to each other, so that
-// a store of the wave is one run of memory.
+// A split's state in the workspace: (m, l) of each row, then sums four at a
+// time in the order in which a wave holds them, `rows` rows next to each other,
+// so that what a wave stores is one run of memory.
 template <int D, int ROWS>
 struct Part {
-    static constexpr int kFloats = ROWS * (D + 2);
-    static __device__ __forceinline__ int state(int row) { return 2 * row; }
-    // the pair at channels D/16 * (4g + j) + m, m + 1
-    static __device__ __forceinline__ int sums(int rows, int row, int g, int j, int m) {
-        return 2 * ROWS + 2 * (((j * (D / 32) + m / 2) * 4 + g) * rows + row);
+    static constexpr int kFloats = ROWS * (D + 4);
+    static __device__ __forceinline__ int state(int row) { return 4 * row; }
+    // sums `quad` (of D/4) of a row; which channels they are is the kernel's affair
+    static __device__ __forceinline__ int sums(int rows, int row, int quad) {
+        return 4 * ROWS + 4 * (quad * rows + row);
     }
 };
+
+// Joins sums `quad` of a row over all its splits, eight at a time, each with its
+// own maximum, against a running one: the sums, their maximum and their weight.
+template <int D, int ROWS>
+__device__ __forceinline__ f32x4 join_splits(const float *part, int splits, int rows, int row,
+                                             int quad, float &top, float &l) {
+    typedef Part<D, ROWS> P;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    top = -1e30f;
+    l = 0.0f;
+    for (int s0 = 0; s0 < splits; s0 += 8) {
+        f32x2 ml[8];
+        f32x4 y[8];
+        const auto fetch = [&](int k) {
+            const float *from = part + (int64_t)min(s0 + k, splits - 1) * P::kFloats;
+            ml[k] = *reinterpret_cast<const f32x2 *>(from + P::state(row));
+            y[k] = *reinterpret_cast<const f32x4 *>(from + P::sums(rows, row, quad));
+        };
+        const bool many = s0 + 4 < splits;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) fetch(k);
+        if (many) {
+#pragma unroll
+            for (int k = 4; k < 8; ++k) fetch(k);
+        }
+        const auto add = [&](int k) {
+            float w = ml[k][0] - top;
+            w = s0 + k < splits ? __builtin_amdgcn_exp2f(w) : 0.0f;
+            l += ml[k][1] * w;
+            o += y[k] * w;
+        };
+        float high = top;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) high = fmaxf(high, ml[k][0]);
+        if (many) {
+#pragma unroll
+            for (int k = 4; k < 8; ++k) high = fmaxf(high, ml[k][0]);
+        }
+        const float f = __builtin_amdgcn_exp2f(top - high);
+        l *= f;
+        o *= f;
+        top = high;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add(k);
+        if (many) {
+#pragma unroll
+            for (int k = 4; k < 8; ++k) add(k);
+        }
+    }
+    return o;
+}
 
 }  // namespace kv4
 }  // namespace lce

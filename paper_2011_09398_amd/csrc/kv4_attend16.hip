@@ -77,32 +77,48 @@ struct Queries {
     uint32_t scale[kSteps];
 };
 
+// The same channels as they come from memory: on their way while the page
+// numbers are, and made into pieces while the first page is.
+template <int D>
+struct RawQueries {
+    static constexpr int kHalves = D < 128 ? 1 : 2;
+    u32x4 w[Keys<D>::kChunks][kHalves][2];
+
+    __device__ __forceinline__ void load(const void *row, bool valid, int g) {
+#pragma unroll
+        for (int c = 0; c < Keys<D>::kChunks; ++c)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                w[c][h][0] = w[c][h][1] = u32x4{0, 0, 0, 0};
+                if (valid) {
+                    const u32x4 *at = reinterpret_cast<const u32x4 *>(
+                        static_cast<const uint16_t *>(row) + 128 * c + 64 * h + 16 * g);
+                    w[c][h][0] = at[0], w[c][h][1] = at[1];
+                }
+            }
+    }
+};
+
 template <typename E, int D>
-__device__ __forceinline__ void load_queries(Queries<E, D> &q, const typename E::T *row, bool valid,
-                                             int g) {
-    constexpr int kChunks = Keys<D>::kChunks, kHalves = D < 128 ? 1 : 2;
+__device__ __forceinline__ void make_pieces(Queries<E, D> &q, const RawQueries<D> &raw, int g) {
+    constexpr int kChunks = Keys<D>::kChunks, kHalves = RawQueries<D>::kHalves;
     float x[kChunks][kHalves][16];
-    float top = 0.0f;
-    bool odd = false;
+    uint32_t bits = 0;   // of the largest absolute value: as whole numbers, in the
+                         // order of the values, infinities and NaN last
 #pragma unroll
     for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
-            u32x4 w[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-            if (valid) {
-                const u32x4 *at = reinterpret_cast<const u32x4 *>(row + 128 * c + 64 * h + 16 * g);
-                w[0] = at[0], w[1] = at[1];
-            }
+        for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t word = w[i / 8][i % 8 / 2];
-                const typename E::T2 pair = bits_as<typename E::T2>(word);
-                x[c][h][i] = (float)pair[i % 2];
-                odd |= !(__builtin_fabsf(x[c][h][i]) < __builtin_inff());
-                top = fmaxf(top, __builtin_fabsf(x[c][h][i]));
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t w = raw.w[c][h][i / 4][i % 4];
+                bits = max(bits, max(w & 0x7FFFu, w >> 16 & 0x7FFFu));
+                const typename E::T2 pair = bits_as<typename E::T2>(w);
+                x[c][h][2 * i] = (float)pair[0];
+                x[c][h][2 * i + 1] = (float)pair[1];
             }
-        }
-    if (odd) top = __builtin_inff();
+    float top = (float)bits_as<typename E::T>((uint16_t)bits);
+    if (!(top < __builtin_inff())) top = __builtin_inff();
     top = across_rows(top, [](float a, float b) { return fmaxf(a, b); });
     const RowScale s = row_scale(top);
     uint32_t bytes[E::kPieces][kChunks][kHalves][4];
@@ -279,16 +295,10 @@ __device__ __forceinline__ void join(RowState<D> &a, float m, float l, const f32
 }
 
 template <int D>
-union Shared {
-    struct {
-        float o[2][D / 16 * 4][64];
-        float m[2][64], l[2][64];
-    } waves;
-    struct {
-        float weight[kMostSplits][kRows];   // of each split in each row
-        float l[kRows], m[kRows];
-        int last;
-    } join;
+struct Shared {
+    float o[kWaves / 2][D / 16 * 4][64];
+    float m[kWaves / 2][64], l[kWaves / 2][64];
+    int last;
 };
 
 }  // namespace
@@ -355,6 +365,10 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
 #pragma unroll
     for (int m = 0; m < D / 16; ++m) st.o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+    RawQueries<D> raw;
+    raw.load((const typename E::T *)p.q + (int64_t)(seq.start + i) * p.q_token +
+                 (int64_t)hq * p.q_head,
+             mine, g);
     const int32_t *named =
         LIST ? p.named + ((int64_t)(seq.start + base / p.group) * p.kv_heads + head) * p.list
              : nullptr;
@@ -400,10 +414,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
         values.load(rec, n, g);
     }
     Queries<E, D> q;
-    load_queries<E, D>(q,
-                       (const typename E::T *)p.q + (int64_t)(seq.start + i) * p.q_token +
-                           (int64_t)hq * p.q_head,
-                       mine, g);
+    make_pieces<E, D>(q, raw, g);
     bool more = any;
     while (more) {
         const int t0 = number * kPage;
@@ -425,16 +436,16 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     }
     st.l = across_rows(st.l, [](float x, float y) { return x + y; });
 
-    // join the waves: 2 and 3 into 0 and 1, then 1 into 0
+    // join the waves: the upper half into the lower one, until one is left
 #pragma unroll
     for (int half = kWaves / 2; half > 0; half /= 2) {
         if (wave >= half && wave < 2 * half) {
-            sh.waves.m[wave - half][lane] = st.m;
-            sh.waves.l[wave - half][lane] = st.l;
+            sh.m[wave - half][lane] = st.m;
+            sh.l[wave - half][lane] = st.l;
 #pragma unroll
             for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sh.waves.o[wave - half][4 * m + j][lane] = st.o[m][j];
+                for (int j = 0; j < 4; ++j) sh.o[wave - half][4 * m + j][lane] = st.o[m][j];
         }
         __syncthreads();
         if (wave < half) {
@@ -442,8 +453,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
 #pragma unroll
             for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[m][j] = sh.waves.o[wave][4 * m + j][lane];
-            join<D>(st, sh.waves.m[wave][lane], sh.waves.l[wave][lane], o);
+                for (int j = 0; j < 4; ++j) o[m][j] = sh.o[wave][4 * m + j][lane];
+            join<D>(st, sh.m[wave][lane], sh.l[wave][lane], o);
         }
         __syncthreads();
     }
@@ -473,81 +484,40 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     if (wave == 0) {
         float *my = part + (int64_t)split * P::kFloats;
         if (mine) {
-            if (g == 0) put(my + P::state(n), st.m, st.l);
+            if (g == 0) put(my + P::state(n), f32x2{st.m, st.l});
+            // quad (j, m / 4, g): channels D/16 * (4g + j) + m .. m + 3
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int m = 0; m < D / 16; m += 2)
-                    put(my + P::sums(valid, n, g, j, m), st.o[m][j], st.o[m + 1][j]);
-        }
-        if (lane == 0) sh.join.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
-    }
-    __syncthreads();
-    if (!sh.join.last) return;
-
-    // a thread for every two channels, eight splits in flight, the first of them
-    // before the weights are known
-    const int pairs = valid * (D / 2);
-    f32x2 y[8];
-    const auto fetch_sums = [&](int x, int s) {
-        const float *from = part + 2 * kRows + 2 * x;   // pairs as they lie in memory
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            y[k] = get(from + (int64_t)min(s + k, splits - 1) * P::kFloats);
-    };
-    fetch_sums(min((int)threadIdx.x, pairs - 1), 0);
-    // sixteen threads a row: its maximum, the splits' weights against it, its sum
-    {
-        constexpr int kEach = kMostSplits / 16;
-        const int r = threadIdx.x / 16, k = threadIdx.x % 16;
-        if (r < valid) {
-            float top = -1e30f, l = 0.0f;
-            f32x2 ml[kEach];
-#pragma unroll
-            for (int u = 0; u < kEach; ++u)
-                if (16 * u < splits)
-                    ml[u] = get(part + (int64_t)min(16 * u + k, splits - 1) * P::kFloats +
-                                P::state(r));
-#pragma unroll
-            for (int u = 0; u < kEach; ++u)
-                if (16 * u < splits) top = fmaxf(top, ml[u][0]);
-#pragma unroll
-            for (int d = 1; d < 16; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-#pragma unroll
-            for (int u = 0; u < kEach; ++u)
-                if (16 * u + k < splits) {
-                    const float f = __builtin_amdgcn_exp2f(ml[u][0] - top);
-                    sh.join.weight[16 * u + k][r] = f;
-                    l += ml[u][1] * f;
+                for (int m = 0; m < D / 16; m += 4) {
+                    float *to = my + P::sums(valid, n, (j * (D / 64) + m / 4) * 4 + g);
+                    put(to, f32x2{st.o[m][j], st.o[m + 1][j]});
+                    put(to + 2, f32x2{st.o[m + 2][j], st.o[m + 3][j]});
                 }
-#pragma unroll
-            for (int d = 1; d < 16; d *= 2) l += __shfl_xor(l, d);
-            if (k == 0) {
-                sh.join.m[r] = top;
-                sh.join.l[r] = l;
-            }
         }
+        if (lane == 0) sh.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < pairs; x += kThreads) {
-        const int r = x % valid, gg = x / valid % 4, jm = x / valid / 4;
-        const int c = D / 16 * (4 * gg + jm / (D / 32)) + jm % (D / 32) * 2;
-        f32x2 o = {0.0f, 0.0f};
-        for (int s = 0; s < splits; s += 8) {
-            if (s > 0 || x >= kThreads) fetch_sums(x, s);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (s + k < splits) o += y[k] * sh.join.weight[s + k][r];
-        }
-        const float l = sh.join.l[r], inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (!sh.last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+
+    // a thread for every four channels of a row, rows next to each other
+    const int shift = valid > 1 ? 32 - __builtin_clz(valid - 1) : 0;   // rows, a power of two
+    for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
+        const int r = x & ((1 << shift) - 1), quad = x >> shift;
+        if (r >= valid) continue;
+        float top, l;
+        const f32x4 o = join_splits<D, kRows>(part, splits, valid, r, quad, top, l);
+        const int c = D / 16 * (4 * (quad % 4) + quad / 4 / (D / 64)) + quad / 4 % (D / 64) * 4;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         const int rr = base + row0 + r;
         const int64_t at = (int64_t)(seq.start + rr / p.group) * (p.kv_heads * p.group) +
                            head * p.group + rr % p.group;
-        *reinterpret_cast<uint32_t *>((typename E::T *)p.out + at * D + c) =
-            pack_pair<E>(o[0] * inv, o[1] * inv);
+        *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + c) =
+            u32x2{pack_pair<E>(o[0] * inv, o[1] * inv), pack_pair<E>(o[2] * inv, o[3] * inv)};
         if (p.lse && c == 0)
             p.lse[at] = l == 0.0f ? -__builtin_inff()
-                                  : (sh.join.m[r] + __builtin_log2f(l)) * 0.69314718055994531f;
+                                  : (top + __builtin_log2f(l)) * 0.69314718055994531f;
     }
 }
 
