@@ -104,7 +104,7 @@ struct Split {
 // 17.6, 18.0, 21.9; lists of 24, 120 units of 256, chunks of 8, 12, 24: 20.7,
 // 19.5, 19.0; 64 sequences of up to 8192 tokens, 512 units of 128, chunks of 16,
 // 64, 128: 50.3, 49.8, 44.8.
-Split split_pages(int64_t units, int64_t pages, double step, double fixed) {
+Split split_pages(int64_t units, int64_t pages, double step, double fixed, int64_t most) {
     const int64_t some = std::max<int64_t>(units, 1);
     const int64_t room =
         std::min<int64_t>(std::max<int64_t>(kMostParts / some, 1), lce::kv4::kMostSplits);
@@ -114,7 +114,7 @@ Split split_pages(int64_t units, int64_t pages, double step, double fixed) {
     } else {
         const double whole = pages * step / 4;
         // the least of whole / z + fixed + 0.06 z
-        const int64_t z = std::min<int64_t>({room, 512 / some, (int64_t)std::sqrt(whole / 0.06)});
+        const int64_t z = std::min<int64_t>({room, most / some, (int64_t)std::sqrt(whole / 0.06)});
         if (z > 1 && whole / z + fixed + 0.06 * z < whole) chunk = (pages + z - 1) / z;
     }
     Split s;
@@ -229,7 +229,7 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     const bool list = query->list > 0;
     const int64_t units = tiles16(*desc, *query, list) * desc->kv_heads;
     const Split s = split_pages(units, list ? query->list : most_pages(*query),
-                                0.25 + 0.4 * desc->head_dim / 128, 1 + 2.5 * desc->head_dim / 128);
+                                0.25 + 0.4 * desc->head_dim / 128, 1 + 2.5 * desc->head_dim / 128, 512);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;
@@ -273,7 +273,7 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
     // a window hides pages but does not renumber them: all up to the last count
     lce_kv4_query_desc all = *query;
     all.window = 0;
-    const Split s = split_pages(units, most_pages(all), 0.5, 2);
+    const Split s = split_pages(units, most_pages(all), 0.5, 2, 2048);
     lce::kv4::SelectParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.keep_first = keep_first, p.keep_last = keep_last;
