@@ -16,7 +16,8 @@ SOURCES = [os.path.join(CSRC, f) for f in ("lce.hip", "mfma_tiles.hip", "mfma_fs
                                                   "mfma_fs_win.hip", "mfma_stream.hip",
                                                   "mfma_stream_ohwi.hip",
                                                   "quant_conv.hip", "kv4.hip", "kv4_codec.hip",
-                                                  "kv4_attend16.hip", "kv4_select.hip")]
+                                                  "kv4_attend16.hip", "kv4_attend128.hip",
+                                                  "kv4_select.hip")]
 BUILD_DIR = os.path.join(PKG, "_build")
 # Measurement-only probe of the xor/popcount VALU rate (not part of the C ABI).
 PROBE_LIB = os.path.join(PKG, "libprobe.so")

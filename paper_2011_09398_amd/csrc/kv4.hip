@@ -70,14 +70,15 @@ lce_status validate_call(const lce_kv4_cache_desc *d, const lce_kv4_query_desc *
     return LCE_OK;
 }
 
-// What the workspace has room for: states of this many tiles of 16 rows.  More
-// workgroups than this would not run at the same time anyway.
+// What the workspace has room for: states of this many tiles of 16 rows, an eighth
+// of it of 128.  More workgroups would not run at the same time anyway.
 constexpr int64_t kMostParts = 4096;
 static_assert(kMostParts / 2 <= lce::kv4::kTickets, "a ticket for each unit that is shared");
 
-int64_t tiles16(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q, bool list) {
+// Tiles of `rows` query rows of a cache head; with a list, of one token each.
+int64_t tiles(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q, int rows, bool list) {
     const int64_t group = q.q_heads / d.kv_heads;
-    return list ? q.tokens * ((group + 15) / 16) : q.tokens * group / 16 + q.seqs;
+    return list ? q.tokens * ((group + rows - 1) / rows) : q.tokens * group / rows + q.seqs;
 }
 
 // Pages that a unit of work can have before it, as far as the call says.
@@ -86,6 +87,16 @@ int64_t most_pages(const lce_kv4_query_desc &q) {
     if (q.max_len > 0) n = std::min<int64_t>(n, (q.max_len + (int64_t)kPage - 1) / kPage);
     if (q.window > 0) n = std::min<int64_t>(n, ((int64_t)q.window + std::max(q.max_q, 1)) / kPage + 2);
     return n;
+}
+
+// Whether the tiles of attention are of 128 query rows.  They take a page's values
+// out of 4 bits once for 128 rows instead of 16, but a tile that is not full does
+// all of its work.
+bool wide_tiles(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
+    if (q.list > 0) return false;
+    if (const int t = tuning(LCE_TUNE_KV4_ROWS)) return t == 128;
+    const int64_t most = q.max_q > 0 ? q.max_q : q.tokens / q.seqs;
+    return most * (q.q_heads / d.kv_heads) >= 64;
 }
 
 struct Split {
@@ -104,10 +115,11 @@ struct Split {
 // 17.6, 18.0, 21.9; lists of 24, 120 units of 256, chunks of 8, 12, 24: 20.7,
 // 19.5, 19.0; 64 sequences of up to 8192 tokens, 512 units of 128, chunks of 16,
 // 64, 128: 50.3, 49.8, 44.8.
-Split split_pages(int64_t units, int64_t pages, double step, double fixed, int64_t most) {
+Split split_pages(int64_t units, int64_t pages, double step, double fixed, int64_t most,
+                  int64_t parts) {
     const int64_t some = std::max<int64_t>(units, 1);
     const int64_t room =
-        std::min<int64_t>(std::max<int64_t>(kMostParts / some, 1), lce::kv4::kMostSplits);
+        std::min<int64_t>(std::max<int64_t>(parts / some, 1), lce::kv4::kMostSplits);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV4_CHUNK)) {
         chunk = std::max<int64_t>(t > 0 ? t : 1, (pages + room - 1) / room);
@@ -192,7 +204,7 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
     if (!bytes) return fail(LCE_EINVAL, "bytes output pointer is NULL");
     if (const lce_status st = validate_query(desc, query)) return st;
     const int64_t heads = desc->kv_heads, width = query->table_width;
-    const int64_t units = std::max(tiles16(*desc, *query, false), tiles16(*desc, *query, true)) *
+    const int64_t units = std::max(tiles(*desc, *query, 16, false), tiles(*desc, *query, 16, true)) *
                           heads;
     // a list may be longer than the table, so its splits are bounded by the room
     const int64_t parts = kMostParts * 16 * (desc->head_dim + 4) * 4;
@@ -227,9 +239,13 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
                     (long long)need);
 
     const bool list = query->list > 0;
-    const int64_t units = tiles16(*desc, *query, list) * desc->kv_heads;
-    const Split s = split_pages(units, list ? query->list : most_pages(*query),
-                                0.25 + 0.4 * desc->head_dim / 128, 1 + 2.5 * desc->head_dim / 128, 512);
+    const bool wide = wide_tiles(*desc, *query);
+    const int64_t units = tiles(*desc, *query, wide ? 128 : 16, list) * desc->kv_heads;
+    const double size = desc->head_dim / 128.0;
+    const Split s =
+        wide ? split_pages(units, most_pages(*query), 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8)
+             : split_pages(units, list ? query->list : most_pages(*query), 0.25 + 0.4 * size,
+                           1 + 2.5 * size, 512, kMostParts);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;
@@ -237,8 +253,11 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     p.lse = lse;
     p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + LCE_KV4_WORKSPACE_ZERO);
     p.scale_log2 = query->scale * 1.44269504088896341f;
-    lce::kv4::launch_attend16(p, query->type, desc->head_dim,
-                              dim3((unsigned)units, (unsigned)s.splits), stream);
+    const dim3 grid((unsigned)units, (unsigned)s.splits);
+    if (wide)
+        lce::kv4::launch_attend128(p, query->type, desc->head_dim, grid, stream);
+    else
+        lce::kv4::launch_attend16(p, query->type, desc->head_dim, grid, stream);
     return check_launch("lce_kv4_attention launch");
 }
 
@@ -273,7 +292,7 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
     // a window hides pages but does not renumber them: all up to the last count
     lce_kv4_query_desc all = *query;
     all.window = 0;
-    const Split s = split_pages(units, most_pages(all), 0.5, 2, 2048);
+    const Split s = split_pages(units, most_pages(all), 0.5, 2, 2048, kMostParts);
     lce::kv4::SelectParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.keep_first = keep_first, p.keep_last = keep_last;

@@ -21,6 +21,9 @@ struct Bf16 {
     static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ f32x16 mfma32(const u32x4 &a, const u32x4 &b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
+    }
 };
 
 struct F16 {
@@ -31,6 +34,9 @@ struct F16 {
     static constexpr uint32_t kMaxScale = 140;   // 6 * 2^13 is finite in float16
     static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(const u32x4 &a, const u32x4 &b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
 };
 

@@ -53,6 +53,8 @@ void launch_append(const AppendParams &p, int type, int dim, hipStream_t s);
 void launch_read(const ReadParams &p, int type, int dim, hipStream_t s);
 // 16 query rows a workgroup; grid = (tiles * kv_heads, splits)
 void launch_attend16(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);
+// 128 query rows a workgroup, no list; grid = (tiles * kv_heads, splits)
+void launch_attend128(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);
 // one token and head of the cache a workgroup; grid = (tokens * kv_heads, splits)
 void launch_select(const SelectParams &p, int type, int dim, dim3 grid, hipStream_t s);
 

@@ -196,14 +196,30 @@ def test_single_tokens(dim, dtype, q_heads, kv_heads, chunk):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 40), (False, 70), (True, 1)])
 @pytest.mark.parametrize("chunk", [0, 2])
-def test_several_tokens(dim, dtype, causal, window, chunk):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_several_tokens(dim, dtype, causal, window, chunk, rows):
     lengths, queries = [150, 3, 64, 0, 90, 129], [5, 3, 1, 0, 90, 17]
     b = Batch(dim, lengths, queries, 6, 2, dim, dtype)
-    with lce.tuning(kv4_chunk=chunk):
+    with lce.tuning(kv4_chunk=chunk, kv4_rows=rows):
         attend(b, causal, window)
 
 
-def test_more_queries_than_tokens_leave_rows_that_see_nothing():
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_long_prompts(dim, dtype):
+    """Tiles of 128 rows that are full, that several pages are whole for, and whose last
+    waves have no rows; sequences shorter than their tile."""
+    b = Batch(25, [260, 33, 500, 1], [260, 33, 111, 1], 5, 1, dim, dtype)
+    out, lse = attend(b, max_q=260)
+    again = lce.kv4_attention(*b.device(lce), max_q=260)
+    assert torch.equal(out, again)
+    with lce.tuning(kv4_rows=128, kv4_chunk=1):
+        attend(b, window=77)
+
+
+@pytest.mark.parametrize("rows", [16, 128])
+def test_more_queries_than_tokens_leave_rows_that_see_nothing(rows):
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(3, [4, 70], [7, 2], 4, 2, 64, "bf16")
     for causal in (True, False):
         out, lse = attend(b, causal)
@@ -211,7 +227,9 @@ def test_more_queries_than_tokens_leave_rows_that_see_nothing():
             assert not out[:3].any() and torch.isneginf(lse[:3]).all()
 
 
-def test_no_sequence_has_tokens():
+@pytest.mark.parametrize("rows", [16, 128])
+def test_no_sequence_has_tokens(rows):
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(3, [0, 0], [2, 1], 4, 2, 128, "f16")
     for causal in (True, False):
         out, lse = attend(b, causal)
@@ -219,16 +237,18 @@ def test_no_sequence_has_tokens():
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-def test_many_sequences_and_long_ones(dtype):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_many_sequences_and_long_ones(dtype, rows):
     """More sequences than lanes; one long enough that a wave takes several of its pages."""
+    lce.set_tuning(kv4_rows=rows)
     rng = np.random.default_rng(2)
     lengths = [int(n) for n in rng.integers(0, 90, 150)]
     lengths[77] = 1900
     queries = [min(n, int(x)) for n, x in zip(lengths, rng.integers(0, 4, 150))]
     b = Batch(8, lengths, queries, 4, 1, 64, dtype)
     attend(b)
-    with lce.tuning(kv4_chunk=1000):
-        attend(b, max_len=1900)
+    lce.set_tuning(kv4_chunk=1000)
+    attend(b, max_len=1900)
 
 
 def test_hints_that_are_wrong_cost_no_result():
@@ -252,15 +272,19 @@ def test_strided_queries_and_scale():
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("spread", [1e-3, 30.0])
-def test_flat_and_sharp_scores(dtype, spread):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_flat_and_sharp_scores(dtype, spread, rows):
     """Scores that are all alike, and rows that one token takes nearly whole (large maxima that
     rise from page to page)."""
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(12, [500], [2], 4, 1, 128, dtype)
     attend(b, scale=spread / 11.3)
 
 
 @pytest.mark.parametrize("dtype,tiny,huge", [("bf16", 2.0 ** -70, 2.0 ** 60), ("f16", 2.0 ** -22, 2.0 ** 14)])
-def test_queries_of_any_size(dtype, tiny, huge):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_queries_of_any_size(dtype, tiny, huge, rows):
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(13, [90], [6], 2, 1, 64, dtype)
     rng = np.random.default_rng(0)
     q = b.q.double().numpy()
@@ -274,7 +298,13 @@ def test_queries_of_any_size(dtype, tiny, huge):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-def test_tokens_without_a_number_reach_only_rows_that_see_them(dtype):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_tokens_without_a_number_reach_only_rows_that_see_them(dtype, rows):
+    with lce.tuning(kv4_rows=rows):
+        tokens_without_a_number(dtype)
+
+
+def tokens_without_a_number(dtype):
     odd = [(0, 70, 0, 5, "k", NAN), (0, 95, 1, 3, "v", INF), (1, 0, 0, 60, "v", NAN)]
     b = Batch(14, [100, 80], [40, 3], 4, 2, 64, dtype, odd=odd)
     out, lse = lce.kv4_attention(*b.device(lce), return_lse=True)
@@ -294,7 +324,9 @@ def test_tokens_without_a_number_reach_only_rows_that_see_them(dtype):
 
 
 @pytest.mark.parametrize("value", [NAN, INF, -INF])
-def test_query_rows_without_a_number(value):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_query_rows_without_a_number(value, rows):
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(15, [70, 9], [2, 1], 4, 2, 128, "bf16")
     clean = attend(b)[0]
     b.q[1, 2, 77] = value
@@ -304,7 +336,9 @@ def test_query_rows_without_a_number(value):
     assert torch.equal(out, clean)
 
 
-def test_pages_outside_the_cache_are_hidden():
+@pytest.mark.parametrize("rows", [16, 128])
+def test_pages_outside_the_cache_are_hidden(rows):
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(16, [200], [2], 4, 2, 64, "bf16")
     cache, q, table, start, lengths = b.device(lce)
     for bad in (-1, b.cache.pages, 2 ** 31 - 1, -2 ** 31):
@@ -315,8 +349,10 @@ def test_pages_outside_the_cache_are_hidden():
         assert not (lce.kv4_select(cache, q, table, start, lengths, 4) == 1).any()
 
 
-def test_array_values_outside_their_range():
+@pytest.mark.parametrize("rows", [16, 128])
+def test_array_values_outside_their_range(rows):
     """q_start and lengths are forced into range on the device; other rows stay as they are."""
+    lce.set_tuning(kv4_rows=rows)
     b = Batch(17, [100, 64], [2, 1], 4, 2, 64, "f16")
     cache, q, table, start, lengths = b.device(lce)
     want = lce.kv4_attention(cache, q, table, start, lengths)
