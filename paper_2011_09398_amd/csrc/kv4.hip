@@ -90,13 +90,20 @@ int64_t most_pages(const lce_kv4_query_desc &q) {
 }
 
 // Whether the tiles of attention are of 128 query rows.  They take a page's values
-// out of 4 bits once for 128 rows instead of 16, but a tile that is not full does
-// all of its work.
+// out of 4 bits once for 128 rows instead of 16, but there are an eighth as many, and
+// fewer of them than run at a time (512) leave CUs without work.  Measured (us, tiles
+// of 16 / 128, bfloat16, 32 heads of 128 on 8, 4000 tokens before the new ones): one
+// sequence of 1024 new tokens 111 / 132 (256 workgroups of 128 rows), of 2048 235 /
+// 176 (512), of 4096 503 / 382; four of up to 512 92 / 126, of 1024 180 / 166, of 2048
+// 340 / 246; sixteen of up to 256 139 / 161, of 512 245 / 233.  In float16, which takes
+// three pieces of a query and more registers: four of up to 1024 193 / 222, of 2048
+// 361 / 342, one of 4096 550 / 527.
 bool wide_tiles(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
-    if (q.list > 0) return false;
+    if (q.list > 0 || d.head_dim > 128) return false;
     if (const int t = tuning(LCE_TUNE_KV4_ROWS)) return t == 128;
     const int64_t most = q.max_q > 0 ? q.max_q : q.tokens / q.seqs;
-    return most * (q.q_heads / d.kv_heads) >= 64;
+    if (most * (q.q_heads / d.kv_heads) < 128) return false;   // tiles would not be full
+    return (int64_t)q.tokens * q.q_heads / 128 >= (q.type == LCE_FLOAT16 ? 1024 : 512);
 }
 
 struct Split {
