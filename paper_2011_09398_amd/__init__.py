@@ -744,6 +744,16 @@ class KV4Cache:
         self.data, self.pages, self.kv_heads, self.head_dim = data, pages, kv_heads, head_dim
         self._ref = ctypes.byref(self.desc)
         self._ptr = data.data_ptr()
+        # what every call compares its tensors with
+        self._index = data.get_device()
+        self._int32, self._int64 = torch.int32, torch.int64
+        self._uint8, self._float32 = torch.uint8, torch.float32
+        self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+    def _holds(self, t, dtype) -> bool:
+        """Whether t is a contiguous `dtype` tensor on the cache's device: the quick
+        check; _require_like says what is wrong."""
+        return (t.dtype is dtype and t.get_device() == self._index and t.is_contiguous())
 
 
 def _require_like(t, dtype, device, name):
@@ -777,26 +787,44 @@ def _require_heads(t, cache, name):
         raise ValueError(f"{name}'s channels must be contiguous")
 
 
-def kv4_append(cache: KV4Cache, k, v, slots) -> None:
-    """Quantize k and v [tokens, kv_heads, head_dim] (float32, float16 or bfloat16; any
-    token and head strides that are multiples of 16 bytes) into the cache's `slots`
-    (int64 [tokens]; a slot outside the cache drops its token)."""
+def _append_refused(cache, k, v, slots):
+    """Raises for what kv4_append does not take."""
     import torch
     _require_cache(cache)
     _require_heads(k, cache, "k")
     _require_heads(v, cache, "v")
-    n = k.shape[0]
     if k.shape != v.shape or k.shape[1] != cache.kv_heads:
         raise ValueError(f"k and v must be [tokens, {cache.kv_heads}, {cache.head_dim}], got "
                          f"{list(k.shape)} and {list(v.shape)}")
     if k.dtype != v.dtype:
         raise TypeError(f"k and v must have one dtype, got {k.dtype} and {v.dtype}")
+    _float_type(k.dtype, "k")
     _require_like(slots, torch.int64, cache.data.device, "slots")
-    if slots.shape != (n,):
-        raise ValueError(f"slots must have {n} elements")
-    _check(lib().lce_kv4_append(cache._ref, cache._ptr, _float_type(k.dtype, "k"), k.data_ptr(),
-                                k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
-                                slots.data_ptr(), n, _stream_handle(k)))
+    if slots.shape != k.shape[:1]:
+        raise ValueError(f"slots must have {k.shape[0]} elements")
+
+
+def kv4_append(cache: KV4Cache, k, v, slots) -> None:
+    """Quantize k and v [tokens, kv_heads, head_dim] (float32, float16 or bfloat16; any
+    token and head strides that are multiples of 16 bytes) into the cache's `slots`
+    (int64 [tokens]; a slot outside the cache drops its token)."""
+    try:
+        n, heads, dim = k.shape
+        ks, vs = k.stride(), v.stride()
+        dtype = k.dtype
+        code = cache._types.get(dtype, -1)
+        fine = (code >= 0 and heads == cache.kv_heads and dim == cache.head_dim
+                and v.shape == k.shape and v.dtype is dtype
+                and ks[2] == vs[2] == 1 and k.get_device() == v.get_device() == cache._index
+                and cache._holds(slots, cache._int64) and slots.shape == (n,))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _append_refused(cache, k, v, slots)
+    st = lib().lce_kv4_append(cache._ref, cache._ptr, code, k.data_ptr(), ks[0], ks[1],
+                              v.data_ptr(), vs[0], vs[1], slots.data_ptr(), n, _stream_handle(k))
+    if st != LCE_OK:
+        raise LceError(st, last_error())
 
 
 def kv4_read(cache: KV4Cache, slots, *, dtype=None, out=None):
@@ -805,47 +833,69 @@ def kv4_read(cache: KV4Cache, slots, *, dtype=None, out=None):
     `out`.  Slots outside the cache read as zeros."""
     import torch
     _require_cache(cache)
-    _require_like(slots, torch.int64, cache.data.device, "slots")
+    if not isinstance(slots, torch.Tensor) or not cache._holds(slots, torch.int64):
+        _require_like(slots, torch.int64, cache.data.device, "slots")
     if slots.dim() != 1:
         raise ValueError("slots must have one dimension")
-    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    n = slots.shape[0]
     if out is None:
         if dtype is None:
             dtype = torch.bfloat16
         code = _float_type(dtype, "dtype")
-        k = torch.empty(shape, dtype=dtype, device=slots.device)
-        v = torch.empty(shape, dtype=dtype, device=slots.device)
+        k = slots.new_empty((n, cache.kv_heads, cache.head_dim), dtype=dtype)
+        v = torch.empty_like(k)
     else:
         k, v = out
+        shape = (n, cache.kv_heads, cache.head_dim)
         for t, name in ((k, "out[0]"), (v, "out[1]")):
             _require_like(t, k.dtype if dtype is None else dtype, slots.device, name)
             if t.shape != shape:
                 raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
         code = _float_type(k.dtype, "out")
-    _check(lib().lce_kv4_read(cache._ref, cache._ptr, slots.data_ptr(), shape[0], code,
-                              k.data_ptr(), v.data_ptr(), _stream_handle(slots)))
+    st = lib().lce_kv4_read(cache._ref, cache._ptr, slots.data_ptr(), n, code, k.data_ptr(),
+                            v.data_ptr(), _stream_handle(slots))
+    if st != LCE_OK:
+        raise LceError(st, last_error())
     return k, v
 
 
-def _kv4_query(cache, q, table, q_start, lengths, *, causal, window, count, max_q, max_len, scale):
-    """Checks the arguments that attention and selection share; their descriptor."""
+def _query_refused(cache, q, table, q_start, lengths):
+    """Raises for what attention and selection do not take."""
     import torch
     _require_cache(cache)
     _require_heads(q, cache, "q")
     device = cache.data.device
+    _require_like(table, torch.int32, device, "table")
     if table.dim() != 2:
         raise ValueError("table must be [sequences, pages]")
-    seqs, width = table.shape
-    for t, name, shape in ((table, "table", table.shape), (q_start, "q_start", (seqs + 1,)),
-                           (lengths, "lengths", (seqs,))):
+    for t, name, n in ((q_start, "q_start", table.shape[0] + 1),
+                       (lengths, "lengths", table.shape[0])):
         _require_like(t, torch.int32, device, name)
-        if t.shape != shape:
-            raise ValueError(f"{name} must have {shape[0]} elements, got {list(t.shape)}")
+        if t.shape != (n,):
+            raise ValueError(f"{name} must have {n} elements, got {list(t.shape)}")
     if q.dtype == torch.float32:
         raise TypeError("q must be float16 or bfloat16, got torch.float32")
-    return KV4QueryDesc(q.shape[0], q.shape[1], seqs, width, _float_type(q.dtype, "q"),
-                        1 if causal else 0, window, count, max_q or 0, max_len or 0, scale,
-                        q.stride(0), q.stride(1))
+    _float_type(q.dtype, "q")
+
+
+def _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, max_len, scale):
+    """Checks the arguments that attention and selection share; their descriptor."""
+    try:
+        tokens, heads, dim = q.shape
+        seqs, width = table.shape
+        strides = q.stride()
+        code = cache._types.get(q.dtype, 0)
+        i32 = cache._int32
+        fine = (code > 0 and dim == cache.head_dim and strides[2] == 1
+                and q.get_device() == cache._index and cache._holds(table, i32)
+                and cache._holds(q_start, i32) and q_start.shape == (seqs + 1,)
+                and cache._holds(lengths, i32) and lengths.shape == (seqs,))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _query_refused(cache, q, table, q_start, lengths)
+    return KV4QueryDesc(tokens, heads, seqs, width, code, 1 if causal else 0, window, count,
+                        max_q or 0, max_len or 0, scale, strides[0], strides[1])
 
 
 def kv4_workspace(cache: KV4Cache, q, table):
@@ -883,31 +933,36 @@ def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optiona
     listed (negative: none).  max_q and max_len, the most new tokens and the longest
     length, help to split the work.  Returns out, or (out, lse float32 [tokens, q_heads]).
     """
-    import torch
-    count = 0
-    if pages is not None:
-        _require_like(pages, torch.int32, cache.data.device, "pages")
-        if pages.dim() != 3 or pages.shape[:2] != (q.shape[0], cache.kv_heads) or not pages.shape[2]:
-            raise ValueError(f"pages must be [{q.shape[0]}, {cache.kv_heads}, n], got "
-                             f"{list(pages.shape)}")
-        count = pages.shape[2]
-    d = _kv4_query(cache, q, table, q_start, lengths, causal=causal, window=window, count=count,
-                   max_q=max_q, max_len=max_len,
-                   scale=cache.head_dim ** -0.5 if scale is None else scale)
+    count = 0 if pages is None else _list_length(cache, q, pages)
+    d = _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, max_len,
+                   cache.head_dim ** -0.5 if scale is None else scale)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     else:
         _require_like(out, q.dtype, q.device, "out")
         if out.shape != q.shape:
             raise ValueError(f"out must be {list(q.shape)}, got {list(out.shape)}")
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    ws = _workspace(workspace, cache, q, table)
-    _check(lib().lce_kv4_attention(
+    lse = q.new_empty(q.shape[:2], dtype=cache._float32) if return_lse else None
+    if workspace is None or not cache._holds(workspace, cache._uint8):
+        workspace = _workspace(workspace, cache, q, table)
+    st = lib().lce_kv4_attention(
         cache._ref, cache._ptr, ctypes.byref(d), q.data_ptr(), table.data_ptr(),
         q_start.data_ptr(), lengths.data_ptr(), None if pages is None else pages.data_ptr(),
-        out.data_ptr(), None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(),
-        _stream_handle(q)))
+        out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+        workspace.numel(), _stream_handle(q))
+    if st != LCE_OK:
+        raise LceError(st, last_error())
     return (out, lse) if return_lse else out
+
+
+def _list_length(cache, q, pages):
+    import torch
+    _require_cache(cache)
+    _require_like(pages, torch.int32, cache.data.device, "pages")
+    if pages.dim() != 3 or pages.shape[:2] != (q.shape[0], cache.kv_heads) or not pages.shape[2]:
+        raise ValueError(f"pages must be [{q.shape[0]}, {cache.kv_heads}, n], got "
+                         f"{list(pages.shape)}")
+    return pages.shape[2]
 
 
 def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_first: int = 1,
@@ -916,21 +971,22 @@ def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_
     """The `count` pages of each token and cache head whose key signs agree best with the
     query signs (lce_kv4_select): int32 [tokens, kv_heads, count], ascending, then -1.
     The first keep_first and the last keep_last pages are always among them."""
-    import torch
-    d = _kv4_query(cache, q, table, q_start, lengths, causal=causal, window=window, count=count,
-                   max_q=None, max_len=max_len, scale=1.0)
+    d = _kv4_query(cache, q, table, q_start, lengths, causal, window, count, None, max_len, 1.0)
     shape = (q.shape[0], cache.kv_heads, count)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int32, device=q.device)
+        out = table.new_empty(shape)
     else:
-        _require_like(out, torch.int32, q.device, "out")
+        _require_like(out, table.dtype, q.device, "out")
         if out.shape != shape:
             raise ValueError(f"out must be {list(shape)}, got {list(out.shape)}")
-    ws = _workspace(workspace, cache, q, table)
-    _check(lib().lce_kv4_select(
+    if workspace is None or not cache._holds(workspace, cache._uint8):
+        workspace = _workspace(workspace, cache, q, table)
+    st = lib().lce_kv4_select(
         cache._ref, cache._ptr, ctypes.byref(d), q.data_ptr(), table.data_ptr(),
         q_start.data_ptr(), lengths.data_ptr(), keep_first, keep_last, out.data_ptr(),
-        ws.data_ptr(), ws.numel(), _stream_handle(q)))
+        workspace.data_ptr(), workspace.numel(), _stream_handle(q))
+    if st != LCE_OK:
+        raise LceError(st, last_error())
     return out
 
 

@@ -418,6 +418,59 @@ def test_streams_and_graphs():
             assert torch.equal(pages, chosen) and torch.equal(out, want), i
 
 
+def test_the_binding_says_what_is_wrong():
+    b = Batch(26, [70, 3], [2, 1], 4, 2, 64, "bf16")
+    cache, q, table, start, lengths = b.device(lce)
+    k = torch.zeros(3, 2, 64, device="cuda")
+    slots = torch.arange(3, device="cuda")
+    lce.kv4_append(cache, k[:0], k[:0], slots[:0])
+    for bad, error in (((k.double(), k.double(), slots), TypeError), ((k, k.half(), slots), TypeError),
+                       ((k, k[:2], slots), ValueError), ((k[:, :1], k[:, :1], slots), ValueError),
+                       ((k, k, slots.int()), TypeError), ((k, k, slots[:2]), ValueError),
+                       ((k, k, slots.cpu()), ValueError), ((k.cpu(), k, slots), ValueError),
+                       ((k, k, [0, 1, 2]), TypeError), ((None, k, slots), TypeError),
+                       ((k[0], k[0], slots), ValueError),
+                       ((k.transpose(1, 2).contiguous().transpose(1, 2), k, slots), ValueError)):
+        with pytest.raises(error):
+            lce.kv4_append(cache, *bad)
+    odd = torch.zeros(3, 2, 65, device="cuda")[:, :, :64]
+    with pytest.raises(lce.LceError):
+        lce.kv4_append(cache, odd, odd, slots)
+    good = dict(q=q, table=table, q_start=start, lengths=lengths)
+    for name, value, error in (("q", q.float(), TypeError), ("q", q.cpu(), ValueError),
+                               ("q", q[:, :, :32], ValueError), ("q", q[0], ValueError),
+                               ("q", None, TypeError), ("table", table.long(), TypeError),
+                               ("table", table[0], ValueError), ("table", table[:, :1], ValueError),
+                               ("q_start", start[:2], ValueError), ("q_start", start.cpu(), ValueError),
+                               ("lengths", lengths[:1], ValueError), ("lengths", [70, 3], TypeError)):
+        with pytest.raises(error):
+            lce.kv4_attention(cache, **{**good, name: value})
+        with pytest.raises(error):
+            lce.kv4_select(cache, **{**good, name: value}, count=2)
+    with pytest.raises(lce.LceError):
+        lce.kv4_attention(cache, q[:, :3].contiguous(), table, start, lengths)
+    with pytest.raises(lce.LceError):
+        lce.kv4_select(cache, *good.values(), 0)
+    for kw in (dict(out=q.float()), dict(out=q[:2]), dict(pages=table[:, None]),
+               dict(workspace=torch.zeros(10, device="cuda")), dict(pages=torch.zeros(3, 2, 0).int().cuda())):
+        with pytest.raises((TypeError, ValueError)):
+            lce.kv4_attention(cache, **good, **kw)
+    with pytest.raises(lce.LceError):
+        lce.kv4_attention(cache, **good, workspace=torch.zeros(10, dtype=torch.uint8, device="cuda"))
+    for kw in (dict(dtype=torch.int32), dict(out=(k, k[:2])), dict(out=(k.cpu(), k))):
+        with pytest.raises((TypeError, ValueError)):
+            lce.kv4_read(cache, slots, **kw)
+    with pytest.raises(TypeError):
+        lce.kv4_read(cache, slots.int())
+    with pytest.raises(ValueError):
+        lce.kv4_read(cache, slots[None])
+    with pytest.raises(ValueError):
+        lce.KV4Cache(2, 64, data=torch.zeros(3, 2, 64, dtype=torch.uint8, device="cuda"))
+    out = torch.empty(3, 2, 64, device="cuda"), torch.empty(3, 2, 64, device="cuda")
+    assert lce.kv4_read(cache, slots, out=out)[0] is out[0]
+    assert torch.equal(out[0], lce.kv4_read(cache, slots, dtype=torch.float32)[0])
+
+
 # ---- lists of pages, and choosing them
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
