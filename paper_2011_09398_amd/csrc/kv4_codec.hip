@@ -164,56 +164,55 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
 
 namespace {
 
-template <typename T>
-struct Out8;
+// Eight values stored; LONG: past the caches.
+template <bool LONG, typename V>
+__device__ __forceinline__ void store16(void *p, const V &v) {
+    if constexpr (LONG)
+        __builtin_nontemporal_store(v, static_cast<V *>(p));
+    else
+        *static_cast<V *>(p) = v;
+}
 
-template <>
-struct Out8<float> {
-    static __device__ __forceinline__ void store(float *p, uint32_t c, float s) {
-        f32x4 a, b;
-        f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0);
-        a[0] = x[0], a[1] = x[1];
-        x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
-        a[2] = x[0], a[3] = x[1];
-        x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2);
-        b[0] = x[0], b[1] = x[1];
-        x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
-        b[2] = x[0], b[3] = x[1];
-        reinterpret_cast<f32x4 *>(p)[0] = a;
-        reinterpret_cast<f32x4 *>(p)[1] = b;
+// Stores the eight values of each of the L lanes of a token at `p`, the token's
+// first channel; every lane of the wave takes part.  Two bytes a value: a lane's
+// eight are 16 bytes.  Four: a lane stores four values of the token's first half
+// and four of its second, whose codes other lanes hold, so that a store of the
+// wave is whole lines here too.
+template <typename T, int L, bool LONG>
+__device__ __forceinline__ void store_values(T *p, int l, uint32_t c, uint32_t scale, bool valid) {
+    if constexpr (__is_same(T, float)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int from = (threadIdx.x & 63) / L * L + (l + j * L) / 2;
+            const uint32_t w = (uint32_t)__shfl((int)c, from) >> (l % 2 * 16);
+            const float s = scale_of((uint32_t)__shfl((int)scale, from));
+            const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0);
+            const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+            if (valid) store16<LONG>(p + 4 * (l + j * L), f32x4{x[0], x[1], y[0], y[1]});
+        }
+    } else {
+        const float s = scale_of(scale);
+        u32x4 w;
+        if constexpr (__is_same(T, __bf16))
+            w = u32x4{bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0)),
+                      bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1)),
+                      bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2)),
+                      bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3))};
+        else
+            w = u32x4{bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 0)),
+                      bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 1)),
+                      bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 2)),
+                      bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 3))};
+        if (valid) store16<LONG>(p + 8 * l, w);
     }
-};
-
-template <>
-struct Out8<__bf16> {
-    static __device__ __forceinline__ void store(__bf16 *p, uint32_t c, float s) {
-        u32x4 a;
-        a[0] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
-        a[1] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
-        a[2] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
-        a[3] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-        *reinterpret_cast<u32x4 *>(p) = a;
-    }
-};
-
-template <>
-struct Out8<_Float16> {
-    static __device__ __forceinline__ void store(_Float16 *p, uint32_t c, float s) {
-        u32x4 a;
-        a[0] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 0));
-        a[1] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 1));
-        a[2] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 2));
-        a[3] = bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, 3));
-        *reinterpret_cast<u32x4 *>(p) = a;
-    }
-};
+}
 
 }  // namespace
 
 // The same split for reading: one thread per eight channels, 4 bytes of codes
 // and one scale of each of key and value in, eight elements of each out.
 // Bound by memory, mostly its writes.
-template <typename T, int D, int U>
+template <typename T, int D, int U, bool LONG>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadParams p) {
     constexpr int L = D / 8, N = kThreads / L;
     const int l = threadIdx.x % L, head = blockIdx.x % p.kv_heads, g = l / 4;
@@ -243,10 +242,9 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadParams p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t i = first + u * N;
-        if (i >= p.tokens) continue;
-        const int64_t at = (i * p.kv_heads + head) * D + 8 * l;
-        Out8<T>::store((T *)p.k + at, kc[u], scale_of(ks[u]));
-        Out8<T>::store((T *)p.v + at, vc[u], scale_of(vs[u]));
+        const int64_t at = (i * p.kv_heads + head) * D;
+        store_values<T, L, LONG>((T *)p.k + at, l, kc[u], ks[u], i < p.tokens);
+        store_values<T, L, LONG>((T *)p.v + at, l, vc[u], vs[u], i < p.tokens);
     }
 }
 
@@ -259,6 +257,7 @@ bool four_per_thread(int64_t tokens, int heads, int dim) {
     return tokens * heads * (dim / 8) >= (int64_t)1024 * kThreads * 4;
 }
 
+// Workgroups of u tokens a thread, of one head.
 template <typename P>
 dim3 grid_of(const P &p, int dim, int u) {
     const int64_t per = (int64_t)kThreads / (dim / 8) * u;
@@ -273,12 +272,19 @@ void launch_append_d(const AppendParams &p, hipStream_t s) {
         hipLaunchKernelGGL((append_kernel<T, D, 1>), grid_of(p, D, 1), dim3(kThreads), 0, s, p);
 }
 
+// Results of more than 100 MB are stored past the caches, which would not hold them
+// for whoever reads them next.  Measured, bfloat16, 8 heads of 128 (us, with and
+// without; then with a pass over the keys behind it): 98 MB 20.4, 19.9 (36.7,
+// 37.5), 134 MB 31.2, 26.2 (51.4, 49.3), 268 MB 76.3, 50.4.
 template <typename T, int D>
 void launch_read_d(const ReadParams &p, hipStream_t s) {
-    if (four_per_thread(p.tokens, p.kv_heads, D))
-        hipLaunchKernelGGL((read_kernel<T, D, 4>), grid_of(p, D, 4), dim3(kThreads), 0, s, p);
+    const int64_t bytes = p.tokens * p.kv_heads * 2 * D * (int64_t)sizeof(T);
+    if (bytes > 100 << 20)
+        hipLaunchKernelGGL((read_kernel<T, D, 4, true>), grid_of(p, D, 4), dim3(kThreads), 0, s, p);
+    else if (four_per_thread(p.tokens, p.kv_heads, D))
+        hipLaunchKernelGGL((read_kernel<T, D, 4, false>), grid_of(p, D, 4), dim3(kThreads), 0, s, p);
     else
-        hipLaunchKernelGGL((read_kernel<T, D, 1>), grid_of(p, D, 1), dim3(kThreads), 0, s, p);
+        hipLaunchKernelGGL((read_kernel<T, D, 1, false>), grid_of(p, D, 1), dim3(kThreads), 0, s, p);
 }
 
 template <typename T>

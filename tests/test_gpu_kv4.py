@@ -84,6 +84,24 @@ def test_long_append_and_read_take_four_tokens_a_thread():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_reads_of_more_than_the_caches_hold(dtype):
+    """The same values as in smaller pieces."""
+    heads, dim, pages = 8, 256, 205
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    data = torch.randint(0, 256, (pages, heads, 76 * dim), dtype=torch.uint8, device="cuda",
+                         generator=g)
+    data[:, :, 64 * dim:68 * dim] = data[:, :, 64 * dim:68 * dim] % 16 + 120
+    cache = lce.KV4Cache(heads, dim, data=data)
+    slots = torch.randperm(pages * PAGE, device="cuda", generator=g)
+    k, v = lce.kv4_read(cache, slots, dtype=DTYPES[dtype])
+    assert k.numel() * k.element_size() * 2 > 100 << 20
+    for at in range(0, len(slots), 1500):
+        a, b = lce.kv4_read(cache, slots[at:at + 1500], dtype=DTYPES[dtype])
+        assert torch.equal(k[at:at + 1500], a) and torch.equal(v[at:at + 1500], b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_append_takes_strided_rows_and_drops_slots_outside(dtype):
     rng = np.random.default_rng(5)
     heads, dim, tokens, pages = 2, 64, 33, 2
