@@ -525,8 +525,9 @@ typedef enum {
     LCE_TUNE_KV4_CHUNK = 12,      /* lce_kv4_attention, lce_kv4_select: pages per
                                      workgroup, >= 1 (raised where the workspace has no
                                      room for that many workgroups)                     */
-    LCE_TUNE_KV4_ROWS = 13,       /* lce_kv4_attention without a list, heads of up to 128
-                                     channels: 16 or 128 query rows per tile            */
+    LCE_TUNE_KV4_ROWS = 13,       /* lce_kv4_attention without a list: 16, 32 or 128 query
+                                     rows per tile, where there is such a kernel (heads
+                                     of up to 128; 32 not of 128 in float16)            */
     LCE_TUNE_COUNT = 14
 } lce_tuning_key;
 

@@ -89,21 +89,30 @@ int64_t most_pages(const lce_kv4_query_desc &q) {
     return n;
 }
 
-// Whether the tiles of attention are of 128 query rows.  They take a page's values
-// out of 4 bits once for 128 rows instead of 16, but there are an eighth as many, and
-// fewer of them than run at a time (512) leave CUs without work.  Measured (us, tiles
-// of 16 / 128, bfloat16, 32 heads of 128 on 8, 4000 tokens before the new ones): one
-// sequence of 1024 new tokens 111 / 132 (256 workgroups of 128 rows), of 2048 235 /
-// 176 (512), of 4096 503 / 382; four of up to 512 92 / 126, of 1024 180 / 166, of 2048
-// 340 / 246; sixteen of up to 256 139 / 161, of 512 245 / 233.  In float16, which takes
-// three pieces of a query and more registers: four of up to 1024 193 / 222, of 2048
-// 361 / 342, one of 4096 550 / 527.
-bool wide_tiles(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
-    if (q.list > 0 || d.head_dim > 128) return false;
-    if (const int t = tuning(LCE_TUNE_KV4_ROWS)) return t == 128;
-    const int64_t most = q.max_q > 0 ? q.max_q : q.tokens / q.seqs;
-    if (most * (q.q_heads / d.kv_heads) < 128) return false;   // tiles would not be full
-    return (int64_t)q.tokens * q.q_heads / 128 >= (q.type == LCE_FLOAT16 ? 1024 : 512);
+// Query rows of a tile of attention.  A tile takes a page's values out of 4 bits once
+// for all its rows, but the more rows it has the fewer tiles there are, and fewer of
+// 128 than run at a time (512) leave CUs without work.  Heads of 256 channels, and
+// 32 rows of 128 in float16 (three pieces of a query, and more registers than there
+// are), stay at 16.  Measured (us, tiles of 16 / 32 / 128, 32 heads on 8, 4000 tokens
+// before the new ones):
+//                                       bfloat16, 128      float16, 64    float16, 128
+//   16 sequences, 64 rows each           24 / 29 /  69
+//   16 sequences, 256 rows each          44 / 41 / 113
+//   one sequence, 1024 new tokens       110 / 94 / 129    85 / 71 / 90   121 / - / 184
+//   one sequence, 2048                  242 / 194 / 177  180 / 150 / 127  263 / - / 261
+//   one sequence, 4096                  517 / 415 / 390  386 / 317 / 269  559 / - / 526
+//   four sequences, up to 512 each       93 / 84 / 126    71 / 66 / 91   101 / - / 177
+//   four sequences, up to 1024          175 / 151 / 161  134 / 118 / 113  198 / - / 220
+//   four sequences, up to 2048          338 / 278 / 246  259 / 216 / 173  380 / - / 341
+int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
+    if (d.head_dim > 128) return 16;
+    const bool large = d.head_dim == 128 && q.type == LCE_FLOAT16;
+    const int forced = tuning(LCE_TUNE_KV4_ROWS);
+    if (q.list || forced == 16) return 16;
+    if (forced == 128 || (forced == 32 && !large)) return forced;
+    const int64_t most = (q.max_q > 0 ? q.max_q : q.tokens / q.seqs) * (int64_t)(q.q_heads / d.kv_heads);
+    if (most >= 128 && (int64_t)q.tokens * q.q_heads / 128 >= (large ? 1024 : 512)) return 128;
+    return most >= 256 && !large ? 32 : 16;
 }
 
 struct Split {
@@ -246,13 +255,15 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
                     (long long)need);
 
     const bool list = query->list > 0;
-    const bool wide = wide_tiles(*desc, *query);
-    const int64_t units = tiles(*desc, *query, wide ? 128 : 16, list) * desc->kv_heads;
+    const int rows = tile_rows(*desc, *query);
+    const int64_t units = tiles(*desc, *query, rows, list) * desc->kv_heads;
     const double size = desc->head_dim / 128.0;
     const Split s =
-        wide ? split_pages(units, most_pages(*query), 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8)
-             : split_pages(units, list ? query->list : most_pages(*query), 0.25 + 0.4 * size,
-                           1 + 2.5 * size, 512, kMostParts);
+        rows == 128
+            ? split_pages(units, most_pages(*query), 2 + 2 * size, 4 + 8 * size, 512,
+                          kMostParts / 8)
+            : split_pages(units, list ? query->list : most_pages(*query), 0.25 + 0.4 * size,
+                          1 + 2.5 * size, 512, kMostParts * 16 / rows);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;
@@ -261,10 +272,10 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + LCE_KV4_WORKSPACE_ZERO);
     p.scale_log2 = query->scale * 1.44269504088896341f;
     const dim3 grid((unsigned)units, (unsigned)s.splits);
-    if (wide)
+    if (rows == 128)
         lce::kv4::launch_attend128(p, query->type, desc->head_dim, grid, stream);
     else
-        lce::kv4::launch_attend16(p, query->type, desc->head_dim, grid, stream);
+        lce::kv4::launch_attend16(p, query->type, desc->head_dim, rows, grid, stream);
     return check_launch("lce_kv4_attention launch");
 }
 

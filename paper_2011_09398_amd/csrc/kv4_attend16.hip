@@ -1,5 +1,5 @@
-// Attention over the 4-bit cache, 16 query rows a tile: single tokens, a few
-// tokens, and lists of pages.
+// Attention over the 4-bit cache, 16 or 32 query rows a tile: single tokens, a few
+// tokens, short prompts, and lists of pages.
 #include "kv4_attend.hpp"
 
 namespace lce {
@@ -7,7 +7,6 @@ namespace kv4 {
 namespace {
 
 constexpr int kWaves = kThreads / 64;
-constexpr int kRows = 16;
 
 // One page of one head as a wave's 64 lanes hold it.  Lane (n, g), n = lane %
 // 16, g = lane / 16: the key codes of tokens 16t + n, 16 bytes of them for each
@@ -209,33 +208,46 @@ __device__ __forceinline__ void decode_values(const Values<D> &r, uint32_t (&eve
     odd[1] = __builtin_amdgcn_perm(x3, x2, 0x07060302u);
 }
 
-template <typename E, int D, int U, int B>
-__device__ __forceinline__ void add_values(RowState<D> &st, const Values<D> &r, const u32x4 &p) {
+template <typename E, int D, int C, int U, int B>
+__device__ __forceinline__ void add_values(RowState<D> (&st)[C], const Values<D> &r,
+                                           const u32x4 (&p)[C][2]) {
     if constexpr (B < D / 32) {
         uint32_t e0[2], o0[2], e1[2], o1[2];
         decode_values<E, D, 2 * U, B>(r, e0, o0);
         decode_values<E, D, 2 * U + 1, B>(r, e1, o1);
-        st.o[2 * B] = E::mfma16(u32x4{e0[0], e0[1], e1[0], e1[1]}, p, st.o[2 * B]);
-        st.o[2 * B + 1] = E::mfma16(u32x4{o0[0], o0[1], o1[0], o1[1]}, p, st.o[2 * B + 1]);
-        add_values<E, D, U, B + 1>(st, r, p);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            st[c].o[2 * B] =
+                E::mfma16(u32x4{e0[0], e0[1], e1[0], e1[1]}, p[c][U], st[c].o[2 * B]);
+            st[c].o[2 * B + 1] =
+                E::mfma16(u32x4{o0[0], o0[1], o1[0], o1[1]}, p[c][U], st[c].o[2 * B + 1]);
+        }
+        add_values<E, D, C, U, B + 1>(st, r, p);
     }
 }
 
 // Hides the tokens outside [lo, hi) (this row's visible ones, counted from the
-// page's first) and makes what the scales of tokens stand for finite: a hidden
-// token's weight is 0, and 0 times its values has to be 0 whatever the page's
-// unwritten bytes are.
-template <typename E, int D>
-__device__ __forceinline__ void hide(f32x4 (&s)[4], Values<D> &r, int lo, int hi, int g) {
+// page's first).
+__device__ __forceinline__ void hide(f32x4 (&s)[4], int lo, int hi, int g) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        uint32_t w = 0;
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int j = 16 * t + 4 * g + i;
             s[t][i] = j >= lo && j < hi ? s[t][i] : -__builtin_inff();
-            w |= min(r.scale[t] >> (8 * i) & 255u, E::kMaxScale) << (8 * i);
         }
+}
+
+// Makes what the scales of tokens stand for finite: a hidden token's weight is 0,
+// and 0 times its values has to be 0 whatever the page's unwritten bytes are.
+template <typename E, int D>
+__device__ __forceinline__ void settle(Values<D> &r) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w |= min(r.scale[t] >> (8 * i) & 255u, E::kMaxScale) << (8 * i);
         r.scale[t] = w;
     }
 }
@@ -276,13 +288,6 @@ __device__ __forceinline__ void weigh(RowState<D> &st, const f32x4 (&s)[4], u32x
     }
 }
 
-template <typename E, int D>
-__device__ __forceinline__ void add_page(RowState<D> &st, const Values<D> &r,
-                                         const u32x4 (&p)[2]) {
-    add_values<E, D, 0, 0>(st, r, p[0]);
-    add_values<E, D, 1, 0>(st, r, p[1]);
-}
-
 // Joins another state of the same rows into this one.
 template <int D>
 __device__ __forceinline__ void join(RowState<D> &a, float m, float l, const f32x4 (&o)[D / 16]) {
@@ -294,28 +299,30 @@ __device__ __forceinline__ void join(RowState<D> &a, float m, float l, const f32
     for (int i = 0; i < D / 16; ++i) a.o[i] = a.o[i] * fa + o[i] * fb;
 }
 
-template <int D>
+template <int D, int C>
 struct Shared {
-    float o[kWaves / 2][D / 16 * 4][64];
-    float m[kWaves / 2][64], l[kWaves / 2][64];
+    float o[kWaves / 2][C][D / 16 * 4][64];
+    float m[kWaves / 2][C][64], l[kWaves / 2][C][64];
     int last;
 };
 
 }  // namespace
 
-// Grid (tiles * kv_heads, splits), four waves.  A tile is 16 rows of one head of
-// the cache: rows are the queries of one sequence times the heads that share
+// Grid (tiles * kv_heads, splits), four waves.  A tile is C times 16 rows of one head
+// of the cache: rows are the queries of one sequence times the heads that share
 // the cache head, in that order (with LIST, those of one token).  The waves take
-// the pages of their workgroup's split in turn, each with the whole 16 rows, and
+// the pages of their workgroup's split in turn, each with all rows, and
 // join their states at the end; the last split of a tile to finish joins all of
 // them, in the order of the splits, so that results do not depend on timing.
 //
 // Keys are the first operand and queries the second, so that a lane's scores
 // belong to one row and the weights leave the softmax as the second operand of
 // the product with the values; no weight and no score crosses lanes.
-template <typename E, int D, bool LIST>
-__global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(AttendParams p) {
-    __shared__ Shared<D> sh;
+template <typename E, int D, bool LIST, int C>
+__global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16_kernel(
+    AttendParams p) {
+    constexpr int kRows = 16 * C;
+    __shared__ Shared<D, C> sh;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % p.kv_heads, slot = blockIdx.x / p.kv_heads, split = blockIdx.y;
@@ -331,7 +338,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
                             [](int s, int) { return (int64_t)s; });
         if (seq.index < 0 || token - seq.start >= seq.queries) return;
     } else {
-        // a sequence's tiles begin at floor(rows before it / 16) + its index:
+        // a sequence's tiles begin at floor(rows before it / kRows) + its index:
         // at most one more than it needs, and none shared
         const auto first = [&](int s, int b) { return (int64_t)s * p.group / kRows + b; };
         seq = find_sequence(p.q_start, p.lengths, p.seqs, p.tokens, p.width, slot, first);
@@ -343,10 +350,17 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     if (row0 >= rows) return;
     const int valid = min(rows - row0, kRows);
     const int base = LIST ? (token - seq.start) * p.group : 0;   // in rows of the sequence
-    const int row = base + row0 + n;
-    const int i = row / p.group, hq = head * p.group + row % p.group;
-    const bool mine = n < valid;
-    const Span span = visible(seq, i, p.causal, p.window);
+    // this lane's row of each sixteen
+    int i[C], hq[C];
+    bool mine[C];
+    Span span[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int row = base + row0 + 16 * c + n;
+        i[c] = row / p.group, hq[c] = head * p.group + row % p.group;
+        mine[c] = 16 * c + n < valid;
+        span[c] = visible(seq, i[c], p.causal, p.window);
+    }
     // spans move up with the rows: the tile's first and last row bound them
     const Span a = visible(seq, (base + row0) / p.group, p.causal, p.window);
     const Span z = visible(seq, (base + row0 + valid - 1) / p.group, p.causal, p.window);
@@ -359,16 +373,18 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     const int begin = split * p.chunk;
     const int end = split == splits - 1 ? count : begin + p.chunk;
 
-    RowState<D> st;
-    st.m = -1e30f;   // finite: a row that has seen nothing weighs exp2(-inf) = 0
-    st.l = 0.0f;
+    RowState<D> st[C];
+    RawQueries<D> raw[C];
 #pragma unroll
-    for (int m = 0; m < D / 16; ++m) st.o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    RawQueries<D> raw;
-    raw.load((const typename E::T *)p.q + (int64_t)(seq.start + i) * p.q_token +
-                 (int64_t)hq * p.q_head,
-             mine, g);
+    for (int c = 0; c < C; ++c) {
+        st[c].m = -1e30f;   // finite: a row that has seen nothing weighs exp2(-inf) = 0
+        st[c].l = 0.0f;
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) st[c].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        raw[c].load((const typename E::T *)p.q + (int64_t)(seq.start + i[c]) * p.q_token +
+                        (int64_t)hq[c] * p.q_head,
+                    mine[c], g);
+    }
     const int32_t *named =
         LIST ? p.named + ((int64_t)(seq.start + base / p.group) * p.kv_heads + head) * p.list
              : nullptr;
@@ -413,14 +429,21 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
         keys.load(rec, n, g);
         values.load(rec, n, g);
     }
-    Queries<E, D> q;
-    make_pieces<E, D>(q, raw, g);
+    Queries<E, D> q[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) make_pieces<E, D>(q[c], raw[c], g);
     bool more = any;
     while (more) {
         const int t0 = number * kPage;
         const bool masked = t0 < z.lo || t0 + kPage > a.hi;
-        f32x4 s[4] = {scores<E, D, 0>(keys, q), scores<E, D, 1>(keys, q),
-                      scores<E, D, 2>(keys, q), scores<E, D, 3>(keys, q)};
+        f32x4 s[C][4];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            s[c][0] = scores<E, D, 0>(keys, q[c]);
+            s[c][1] = scores<E, D, 1>(keys, q[c]);
+            s[c][2] = scores<E, D, 2>(keys, q[c]);
+            s[c][3] = scores<E, D, 3>(keys, q[c]);
+        }
         fetch();
         more = todo != 0;
         const uint8_t *rec = nullptr;
@@ -428,51 +451,69 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
             rec = next(number);
             keys.load(rec, n, g);
         }
-        if (masked) hide<E, D>(s, values, span.lo - t0, span.hi - t0, g);
-        u32x4 w[2];
-        weigh<E, D>(st, s, w, p.scale_log2);
-        add_page<E, D>(st, values, w);
+        if (masked) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) hide(s[c], span[c].lo - t0, span[c].hi - t0, g);
+            settle<E, D>(values);
+        }
+        u32x4 w[C][2];
+#pragma unroll
+        for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], p.scale_log2);
+        add_values<E, D, C, 0, 0>(st, values, w);
+        add_values<E, D, C, 1, 0>(st, values, w);
         if (more) values.load(rec, n, g);
     }
-    st.l = across_rows(st.l, [](float x, float y) { return x + y; });
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        st[c].l = across_rows(st[c].l, [](float x, float y) { return x + y; });
 
     // join the waves: the upper half into the lower one, until one is left
 #pragma unroll
     for (int half = kWaves / 2; half > 0; half /= 2) {
         if (wave >= half && wave < 2 * half) {
-            sh.m[wave - half][lane] = st.m;
-            sh.l[wave - half][lane] = st.l;
 #pragma unroll
-            for (int m = 0; m < D / 16; ++m)
+            for (int c = 0; c < C; ++c) {
+                sh.m[wave - half][c][lane] = st[c].m;
+                sh.l[wave - half][c][lane] = st[c].l;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sh.o[wave - half][4 * m + j][lane] = st.o[m][j];
+                for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        sh.o[wave - half][c][4 * m + j][lane] = st[c].o[m][j];
+            }
         }
         __syncthreads();
         if (wave < half) {
-            f32x4 o[D / 16];
 #pragma unroll
-            for (int m = 0; m < D / 16; ++m)
+            for (int c = 0; c < C; ++c) {
+                f32x4 o[D / 16];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[m][j] = sh.o[wave][4 * m + j][lane];
-            join<D>(st, sh.m[wave][lane], sh.l[wave][lane], o);
+                for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[m][j] = sh.o[wave][c][4 * m + j][lane];
+                join<D>(st[c], sh.m[wave][c][lane], sh.l[wave][c][lane], o);
+            }
         }
         __syncthreads();
     }
 
     if (splits == 1) {
-        if (wave == 0 && mine) {
-            const float inv = st.l == 0.0f ? 0.0f : 1.0f / st.l;
-            const int64_t at = (int64_t)(seq.start + i) * (p.kv_heads * p.group) + hq;
+        if (wave != 0) return;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (!mine[c]) continue;
+            const float l = st[c].l, inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int64_t at = (int64_t)(seq.start + i[c]) * (p.kv_heads * p.group) + hq[c];
             typename E::T *out = (typename E::T *)p.out + at * D + D / 16 * 4 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int m = 0; m < D / 16; m += 2)
                     *reinterpret_cast<uint32_t *>(out + D / 16 * j + m) =
-                        pack_pair<E>(st.o[m][j] * inv, st.o[m + 1][j] * inv);
+                        pack_pair<E>(st[c].o[m][j] * inv, st[c].o[m + 1][j] * inv);
             if (p.lse && g == 0)
-                p.lse[at] = st.l == 0.0f ? -__builtin_inff()
-                                         : (st.m + __builtin_log2f(st.l)) * 0.69314718055994531f;
+                p.lse[at] = l == 0.0f ? -__builtin_inff()
+                                      : (st[c].m + __builtin_log2f(l)) * 0.69314718055994531f;
         }
         return;
     }
@@ -483,16 +524,19 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
     float *part = p.part + (int64_t)blockIdx.x * gridDim.y * P::kFloats;
     if (wave == 0) {
         float *my = part + (int64_t)split * P::kFloats;
-        if (mine) {
-            if (g == 0) put(my + P::state(n), f32x2{st.m, st.l});
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if (!mine[c]) continue;
+            const int row = 16 * c + n;
+            if (g == 0) put(my + P::state(row), f32x2{st[c].m, st[c].l});
             // quad (j, m / 4, g): channels D/16 * (4g + j) + m .. m + 3
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int m = 0; m < D / 16; m += 4) {
-                    float *to = my + P::sums(valid, n, (j * (D / 64) + m / 4) * 4 + g);
-                    put(to, f32x2{st.o[m][j], st.o[m + 1][j]});
-                    put(to + 2, f32x2{st.o[m + 2][j], st.o[m + 3][j]});
+                    float *to = my + P::sums(valid, row, (j * (D / 64) + m / 4) * 4 + g);
+                    put(to, f32x2{st[c].o[m][j], st[c].o[m + 1][j]});
+                    put(to + 2, f32x2{st[c].o[m + 2][j], st[c].o[m + 3][j]});
                 }
         }
         if (lane == 0) sh.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
@@ -523,26 +567,39 @@ __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void attend16_kernel(At
 
 namespace {
 
+template <typename E, int D, int C>
+void launch_c(const AttendParams &p, dim3 grid, hipStream_t s) {
+    if constexpr (C == 1) {
+        if (p.named) {
+            hipLaunchKernelGGL((attend16_kernel<E, D, true, 1>), grid, dim3(kThreads), 0, s, p);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((attend16_kernel<E, D, false, C>), grid, dim3(kThreads), 0, s, p);
+}
+
 template <typename E, int D>
-void launch_d(const AttendParams &p, dim3 grid, hipStream_t s) {
-    if (p.named)
-        hipLaunchKernelGGL((attend16_kernel<E, D, true>), grid, dim3(kThreads), 0, s, p);
-    else
-        hipLaunchKernelGGL((attend16_kernel<E, D, false>), grid, dim3(kThreads), 0, s, p);
+void launch_d(const AttendParams &p, int rows, dim3 grid, hipStream_t s) {
+    // 32 rows of 128 channels in float16, or of 256, have more state than registers
+    if constexpr (D * E::kPieces <= 256) {
+        if (rows == 32) return launch_c<E, D, 2>(p, grid, s);
+    }
+    launch_c<E, D, 1>(p, grid, s);
 }
 
 template <typename E>
-void launch_t(const AttendParams &p, int dim, dim3 grid, hipStream_t s) {
-    if (dim == 64) launch_d<E, 64>(p, grid, s);
-    else if (dim == 128) launch_d<E, 128>(p, grid, s);
-    else launch_d<E, 256>(p, grid, s);
+void launch_t(const AttendParams &p, int dim, int rows, dim3 grid, hipStream_t s) {
+    if (dim == 64) launch_d<E, 64>(p, rows, grid, s);
+    else if (dim == 128) launch_d<E, 128>(p, rows, grid, s);
+    else launch_d<E, 256>(p, rows, grid, s);
 }
 
 }  // namespace
 
-void launch_attend16(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s) {
-    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, grid, s);
-    else launch_t<Bf16>(p, dim, grid, s);
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, dim3 grid,
+                     hipStream_t s) {
+    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, rows, grid, s);
+    else launch_t<Bf16>(p, dim, rows, grid, s);
 }
 
 }  // namespace kv4

@@ -51,8 +51,10 @@ struct SelectParams : QueryParams {
 
 void launch_append(const AppendParams &p, int type, int dim, hipStream_t s);
 void launch_read(const ReadParams &p, int type, int dim, hipStream_t s);
-// 16 query rows a workgroup; grid = (tiles * kv_heads, splits)
-void launch_attend16(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);
+// 16 or 32 query rows a workgroup (32: heads of up to 128); grid = (tiles *
+// kv_heads, splits)
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, dim3 grid,
+                     hipStream_t s);
 // 128 query rows a workgroup, no list; grid = (tiles * kv_heads, splits)
 void launch_attend128(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);
 // one token and head of the cache a workgroup; grid = (tokens * kv_heads, splits)

@@ -214,7 +214,7 @@ def test_single_tokens(dim, dtype, q_heads, kv_heads, chunk):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 40), (False, 70), (True, 1)])
 @pytest.mark.parametrize("chunk", [0, 2])
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_several_tokens(dim, dtype, causal, window, chunk, rows):
     lengths, queries = [150, 3, 64, 0, 90, 129], [5, 3, 1, 0, 90, 17]
     b = Batch(dim, lengths, queries, 6, 2, dim, dtype)
@@ -225,17 +225,18 @@ def test_several_tokens(dim, dtype, causal, window, chunk, rows):
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_long_prompts(dim, dtype):
-    """Tiles of 128 rows that are full, that several pages are whole for, and whose last
+    """Tiles of 32 and 128 rows that are full, that several pages are whole for, and whose last
     waves have no rows; sequences shorter than their tile."""
     b = Batch(25, [260, 33, 500, 1], [260, 33, 111, 1], 5, 1, dim, dtype)
     out, lse = attend(b, max_q=260)
     again = lce.kv4_attention(*b.device(lce), max_q=260)
     assert torch.equal(out, again)
-    with lce.tuning(kv4_rows=128, kv4_chunk=1):
-        attend(b, window=77)
+    for rows in (32, 128):
+        with lce.tuning(kv4_rows=rows, kv4_chunk=1):
+            attend(b, window=77)
 
 
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_more_queries_than_tokens_leave_rows_that_see_nothing(rows):
     lce.set_tuning(kv4_rows=rows)
     b = Batch(3, [4, 70], [7, 2], 4, 2, 64, "bf16")
@@ -245,7 +246,7 @@ def test_more_queries_than_tokens_leave_rows_that_see_nothing(rows):
             assert not out[:3].any() and torch.isneginf(lse[:3]).all()
 
 
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_no_sequence_has_tokens(rows):
     lce.set_tuning(kv4_rows=rows)
     b = Batch(3, [0, 0], [2, 1], 4, 2, 128, "f16")
@@ -255,7 +256,7 @@ def test_no_sequence_has_tokens(rows):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_many_sequences_and_long_ones(dtype, rows):
     """More sequences than lanes; one long enough that a wave takes several of its pages."""
     lce.set_tuning(kv4_rows=rows)
@@ -290,7 +291,7 @@ def test_strided_queries_and_scale():
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("spread", [1e-3, 30.0])
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_flat_and_sharp_scores(dtype, spread, rows):
     """Scores that are all alike, and rows that one token takes nearly whole (large maxima that
     rise from page to page)."""
@@ -300,7 +301,7 @@ def test_flat_and_sharp_scores(dtype, spread, rows):
 
 
 @pytest.mark.parametrize("dtype,tiny,huge", [("bf16", 2.0 ** -70, 2.0 ** 60), ("f16", 2.0 ** -22, 2.0 ** 14)])
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_queries_of_any_size(dtype, tiny, huge, rows):
     lce.set_tuning(kv4_rows=rows)
     b = Batch(13, [90], [6], 2, 1, 64, dtype)
@@ -316,7 +317,7 @@ def test_queries_of_any_size(dtype, tiny, huge, rows):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_tokens_without_a_number_reach_only_rows_that_see_them(dtype, rows):
     with lce.tuning(kv4_rows=rows):
         tokens_without_a_number(dtype)
@@ -342,7 +343,7 @@ def tokens_without_a_number(dtype):
 
 
 @pytest.mark.parametrize("value", [NAN, INF, -INF])
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_query_rows_without_a_number(value, rows):
     lce.set_tuning(kv4_rows=rows)
     b = Batch(15, [70, 9], [2, 1], 4, 2, 128, "bf16")
@@ -354,7 +355,7 @@ def test_query_rows_without_a_number(value, rows):
     assert torch.equal(out, clean)
 
 
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_pages_outside_the_cache_are_hidden(rows):
     lce.set_tuning(kv4_rows=rows)
     b = Batch(16, [200], [2], 4, 2, 64, "bf16")
@@ -367,7 +368,7 @@ def test_pages_outside_the_cache_are_hidden(rows):
         assert not (lce.kv4_select(cache, q, table, start, lengths, 4) == 1).any()
 
 
-@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
 def test_array_values_outside_their_range(rows):
     """q_start and lengths are forced into range on the device; other rows stay as they are."""
     lce.set_tuning(kv4_rows=rows)
