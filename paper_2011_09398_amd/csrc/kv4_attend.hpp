@@ -128,7 +128,7 @@ struct Part {
     }
 };
 
-// Joins sums `quad` of a row over all its splits, eight at a time, each with its
+// Joins sums `quad` of a row over all its splits, sixteen at a time, each with its
 // own maximum, against a running one: the sums, their maximum and their weight.
 template <int D, int ROWS>
 __device__ __forceinline__ f32x4 join_splits(const float *part, int splits, int rows, int row,
@@ -137,43 +137,38 @@ __device__ __forceinline__ f32x4 join_splits(const float *part, int splits, int 
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     top = -1e30f;
     l = 0.0f;
-    for (int s0 = 0; s0 < splits; s0 += 8) {
-        f32x2 ml[8];
-        f32x4 y[8];
-        const auto fetch = [&](int k) {
-            const float *from = part + (int64_t)min(s0 + k, splits - 1) * P::kFloats;
-            ml[k] = *reinterpret_cast<const f32x2 *>(from + P::state(row));
-            y[k] = *reinterpret_cast<const f32x4 *>(from + P::sums(rows, row, quad));
-        };
-        const bool many = s0 + 4 < splits;
+    for (int s0 = 0; s0 < splits; s0 += 16) {
+        f32x2 ml[16];
+        f32x4 y[16];
+        // four at a time are there or not: what is past the last split is read again,
+        // and weighs nothing
 #pragma unroll
-        for (int k = 0; k < 4; ++k) fetch(k);
-        if (many) {
-#pragma unroll
-            for (int k = 4; k < 8; ++k) fetch(k);
+        for (int k = 0; k < 16; ++k) {
+            ml[k] = f32x2{-1e30f, 0.0f};
+            y[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        const auto add = [&](int k) {
-            float w = ml[k][0] - top;
-            w = s0 + k < splits ? __builtin_amdgcn_exp2f(w) : 0.0f;
-            l += ml[k][1] * w;
-            o += y[k] * w;
-        };
+#pragma unroll
+        for (int k0 = 0; k0 < 16; k0 += 4)
+            if (s0 + k0 < splits) {
+#pragma unroll
+                for (int k = k0; k < k0 + 4; ++k) {
+                    const float *from = part + (int64_t)min(s0 + k, splits - 1) * P::kFloats;
+                    ml[k] = *reinterpret_cast<const f32x2 *>(from + P::state(row));
+                    y[k] = *reinterpret_cast<const f32x4 *>(from + P::sums(rows, row, quad));
+                }
+            }
         float high = top;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) high = fmaxf(high, ml[k][0]);
-        if (many) {
-#pragma unroll
-            for (int k = 4; k < 8; ++k) high = fmaxf(high, ml[k][0]);
-        }
+        for (int k = 0; k < 16; ++k) high = fmaxf(high, ml[k][0]);
         const float f = __builtin_amdgcn_exp2f(top - high);
         l *= f;
         o *= f;
         top = high;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) add(k);
-        if (many) {
-#pragma unroll
-            for (int k = 4; k < 8; ++k) add(k);
+        for (int k = 0; k < 16; ++k) {
+            const float w = s0 + k < splits ? __builtin_amdgcn_exp2f(ml[k][0] - top) : 0.0f;
+            l += ml[k][1] * w;
+            o += y[k] * w;
         }
     }
     return o;

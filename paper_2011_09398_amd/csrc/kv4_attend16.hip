@@ -288,21 +288,12 @@ __device__ __forceinline__ void weigh(RowState<D> &st, const f32x4 (&s)[4], u32x
     }
 }
 
-// Joins another state of the same rows into this one.
-template <int D>
-__device__ __forceinline__ void join(RowState<D> &a, float m, float l, const f32x4 (&o)[D / 16]) {
-    const float all = fmaxf(a.m, m);
-    const float fa = __builtin_amdgcn_exp2f(a.m - all), fb = __builtin_amdgcn_exp2f(m - all);
-    a.m = all;
-    a.l = a.l * fa + l * fb;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) a.o[i] = a.o[i] * fa + o[i] * fb;
-}
-
+// The waves' states, where they are joined: sums four channels at a time, rows next
+// to each other.
 template <int D, int C>
 struct Shared {
-    float o[kWaves / 2][C][D / 16 * 4][64];
-    float m[kWaves / 2][C][64], l[kWaves / 2][C][64];
+    f32x4 o[kWaves][D / 4][16 * C];
+    f32x2 ml[kWaves][16 * C];
     int last;
 };
 
@@ -417,7 +408,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     };
 
     // Keys and values of one page are in registers at a time: the next page's
-    // keys are on their way once this page's scores are there, its values once
+    // keys are on their way once this page's weights are there, its values once
     // this page's are added.
     fetch();
     Keys<D> keys;
@@ -447,10 +438,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         fetch();
         more = todo != 0;
         const uint8_t *rec = nullptr;
-        if (more) {
-            rec = next(number);
-            keys.load(rec, n, g);
-        }
+        if (more) rec = next(number);
         if (masked) {
 #pragma unroll
             for (int c = 0; c < C; ++c) hide(s[c], span[c].lo - t0, span[c].hi - t0, g);
@@ -459,99 +447,28 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         u32x4 w[C][2];
 #pragma unroll
         for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], p.scale_log2);
+        if (more) keys.load(rec, n, g);
         add_values<E, D, C, 0, 0>(st, values, w);
         add_values<E, D, C, 1, 0>(st, values, w);
         if (more) values.load(rec, n, g);
     }
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        st[c].l = across_rows(st[c].l, [](float x, float y) { return x + y; });
-
-    // join the waves: the upper half into the lower one, until one is left
+    for (int c = 0; c < C; ++c) {
+        const float l = across_rows(st[c].l, [](float x, float y) { return x + y; });
+        if (g == 0) sh.ml[wave][16 * c + n] = f32x2{st[c].m, l};
+        // quad (j, m / 4, g): channels D/16 * (4g + j) + m .. m + 3
 #pragma unroll
-    for (int half = kWaves / 2; half > 0; half /= 2) {
-        if (wave >= half && wave < 2 * half) {
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                sh.m[wave - half][c][lane] = st[c].m;
-                sh.l[wave - half][c][lane] = st[c].l;
-#pragma unroll
-                for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        sh.o[wave - half][c][4 * m + j][lane] = st[c].o[m][j];
-            }
-        }
-        __syncthreads();
-        if (wave < half) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                f32x4 o[D / 16];
-#pragma unroll
-                for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[m][j] = sh.o[wave][c][4 * m + j][lane];
-                join<D>(st[c], sh.m[wave][c][lane], sh.l[wave][c][lane], o);
-            }
-        }
-        __syncthreads();
-    }
-
-    if (splits == 1) {
-        if (wave != 0) return;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (!mine[c]) continue;
-            const float l = st[c].l, inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int64_t at = (int64_t)(seq.start + i[c]) * (p.kv_heads * p.group) + hq[c];
-            typename E::T *out = (typename E::T *)p.out + at * D + D / 16 * 4 * g;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int m = 0; m < D / 16; m += 2)
-                    *reinterpret_cast<uint32_t *>(out + D / 16 * j + m) =
-                        pack_pair<E>(st[c].o[m][j] * inv, st[c].o[m + 1][j] * inv);
-            if (p.lse && g == 0)
-                p.lse[at] = l == 0.0f ? -__builtin_inff()
-                                      : (st[c].m + __builtin_log2f(l)) * 0.69314718055994531f;
-        }
-        return;
-    }
-
-    // several splits: leave this one's state in the workspace; the last to get
-    // here joins them
-    typedef Part<D, kRows> P;
-    float *part = p.part + (int64_t)blockIdx.x * gridDim.y * P::kFloats;
-    if (wave == 0) {
-        float *my = part + (int64_t)split * P::kFloats;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (!mine[c]) continue;
-            const int row = 16 * c + n;
-            if (g == 0) put(my + P::state(row), f32x2{st[c].m, st[c].l});
-            // quad (j, m / 4, g): channels D/16 * (4g + j) + m .. m + 3
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int m = 0; m < D / 16; m += 4) {
-                    float *to = my + P::sums(valid, row, (j * (D / 64) + m / 4) * 4 + g);
-                    put(to, f32x2{st[c].o[m][j], st[c].o[m + 1][j]});
-                    put(to + 2, f32x2{st[c].o[m + 2][j], st[c].o[m + 3][j]});
-                }
-        }
-        if (lane == 0) sh.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
+            for (int m = 0; m < D / 16; m += 4)
+                sh.o[wave][(j * (D / 64) + m / 4) * 4 + g][16 * c + n] =
+                    f32x4{st[c].o[m][j], st[c].o[m + 1][j], st[c].o[m + 2][j], st[c].o[m + 3][j]};
     }
     __syncthreads();
-    if (!sh.last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 
     // a thread for every four channels of a row, rows next to each other
     const int shift = valid > 1 ? 32 - __builtin_clz(valid - 1) : 0;   // rows, a power of two
-    for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
-        const int r = x & ((1 << shift) - 1), quad = x >> shift;
-        if (r >= valid) continue;
-        float top, l;
-        const f32x4 o = join_splits<D, kRows>(part, splits, valid, r, quad, top, l);
+    const auto write = [&](int r, int quad, const f32x4 &o, float top, float l) {
         const int c = D / 16 * (4 * (quad % 4) + quad / 4 / (D / 64)) + quad / 4 % (D / 64) * 4;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         const int rr = base + row0 + r;
@@ -559,9 +476,55 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
                            head * p.group + rr % p.group;
         *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + c) =
             u32x2{pack_pair<E>(o[0] * inv, o[1] * inv), pack_pair<E>(o[2] * inv, o[3] * inv)};
-        if (p.lse && c == 0)
+        if (p.lse && quad == 0)
             p.lse[at] = l == 0.0f ? -__builtin_inff()
                                   : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+    };
+    typedef Part<D, kRows> P;
+    float *part = p.part + (int64_t)blockIdx.x * gridDim.y * P::kFloats;
+    float *my = part + (int64_t)split * P::kFloats;
+    for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
+        const int r = x & ((1 << shift) - 1), quad = x >> shift;
+        if (r >= valid) continue;
+        // the waves' states in their order
+        float top = sh.ml[0][r][0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][r][0]);
+        float l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const f32x2 ml = sh.ml[w][r];
+            const float f = __builtin_amdgcn_exp2f(ml[0] - top);
+            l += ml[1] * f;
+            o += sh.o[w][quad][r] * f;
+        }
+        if (splits == 1) {
+            write(r, quad, o, top, l);
+        } else {
+            // several splits: this one's state into the workspace
+            if (quad == 0) put(my + P::state(r), f32x2{top, l});
+            float *to = my + P::sums(valid, r, quad);
+            put(to, f32x2{o[0], o[1]});
+            put(to + 2, f32x2{o[2], o[3]});
+        }
+    }
+    if (splits == 1) return;
+
+    // the last split to get here joins them
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        sh.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
+    __syncthreads();
+    if (!sh.last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
+        const int r = x & ((1 << shift) - 1), quad = x >> shift;
+        if (r >= valid) continue;
+        float top, l;
+        const f32x4 o = join_splits<D, kRows>(part, splits, valid, r, quad, top, l);
+        write(r, quad, o, top, l);
     }
 }
 
