@@ -450,8 +450,9 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
  *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a
  *           length are not read; tokens on a page outside the cache are hidden
- *   q_start int32 [seqs+1], lengths int32 [seqs] (device); values outside
- *           [0, tokens] and [0, 64*table_width] are taken as the nearest bound
+ *   q_start int32 [seqs+1], not decreasing, lengths int32 [seqs] (device);
+ *           values outside [0, tokens] and [0, 64*table_width] are taken as the
+ *           nearest bound
  *   pages   with query->list > 0, int32 [tokens][kv_heads][list] (device): only
  *           tokens j on the pages j/64 named here are visible; numbers that
  *           are negative or past the length name nothing; naming a page twice
@@ -464,7 +465,8 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  * cached values of 65536 and more count as infinities, as in lce_kv4_read.
  * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
  *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
- *         grid past the device's limits), LCE_EALIGN, LCE_EHIP. */
+ *         table_width over 2^24, more rows or tiles than a grid holds),
+ *         LCE_EALIGN, LCE_EHIP. */
 lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
                              const lce_kv4_query_desc *query, const void *q, const int32_t *table,
                              const int32_t *q_start, const int32_t *lengths, const int32_t *pages,

@@ -15,6 +15,9 @@ using lce::ok;
 using lce::tuning;
 using lce::kv4::kPage;
 
+// Workgroups of 256 threads in a grid: threads are counted in 32 bits.
+constexpr int64_t kMostGroups = (1LL << 24) - 1;
+
 lce_status validate_cache(const lce_kv4_cache_desc *d) {
     if (!d) return fail(LCE_EINVAL, "desc is NULL");
     if (d->pages < 1 || d->kv_heads < 1)
@@ -33,7 +36,7 @@ lce_status validate_tokens(const lce_kv4_cache_desc *d, int32_t type, int64_t to
     if (tokens < 0 || tokens > INT32_MAX)
         return fail(LCE_EINVAL, "tokens %lld outside [0, 2^31)", (long long)tokens);
     // workgroups of at least 8 tokens of one head
-    if ((tokens / 8 + 1) * d->kv_heads > INT32_MAX)
+    if ((tokens / 8 + 1) * d->kv_heads > kMostGroups)
         return fail(LCE_EUNSUPPORTED, "%lld tokens of %d heads: too many for one call",
                     (long long)tokens, d->kv_heads);
     return LCE_OK;
@@ -48,8 +51,8 @@ lce_status validate_query(const lce_kv4_cache_desc *d, const lce_kv4_query_desc 
     if (q->q_heads < 1 || q->q_heads % d->kv_heads)
         return fail(LCE_EINVAL, "q_heads %d is not a multiple of kv_heads %d", q->q_heads,
                     d->kv_heads);
-    if (q->table_width > INT32_MAX / kPage)
-        return fail(LCE_EUNSUPPORTED, "table_width %d: sequences of 2^31 tokens or more",
+    if (q->table_width > 1 << 24)
+        return fail(LCE_EUNSUPPORTED, "table_width %d: sequences of more than 2^30 tokens",
                     q->table_width);
     // rows and workgroups are counted in 32 bits
     if (((int64_t)q->tokens + q->seqs) * q->q_heads > INT32_MAX)
@@ -235,7 +238,8 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
                              void *out, float *lse, void *workspace, int64_t workspace_bytes,
                              hipStream_t stream) {
     if (const lce_status st = validate_call(desc, query)) return st;
-    if (!(query->scale > 0.0f) || !std::isfinite(query->scale))
+    const float scale_log2 = query->scale * 1.44269504088896341f;
+    if (!(query->scale > 0.0f) || !std::isfinite(scale_log2))
         return fail(LCE_EINVAL, "scale %g is not a finite number > 0", query->scale);
     if (query->tokens == 0) return ok();
     if (!cache || !q || !table || !q_start || !lengths || !out || !workspace)
@@ -270,7 +274,9 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     p.out = out;
     p.lse = lse;
     p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + LCE_KV4_WORKSPACE_ZERO);
-    p.scale_log2 = query->scale * 1.44269504088896341f;
+    p.scale_log2 = scale_log2;
+    if (units > kMostGroups)
+        return fail(LCE_EUNSUPPORTED, "%lld tiles: too many for one call", (long long)units);
     const dim3 grid((unsigned)units, (unsigned)s.splits);
     if (rows == 128)
         lce::kv4::launch_attend128(p, query->type, desc->head_dim, grid, stream);
@@ -307,6 +313,9 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
                     (long long)need);
 
     const int64_t units = (int64_t)query->tokens * desc->kv_heads;
+    if (units > kMostGroups)
+        return fail(LCE_EUNSUPPORTED, "%lld tokens and heads: too many for one call",
+                    (long long)units);
     // a window hides pages but does not renumber them: all up to the last count
     lce_kv4_query_desc all = *query;
     all.window = 0;

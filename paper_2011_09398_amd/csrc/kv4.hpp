@@ -61,6 +61,13 @@ __device__ __forceinline__ float across_rows(float x, F f) {
     return f(bits_as<float>((uint32_t)b[0]), bits_as<float>((uint32_t)b[1]));
 }
 
+// Below every score, and finite: a row that has seen nothing yet weighs a hidden
+// token exp2(-infinity - kNone) = 0.
+constexpr float kNone = -3.402823466e38f;
+
+// Scores (log2) from which half a last place passes a half.
+constexpr float kLarge = 16777216.0f;
+
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 // One sequence of a batch, as the device arrays give it; every value is
@@ -112,7 +119,7 @@ __device__ __forceinline__ Span visible(const Sequence &s, int i, int causal, in
     const int p = s.length - s.queries + i;
     Span v;
     v.hi = causal ? clampi(p + 1, 0, s.length) : s.length;
-    v.lo = window > 0 ? clampi(p - window + 1, 0, s.length) : 0;
+    v.lo = window > 0 ? (int)min(max((int64_t)p - window + 1, (int64_t)0), (int64_t)s.length) : 0;
     return v;
 }
 

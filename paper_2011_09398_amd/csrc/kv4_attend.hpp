@@ -135,7 +135,7 @@ __device__ __forceinline__ f32x4 join_splits(const float *part, int splits, int 
                                              int quad, float &top, float &l) {
     typedef Part<D, ROWS> P;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    top = -1e30f;
+    top = kNone;
     l = 0.0f;
     for (int s0 = 0; s0 < splits; s0 += 16) {
         f32x2 ml[16];
@@ -144,7 +144,7 @@ __device__ __forceinline__ f32x4 join_splits(const float *part, int splits, int 
         // and weighs nothing
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-            ml[k] = f32x2{-1e30f, 0.0f};
+            ml[k] = f32x2{kNone, 0.0f};
             y[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 #pragma unroll

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
 
     // the state of a row: running maximum (log2), this lane's share of the sum, sums
     // of weighted values: o[m][i] is place 32m + 8 (i / 4) + 4h + i % 4
-    float top = -1e30f, l = 0.0f;
+    float top = kNone, l = 0.0f;
     f32x16 o[D / 32];
 #pragma unroll
     for (int m = 0; m < D / 32; ++m) o[m] = f32x16{};
@@ -298,12 +298,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     // weights of 16 scores, two second operands of 16 tokens each
     f32x16 s[2];
     u32x4 w[4];
-    const auto weigh = [&](int t) {
+    const auto weigh = [&](int t, float c) {
 #pragma unroll
         for (int k = 0; k < 16; k += 2) {
-            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k], p.scale_log2, -top));
-            const float y =
-                __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k + 1], p.scale_log2, -top));
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k], c, -top));
+            const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k + 1], c, -top));
             l += x;
             l += y;
             w[2 * t + k / 8][k % 8 / 2] = pack_pair<E>(x, y);
@@ -367,11 +366,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
 #pragma unroll
                 for (int m = 0; m < D / 32; ++m) o[m] *= f;
             }
-            weigh(0);
+            // the fused product differs from the rounded one that the maximum is: where
+            // that could show, round the scores' products too
+            float c = p.scale_log2;
+            if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(top) > kLarge)) {
+                s[0] *= c;
+                s[1] *= c;
+                c = 1.0f;
+            }
+            weigh(0, c);
             __builtin_amdgcn_sched_barrier(0);
             add(0);
             s[0] = scores<E, D, 0>(keys, q);
-            weigh(1);
+            weigh(1, c);
             interleave<D / 16 + Keys<D>::kChunks * E::kPieces, 6>();
             __builtin_amdgcn_sched_barrier(0);
             add(1);

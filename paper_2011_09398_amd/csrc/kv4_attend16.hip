@@ -255,8 +255,7 @@ __device__ __forceinline__ void settle(Values<D> &r) {
 // A page's scores into the rows' maximum and sum; its weights, ready to be
 // multiplied.
 template <typename E, int D>
-__device__ __forceinline__ void weigh(RowState<D> &st, const f32x4 (&s)[4], u32x4 (&p)[2],
-                                      float c) {
+__device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)[2], float c) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -274,6 +273,13 @@ __device__ __forceinline__ void weigh(RowState<D> &st, const f32x4 (&s)[4], u32x
         st.l *= f;
 #pragma unroll
         for (int m = 0; m < D / 16; ++m) st.o[m] *= f;
+    }
+    // The fused product below differs from the rounded one that the maximum is; where
+    // that could show (scores past 2^24), round the scores' products too.
+    if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(st.m) > kLarge)) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] *= c;
+        c = 1.0f;
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -368,7 +374,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     RawQueries<D> raw[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        st[c].m = -1e30f;   // finite: a row that has seen nothing weighs exp2(-inf) = 0
+        st[c].m = kNone;
         st[c].l = 0.0f;
 #pragma unroll
         for (int m = 0; m < D / 16; ++m) st[c].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};

@@ -392,6 +392,27 @@ def test_array_values_outside_their_range(rows):
     assert not out[:2].any() and torch.isneginf(lse[:2]).all()
 
 
+@pytest.mark.parametrize("rows", [16, 32, 128])
+def test_windows_and_scales_at_the_ends_of_their_range(rows):
+    lce.set_tuning(kv4_rows=rows)
+    b = Batch(27, [90, 3], [5, 3], 2, 1, 64, "bf16")
+    for causal in (True, False):
+        for window in (2 ** 31 - 1, 2 ** 30, 91):
+            attend(b, causal, window)
+    b = Batch(27, [2, 90], [9, 3], 2, 1, 64, "bf16")     # positions below 0
+    attend(b, False, 2 ** 31 - 1)
+    # scores of about 10^34: each row is the token with the largest one
+    args = b.device(lce)
+    args[1].mul_(2.0 ** 100)
+    out, lse = lce.kv4_attention(*args, scale=1e3, return_lse=True)
+    q = args[1].cpu().double().numpy()
+    for t in range(9, 12):
+        for h in range(2):
+            best = np.argmax((b.k[1][:, 0] @ q[t, h])[:88 + t - 9])
+            assert np.array_equal(out[t, h].cpu().double().numpy(), b.v[1][best, 0])
+    assert lse[9:].isfinite().all()
+
+
 def test_same_bits_every_time_and_workspace_left_ready():
     b = Batch(18, [900, 40], [1, 1], 16, 2, 128, "bf16")
     args = b.device(lce)

@@ -132,6 +132,12 @@ def test_attention_and_select_refusals():
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         assert call_attention(q=query(scale=scale)) == lce.LCE_EINVAL
         assert "scale" in lce.last_error()
+    assert call_attention(q=query(scale=3e38)) == lce.LCE_EINVAL       # times log2(e)
+    one = dict(q_heads=1, q_token_stride=64, q_head_stride=64)
+    wide = cache(kv_heads=1, head_dim=64)
+    assert call_select(c=wide, q=query(list=1, tokens=2 ** 24, **one)) == lce.LCE_EUNSUPPORTED
+    assert call_attention(c=wide, q=query(list=1, tokens=2 ** 24, **one), pages=P) == \
+        lce.LCE_EUNSUPPORTED
     assert call_attention(q=query(list=2)) == lce.LCE_EINVAL
     assert call_attention(q=query(list=2), pages=P + 1) == lce.LCE_EALIGN
     assert call_attention(out=P + 8) == lce.LCE_EALIGN
