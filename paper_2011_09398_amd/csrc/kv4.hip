@@ -92,6 +92,13 @@ int64_t most_pages(const lce_kv4_query_desc &q) {
     return n;
 }
 
+// The most rows that read the same pages, as far as the call says: the new tokens of
+// a sequence (of a list: one), times the heads that share a cache head.
+int64_t query_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
+    const int64_t tokens = q.list ? 1 : q.max_q > 0 ? q.max_q : q.tokens / q.seqs;
+    return tokens * (q.q_heads / d.kv_heads);
+}
+
 // Query rows of a tile of attention.  A tile takes a page's values out of 4 bits once
 // for all its rows, but the more rows it has the fewer tiles there are, and fewer of
 // 128 than run at a time (512) leave CUs without work.  Heads of 256 channels, and
@@ -113,7 +120,7 @@ int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
     const int forced = tuning(LCE_TUNE_KV4_ROWS);
     if (q.list || forced == 16) return 16;
     if (forced == 128 || (forced == 32 && !large)) return forced;
-    const int64_t most = (q.max_q > 0 ? q.max_q : q.tokens / q.seqs) * (int64_t)(q.q_heads / d.kv_heads);
+    const int64_t most = query_rows(d, q);
     if (most >= 128 && (int64_t)q.tokens * q.q_heads / 128 >= (large ? 1024 : 512)) return 128;
     return most >= 256 && !large ? 32 : 16;
 }
@@ -127,13 +134,7 @@ struct Split {
 // take one: how many workgroups (of four waves) share a unit.  Sharing costs
 // about `fixed` microseconds for the partial states, the ticket and the joining,
 // and 0.06 for each state joined, so a unit is divided only where its pages take
-// longer, and no further than 512 workgroups in all: two a CU keep as many loads
-// in flight as the memory answers.  Measured (us): one sequence of 20001 tokens,
-// 8 heads of 128, chunks of 8, 12, 16, 32, 64 pages 13.5, 12.2, 12.1, 14.0, 20.0;
-// lists of 64 pages, 128 units of 128, chunks of 8, 12, 16, 24, 64: 20.9, 18.5,
-// 17.6, 18.0, 21.9; lists of 24, 120 units of 256, chunks of 8, 12, 24: 20.7,
-// 19.5, 19.0; 64 sequences of up to 8192 tokens, 512 units of 128, chunks of 16,
-// 64, 128: 50.3, 49.8, 44.8.
+// longer, and no further than `most` workgroups in all.
 Split split_pages(int64_t units, int64_t pages, double step, double fixed, int64_t most,
                   int64_t parts) {
     const int64_t some = std::max<int64_t>(units, 1);
@@ -262,12 +263,29 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     const int rows = tile_rows(*desc, *query);
     const int64_t units = tiles(*desc, *query, rows, list) * desc->kv_heads;
     const double size = desc->head_dim / 128.0;
-    const Split s =
-        rows == 128
-            ? split_pages(units, most_pages(*query), 2 + 2 * size, 4 + 8 * size, 512,
-                          kMostParts / 8)
-            : split_pages(units, list ? query->list : most_pages(*query), 0.25 + 0.4 * size,
-                          1 + 2.5 * size, 512, kMostParts * 16 / rows);
+    // Of lists and windows, which are mostly of one length, 512 workgroups: two a CU
+    // keep as many loads in flight as the memory answers.  Sequences are of different
+    // lengths, of which the call knows the longest: up to 1500, so that the long ones
+    // do not run alone at the end.  Measured (us, heads of 128, 32 on 8, or lists of 64 and 24 pages):
+    //   pages a workgroup                  8     12     16     24     32     64    all
+    //   1 sequence of 20001              13.6   12.0   12.4   13.4   15.2   22.8   80
+    //   32 of up to 8192                                      25.9          29.2  43.5
+    //   4 of up to 65536                                      28.2          33.4   -
+    //   64 of up to 8192, 64 heads       64.1   64.1   64.1   64.0   64.1   63.4  59.5
+    //   128 lists of 64                  20.6   18.0   17.3   18.0   19.3   22.5  22.5
+    //   120 lists of 24, heads of 256    20.3   19.8   20.7   19.2   19.2   19.2  19.2
+    const int64_t most = list ? query->list : most_pages(*query);
+    const Split s = rows == 128 ? split_pages(units, most, 2 + 2 * size, 4 + 8 * size, 512,
+                                              kMostParts / 8)
+                                : split_pages(units, most, 0.25 + 0.4 * size, 1 + 2.5 * size,
+                                              list || query->window ? 512 : 1500,
+                                              kMostParts * 16 / rows);
+    // Loads past the caches where no other tile reads the same pages and the whole is
+    // much more than the caches hold: 64 sequences of up to 8192 tokens, 64 heads of
+    // 128 on 8 (238 MB), 59.5 -> 52.6 us; 512 lists of 64 pages (143 MB) 39.5 -> 36.1;
+    // but less, or lines read in two halves (other head sizes), is up to a fifth slower.
+    const bool once = query_rows(*desc, *query) <= 16 &&
+                      68.0 * desc->head_dim * most * units >= 256 << 20;
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;
@@ -281,7 +299,7 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     if (rows == 128)
         lce::kv4::launch_attend128(p, query->type, desc->head_dim, grid, stream);
     else
-        lce::kv4::launch_attend16(p, query->type, desc->head_dim, rows, grid, stream);
+        lce::kv4::launch_attend16(p, query->type, desc->head_dim, rows, once, grid, stream);
     return check_launch("lce_kv4_attention launch");
 }
 

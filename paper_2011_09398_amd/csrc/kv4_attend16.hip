@@ -8,6 +8,15 @@ namespace {
 
 constexpr int kWaves = kThreads / 64;
 
+// A load from the cache; ONCE: past the caches, of what nobody else will read soon.
+template <bool ONCE, typename V>
+__device__ __forceinline__ V fetch(const uint8_t *p) {
+    if constexpr (ONCE)
+        return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+    else
+        return *reinterpret_cast<const V *>(p);
+}
+
 // One page of one head as a wave's 64 lanes hold it.  Lane (n, g), n = lane %
 // 16, g = lane / 16: the key codes of tokens 16t + n, 16 bytes of them for each
 // 128 channels (the first operand of a 16x16x128 product: 32 channels in a row),
@@ -19,6 +28,7 @@ struct Keys {
     u32x4 k[4][kChunks];
     uint32_t scale[kChunks];   // byte t: scale of tokens 16t + n
 
+    template <bool ONCE>
     __device__ __forceinline__ void load(const uint8_t *rec, int n, int g) {
         // a head of 64 channels fills half of the product's 128: the other half
         // repeats them, against another piece of the queries
@@ -27,11 +37,11 @@ struct Keys {
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int c = 0; c < kChunks; ++c)
-                k[t][c] = *reinterpret_cast<const u32x4 *>(rec + (16 * t + n) * (D / 2) + 64 * c +
+                k[t][c] = fetch<ONCE, u32x4>(rec + (16 * t + n) * (D / 2) + 64 * c +
                                                            16 * kg);
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
-            scale[c] = *reinterpret_cast<const uint32_t *>(rec + Record<D>::kKeyScale +
+            scale[c] = fetch<ONCE, uint32_t>(rec + Record<D>::kKeyScale +
                                                            (n * (D / 32) + 4 * c + kg) * 4);
     }
 };
@@ -41,24 +51,25 @@ struct Values {
     uint32_t v[4][D / 32];
     u32x4 scale;               // byte i of word t: scale of token 16t + 4g + i
 
+    template <bool ONCE>
     __device__ __forceinline__ void load(const uint8_t *rec, int n, int g) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const uint8_t *at = rec + Record<D>::kValue + ((4 * t + g) * 16 + n) * (D / 8);
             if constexpr (D == 64) {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(at);
+                const u32x2 w = fetch<ONCE, u32x2>(at);
                 v[t][0] = w[0], v[t][1] = w[1];
             } else {
 #pragma unroll
                 for (int j = 0; j < D / 128; ++j) {
-                    const u32x4 w = reinterpret_cast<const u32x4 *>(at)[j];
+                    const u32x4 w = fetch<ONCE, u32x4>(at + 16 * j);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[t][4 * j + i] = w[i];
                 }
             }
         }
         // channels D/16 * n lie in group n * D / 512
-        scale = *reinterpret_cast<const u32x4 *>(rec + Record<D>::kValueScale +
+        scale = fetch<ONCE, u32x4>(rec + Record<D>::kValueScale +
                                                  (n * D / 512) * 64 + 16 * g);
     }
 };
@@ -315,7 +326,7 @@ struct Shared {
 // Keys are the first operand and queries the second, so that a lane's scores
 // belong to one row and the weights leave the softmax as the second operand of
 // the product with the values; no weight and no score crosses lanes.
-template <typename E, int D, bool LIST, int C>
+template <typename E, int D, bool LIST, int C, bool ONCE>
 __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16_kernel(
     AttendParams p) {
     constexpr int kRows = 16 * C;
@@ -423,8 +434,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     const bool any = todo != 0;
     if (any) {
         const uint8_t *rec = next(number);
-        keys.load(rec, n, g);
-        values.load(rec, n, g);
+        keys.template load<ONCE>(rec, n, g);
+        values.template load<ONCE>(rec, n, g);
     }
     Queries<E, D> q[C];
 #pragma unroll
@@ -453,10 +464,10 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         u32x4 w[C][2];
 #pragma unroll
         for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], p.scale_log2);
-        if (more) keys.load(rec, n, g);
+        if (more) keys.template load<ONCE>(rec, n, g);
         add_values<E, D, C, 0, 0>(st, values, w);
         add_values<E, D, C, 1, 0>(st, values, w);
-        if (more) values.load(rec, n, g);
+        if (more) values.template load<ONCE>(rec, n, g);
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -536,39 +547,42 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
 
 namespace {
 
-template <typename E, int D, int C>
+template <typename E, int D, int C, bool ONCE>
 void launch_c(const AttendParams &p, dim3 grid, hipStream_t s) {
     if constexpr (C == 1) {
         if (p.named) {
-            hipLaunchKernelGGL((attend16_kernel<E, D, true, 1>), grid, dim3(kThreads), 0, s, p);
+            hipLaunchKernelGGL((attend16_kernel<E, D, true, 1, ONCE>), grid, dim3(kThreads), 0, s, p);
             return;
         }
     }
-    hipLaunchKernelGGL((attend16_kernel<E, D, false, C>), grid, dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((attend16_kernel<E, D, false, C, ONCE>), grid, dim3(kThreads), 0, s, p);
 }
 
 template <typename E, int D>
-void launch_d(const AttendParams &p, int rows, dim3 grid, hipStream_t s) {
+void launch_d(const AttendParams &p, int rows, bool once, dim3 grid, hipStream_t s) {
     // 32 rows of 128 channels in float16, or of 256, have more state than registers
     if constexpr (D * E::kPieces <= 256) {
-        if (rows == 32) return launch_c<E, D, 2>(p, grid, s);
+        if (rows == 32) return launch_c<E, D, 2, false>(p, grid, s);
     }
-    launch_c<E, D, 1>(p, grid, s);
+    if constexpr (D == 128) {
+        if (once) return launch_c<E, D, 1, true>(p, grid, s);
+    }
+    launch_c<E, D, 1, false>(p, grid, s);
 }
 
 template <typename E>
-void launch_t(const AttendParams &p, int dim, int rows, dim3 grid, hipStream_t s) {
-    if (dim == 64) launch_d<E, 64>(p, rows, grid, s);
-    else if (dim == 128) launch_d<E, 128>(p, rows, grid, s);
-    else launch_d<E, 256>(p, rows, grid, s);
+void launch_t(const AttendParams &p, int dim, int rows, bool once, dim3 grid, hipStream_t s) {
+    if (dim == 64) launch_d<E, 64>(p, rows, once, grid, s);
+    else if (dim == 128) launch_d<E, 128>(p, rows, once, grid, s);
+    else launch_d<E, 256>(p, rows, once, grid, s);
 }
 
 }  // namespace
 
-void launch_attend16(const AttendParams &p, int type, int dim, int rows, dim3 grid,
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool once, dim3 grid,
                      hipStream_t s) {
-    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, rows, grid, s);
-    else launch_t<Bf16>(p, dim, rows, grid, s);
+    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, rows, once, grid, s);
+    else launch_t<Bf16>(p, dim, rows, once, grid, s);
 }
 
 }  // namespace kv4

@@ -52,8 +52,8 @@ struct SelectParams : QueryParams {
 void launch_append(const AppendParams &p, int type, int dim, hipStream_t s);
 void launch_read(const ReadParams &p, int type, int dim, hipStream_t s);
 // 16 or 32 query rows a workgroup (32: heads of up to 128); grid = (tiles *
-// kv_heads, splits)
-void launch_attend16(const AttendParams &p, int type, int dim, int rows, dim3 grid,
+// kv_heads, splits); once: heads of 128 are loaded past the caches
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool once, dim3 grid,
                      hipStream_t s);
 // 128 query rows a workgroup, no list; grid = (tiles * kv_heads, splits)
 void launch_attend128(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);

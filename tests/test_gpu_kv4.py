@@ -531,6 +531,18 @@ def test_lists(dim, dtype, q_heads, kv_heads, chunk):
         attend(b, causal=False, window=90, pages=pages)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_tables_and_lists_so_wide_that_loads_pass_the_caches(dtype):
+    """What the call says of its size decides; the tokens are few all the same."""
+    b = Batch(28, [300, 70, 1], [1, 1, 1], 8, 2, 128, dtype, width=6000)
+    attend(b)
+    pages = np.full((b.tokens, 2, 9000), -1, np.int32)
+    for t in range(3):
+        for h in range(2):
+            pages[t, h, b.rng.permutation(9000)[:5]] = b.rng.permutation(5)
+    attend(b, pages=pages)
+
+
 def test_a_list_of_all_pages_is_no_list():
     b = Batch(21, [500, 64], [3, 1], 8, 2, 128, "bf16")
     every = np.broadcast_to(np.arange(8, dtype=np.int32), (4, 2, 8)).copy()
