@@ -749,6 +749,7 @@ class KV4Cache:
         self._int32, self._int64 = torch.int32, torch.int64
         self._uint8, self._float32 = torch.uint8, torch.float32
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        self._scale = head_dim ** -0.5
 
     def _holds(self, t, dtype) -> bool:
         """Whether t is a contiguous `dtype` tensor on the cache's device: the quick
@@ -887,9 +888,11 @@ def _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, 
         code = cache._types.get(q.dtype, 0)
         i32 = cache._int32
         fine = (code > 0 and dim == cache.head_dim and strides[2] == 1
-                and q.get_device() == cache._index and cache._holds(table, i32)
-                and cache._holds(q_start, i32) and q_start.shape == (seqs + 1,)
-                and cache._holds(lengths, i32) and lengths.shape == (seqs,))
+                and table.dtype is q_start.dtype is lengths.dtype is i32
+                and q.get_device() == table.get_device() == q_start.get_device()
+                == lengths.get_device() == cache._index
+                and table.is_contiguous() and q_start.is_contiguous() and lengths.is_contiguous()
+                and q_start.shape == (seqs + 1,) and lengths.shape == (seqs,))
     except (AttributeError, TypeError, ValueError):
         fine = False
     if not fine:
@@ -935,7 +938,7 @@ def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optiona
     """
     count = 0 if pages is None else _list_length(cache, q, pages)
     d = _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, max_len,
-                   cache.head_dim ** -0.5 if scale is None else scale)
+                   cache._scale if scale is None else scale)
     if out is None:
         out = q.new_empty(q.shape)
     else:

@@ -100,13 +100,12 @@ int64_t query_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
 }
 
 // Query rows of a tile of attention.  A tile takes a page's values out of 4 bits once
-// for all its rows, but the more rows it has the fewer tiles there are, and fewer of
-// 128 than run at a time (512) leave CUs without work.  Heads of 256 channels, and
-// 32 rows of 128 in float16 (three pieces of a query, and more registers than there
+// for all its rows, but the more rows it has the fewer tiles there are, and fewer than
+// run at a time (1024 of 32, 512 of 128) leave CUs without work.  Heads of 256 channels,
+// and 32 rows of 128 in float16 (three pieces of a query, and more registers than there
 // are), stay at 16.  Measured (us, tiles of 16 / 32 / 128, 32 heads on 8, 4000 tokens
 // before the new ones):
 //                                       bfloat16, 128      float16, 64    float16, 128
-//   16 sequences, 64 rows each           24 / 29 /  69
 //   16 sequences, 256 rows each          44 / 41 / 113
 //   one sequence, 1024 new tokens       110 / 94 / 129    85 / 71 / 90   121 / - / 184
 //   one sequence, 2048                  242 / 194 / 177  180 / 150 / 127  263 / - / 261
@@ -114,15 +113,17 @@ int64_t query_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
 //   four sequences, up to 512 each       93 / 84 / 126    71 / 66 / 91   101 / - / 177
 //   four sequences, up to 1024          175 / 151 / 161  134 / 118 / 113  198 / - / 220
 //   four sequences, up to 2048          338 / 278 / 246  259 / 216 / 173  380 / - / 341
+//   two, up to 359 on 5025, 8 on 2       23 /  27 /  51
+//   four prompts of up to 1943, 2 heads  13 /  18 /  38
 int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
     if (d.head_dim > 128) return 16;
     const bool large = d.head_dim == 128 && q.type == LCE_FLOAT16;
     const int forced = tuning(LCE_TUNE_KV4_ROWS);
     if (q.list || forced == 16) return 16;
     if (forced == 128 || (forced == 32 && !large)) return forced;
-    const int64_t most = query_rows(d, q);
-    if (most >= 128 && (int64_t)q.tokens * q.q_heads / 128 >= (large ? 1024 : 512)) return 128;
-    return most >= 256 && !large ? 32 : 16;
+    const int64_t most = query_rows(d, q), all = (int64_t)q.tokens * q.q_heads;
+    if (most >= 128 && all >= 128 * (large ? 1024 : 512)) return 128;
+    return most >= 256 && !large && all >= 32 * 1024 ? 32 : 16;
 }
 
 struct Split {
@@ -263,10 +264,11 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     const int rows = tile_rows(*desc, *query);
     const int64_t units = tiles(*desc, *query, rows, list) * desc->kv_heads;
     const double size = desc->head_dim / 128.0;
-    // Of lists and windows, which are mostly of one length, 512 workgroups: two a CU
-    // keep as many loads in flight as the memory answers.  Sequences are of different
-    // lengths, of which the call knows the longest: up to 1500, so that the long ones
-    // do not run alone at the end.  Measured (us, heads of 128, 32 on 8, or lists of 64 and 24 pages):
+    // Lists and windows are mostly of one length: 512 workgroups, two a CU, keep as many
+    // loads in flight as the memory answers.  Sequences are of different lengths, of
+    // which the call knows the longest: up to 1500, so that the long ones do not run
+    // alone at the end.  Where a sequence has several tiles already, 768, and states of
+    // all their rows to store and join.  Measured (us, heads of 128, 32 on 8, or lists):
     //   pages a workgroup                  8     12     16     24     32     64    all
     //   1 sequence of 20001              13.6   12.0   12.4   13.4   15.2   22.8   80
     //   32 of up to 8192                                      25.9          29.2  43.5
@@ -274,18 +276,24 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     //   64 of up to 8192, 64 heads       64.1   64.1   64.1   64.0   64.1   63.4  59.5
     //   128 lists of 64                  20.6   18.0   17.3   18.0   19.3   22.5  22.5
     //   120 lists of 24, heads of 256    20.3   19.8   20.7   19.2   19.2   19.2  19.2
+    //   2 of up to 359 on 5025, 8 heads                30.5   28.0                23.2
     const int64_t most = list ? query->list : most_pages(*query);
-    const Split s = rows == 128 ? split_pages(units, most, 2 + 2 * size, 4 + 8 * size, 512,
-                                              kMostParts / 8)
-                                : split_pages(units, most, 0.25 + 0.4 * size, 1 + 2.5 * size,
-                                              list || query->window ? 512 : 1500,
-                                              kMostParts * 16 / rows);
-    // Loads past the caches where no other tile reads the same pages and the whole is
-    // much more than the caches hold: 64 sequences of up to 8192 tokens, 64 heads of
-    // 128 on 8 (238 MB), 59.5 -> 52.6 us; 512 lists of 64 pages (143 MB) 39.5 -> 36.1;
-    // but less, or lines read in two halves (other head sizes), is up to a fifth slower.
+    const bool several = !list && query_rows(*desc, *query) > 64;
+    const Split s =
+        rows == 128
+            ? split_pages(units, most, 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8)
+            : split_pages(units, most, 0.25 + 0.4 * size,
+                          (1 + 2.5 * size) * (several ? 2.5 : 1.0),
+                          list || query->window ? 512 : several ? 768 : 1500,
+                          kMostParts * 16 / rows);
+    // Loads past the caches where no other tile reads the same pages and the whole keeps
+    // the memory busy: 64 sequences of up to 8192 tokens, 64 heads of 128 on 8 (238 MB),
+    // 59.5 -> 52.6 us; 512 lists of 64 pages (143 MB) 39.5 -> 36.1; but where latency
+    // counts (32 sequences of up to 53109, 16 heads on one, 76 MB: 44 -> 53) or lines are
+    // read in two halves (other head sizes) they are slower.  The bounds are of what the
+    // call could read, which for sequences is a few times what it does.
     const bool once = query_rows(*desc, *query) <= 16 &&
-                      68.0 * desc->head_dim * most * units >= 256 << 20;
+                      68.0 * desc->head_dim * most * units >= (list ? 256 << 20 : 768 << 20);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;

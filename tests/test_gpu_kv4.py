@@ -534,7 +534,7 @@ def test_lists(dim, dtype, q_heads, kv_heads, chunk):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_tables_and_lists_so_wide_that_loads_pass_the_caches(dtype):
     """What the call says of its size decides; the tokens are few all the same."""
-    b = Batch(28, [300, 70, 1], [1, 1, 1], 8, 2, 128, dtype, width=6000)
+    b = Batch(28, [300, 70, 1], [1, 1, 1], 8, 2, 128, dtype, width=20000)
     attend(b)
     pages = np.full((b.tokens, 2, 9000), -1, np.int32)
     for t in range(3):
