@@ -601,3 +601,23 @@ def test_select_of_sign_zero_and_nan_queries():
     b.q[0, 0, :20] = NAN
     again = lce.kv4_select(*b.device(lce), 2, keep_first=0, keep_last=0)
     assert torch.equal(got, again)
+
+
+# ---- all of it together
+
+def test_the_decoding_example():
+    """Prompts and steps as a serving loop runs them.  With all pages kept, sparse steps are
+    dense ones; the 4-bit format's error of each key and value, about 0.11 of its size
+    (a step of at most a quarter of a value between 1 and 2 of its binade, half of that at
+    most, and a shared scale), is averaged by the sums and stays below 0.25."""
+    import importlib.util
+    import os
+    from tests.conftest import ROOT
+    spec = importlib.util.spec_from_file_location("kv4_decoding",
+                                                  os.path.join(ROOT, "examples", "kv4_decoding.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    r = example.run(seqs=3, prompt=300, steps=10, keep=6, q_heads=8, kv_heads=2, dim=64)
+    assert r["prompt"] < 0.25 and r["dense"] < 0.25
+    assert abs(r["sparse"] - r["dense"]) < 0.02        # 6 pages hold 310 tokens
+    assert abs(r["size"] - 76 / 256) < 1e-6
