@@ -101,20 +101,24 @@ int64_t query_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
 
 // Query rows of a tile of attention.  A tile takes a page's values out of 4 bits once
 // for all its rows, but the more rows it has the fewer tiles there are, and fewer than
-// run at a time (1024 of 32, 512 of 128) leave CUs without work.  Heads of 256 channels,
-// and 32 rows of 128 in float16 (three pieces of a query, and more registers than there
-// are), stay at 16.  Measured (us, tiles of 16 / 32 / 128, 32 heads on 8, 4000 tokens
-// before the new ones):
-//                                       bfloat16, 128      float16, 64    float16, 128
-//   16 sequences, 256 rows each          44 / 41 / 113
-//   one sequence, 1024 new tokens       110 / 94 / 129    85 / 71 / 90   121 / - / 184
-//   one sequence, 2048                  242 / 194 / 177  180 / 150 / 127  263 / - / 261
-//   one sequence, 4096                  517 / 415 / 390  386 / 317 / 269  559 / - / 526
-//   four sequences, up to 512 each       93 / 84 / 126    71 / 66 / 91   101 / - / 177
-//   four sequences, up to 1024          175 / 151 / 161  134 / 118 / 113  198 / - / 220
-//   four sequences, up to 2048          338 / 278 / 246  259 / 216 / 173  380 / - / 341
-//   two, up to 359 on 5025, 8 on 2       23 /  27 /  51
-//   four prompts of up to 1943, 2 heads  13 /  18 /  38
+// run at a time (1024 of 32, 512 of 128) leave CUs without work; where no sequence is
+// long, half as many tiles of 128 do.  Heads of 256 channels, and 32 rows of 128 in
+// float16 (three pieces of a query, and more registers than there are), stay at 16.
+// Measured (us, tiles of 16 / 32 / 128, 32 heads on 8, 4000 tokens before the new ones
+// if not said otherwise):
+//                                        bfloat16, 128     float16, 64    float16, 128
+//   16 sequences, 256 rows each           44 / 43 / 92     32 / 32 / 68    46 / - / 106
+//   one sequence, 1024 new tokens        114 / 95 / 106    94 / 77 / 85   117 / - / 121
+//   one sequence, 2048                   231 / 187 / 167  174 / 142 / 117 245 / - / 195
+//   one sequence, 4096                   524 / 426 / 359  382 / 319 / 254 567 / - / 423
+//   four sequences, up to 512 each        91 / 81 / 101    68 / 62 / 75    97 / - / 117
+//   four sequences, up to 1024           174 / 146 / 134  128 / 110 / 96  185 / - / 154
+//   four sequences, up to 2048           336 / 282 / 228  245 / 214 / 161 362 / - / 267
+//   16 sequences, up to 128 on 896        38 / 40 / 34     30 / 30 / 25    40 / - / 38
+//   16, up to 64 on 960, 64 heads         38 / 40 / 35     30 / 31 / 25    41 / - / 39
+//   one prompt of 1024                    30 / 29 / 30     23 / 22 / 22    31 / - / 32
+//   two, up to 359 on 5025, 8 on 2        24 / 30 / 53     21 / 23 / 33    25 / - / 54
+//   four prompts of up to 1943, 2 heads   14 / 18 / 42     12 / 15 / 27    15 / - / 44
 int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
     if (d.head_dim > 128) return 16;
     const bool large = d.head_dim == 128 && q.type == LCE_FLOAT16;
@@ -122,7 +126,8 @@ int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
     if (q.list || forced == 16) return 16;
     if (forced == 128 || (forced == 32 && !large)) return forced;
     const int64_t most = query_rows(d, q), all = (int64_t)q.tokens * q.q_heads;
-    if (most >= 128 && all >= 128 * (large ? 1024 : 512)) return 128;
+    const bool brief = most_pages(q) <= 16;
+    if (most >= 128 && all >= 128 * (brief ? 256 : 512)) return 128;
     return most >= 256 && !large && all >= 32 * 1024 ? 32 : 16;
 }
 

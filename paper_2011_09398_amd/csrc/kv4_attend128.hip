@@ -205,7 +205,7 @@ __device__ __forceinline__ void lds_barrier() {
 // and queries leave no registers for a second wave (0.4 of the rate).
 //
 // Measured, bfloat16, 32 heads on 8 of 128 channels, causal: 4 sequences of 2048 new
-// tokens on up to 16384, 1077 TFLOP/s (a large library product: 1217); the matrix
+// tokens on up to 16384, 1135 TFLOP/s (a large library product: 1217); the matrix
 // and the vector pipe are each busy about half of the time, with two waves a SIMD
 // to fill each other's gaps.
 template <typename E, int D>
