@@ -741,15 +741,19 @@ class KV4Cache:
         _check(lib().lce_kv4_cache_size(ctypes.byref(self.desc), ctypes.byref(n)))
         if data is None:
             data = torch.empty((pages, kv_heads, 76 * head_dim), dtype=torch.uint8, device=device)
-        self.data, self.pages, self.kv_heads, self.head_dim = data, pages, kv_heads, head_dim
+        self._data, self.pages, self.kv_heads, self.head_dim = data, pages, kv_heads, head_dim
         self._ref = ctypes.byref(self.desc)
-        self._ptr = data.data_ptr()
         # what every call compares its tensors with
         self._index = data.get_device()
         self._int32, self._int64 = torch.int32, torch.int64
         self._uint8, self._float32 = torch.uint8, torch.float32
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
         self._scale = head_dim ** -0.5
+
+    @property
+    def data(self):
+        """The buffer, uint8 [pages, kv_heads, 76*head_dim]."""
+        return self._data
 
     def _holds(self, t, dtype) -> bool:
         """Whether t is a contiguous `dtype` tensor on the cache's device: the quick
@@ -822,7 +826,7 @@ def kv4_append(cache: KV4Cache, k, v, slots) -> None:
         fine = False
     if not fine:
         _append_refused(cache, k, v, slots)
-    st = lib().lce_kv4_append(cache._ref, cache._ptr, code, k.data_ptr(), ks[0], ks[1],
+    st = lib().lce_kv4_append(cache._ref, cache._data.data_ptr(), code, k.data_ptr(), ks[0], ks[1],
                               v.data_ptr(), vs[0], vs[1], slots.data_ptr(), n, _stream_handle(k))
     if st != LCE_OK:
         raise LceError(st, last_error())
@@ -853,7 +857,7 @@ def kv4_read(cache: KV4Cache, slots, *, dtype=None, out=None):
             if t.shape != shape:
                 raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
         code = _float_type(k.dtype, "out")
-    st = lib().lce_kv4_read(cache._ref, cache._ptr, slots.data_ptr(), n, code, k.data_ptr(),
+    st = lib().lce_kv4_read(cache._ref, cache._data.data_ptr(), slots.data_ptr(), n, code, k.data_ptr(),
                             v.data_ptr(), _stream_handle(slots))
     if st != LCE_OK:
         raise LceError(st, last_error())
@@ -949,7 +953,7 @@ def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optiona
     if workspace is None or not cache._holds(workspace, cache._uint8):
         workspace = _workspace(workspace, cache, q, table)
     st = lib().lce_kv4_attention(
-        cache._ref, cache._ptr, ctypes.byref(d), q.data_ptr(), table.data_ptr(),
+        cache._ref, cache._data.data_ptr(), ctypes.byref(d), q.data_ptr(), table.data_ptr(),
         q_start.data_ptr(), lengths.data_ptr(), None if pages is None else pages.data_ptr(),
         out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
         workspace.numel(), _stream_handle(q))
@@ -985,7 +989,7 @@ def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_
     if workspace is None or not cache._holds(workspace, cache._uint8):
         workspace = _workspace(workspace, cache, q, table)
     st = lib().lce_kv4_select(
-        cache._ref, cache._ptr, ctypes.byref(d), q.data_ptr(), table.data_ptr(),
+        cache._ref, cache._data.data_ptr(), ctypes.byref(d), q.data_ptr(), table.data_ptr(),
         q_start.data_ptr(), lengths.data_ptr(), keep_first, keep_last, out.data_ptr(),
         workspace.data_ptr(), workspace.numel(), _stream_handle(q))
     if st != LCE_OK:
