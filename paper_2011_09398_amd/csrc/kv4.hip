@@ -306,6 +306,7 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     p.lse = lse;
     p.part = reinterpret_cast<float *>(static_cast<char *>(workspace) + LCE_KV4_WORKSPACE_ZERO);
     p.scale_log2 = scale_log2;
+    p.turn = units % 8 == 0 && desc->kv_heads % 8 ? (int)units : 0;
     if (units > kMostGroups)
         return fail(LCE_EUNSUPPORTED, "%lld tiles: too many for one call", (long long)units);
     const dim3 grid((unsigned)units, (unsigned)s.splits);

@@ -333,7 +333,17 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     __shared__ Shared<D, C> sh;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = blockIdx.x % p.kv_heads, slot = blockIdx.x / p.kv_heads, split = blockIdx.y;
+    // Workgroups go to the eight XCDs in turn, and where the grid is a multiple of eight
+    // wide all splits of a tile would go to one.  Where the heads do not spread a long
+    // sequence over the XCDs, its tiles are moved on by one a split (32 sequences of up
+    // to 53109 tokens, 16 heads on one: 47 -> 33 us).
+    const int split = blockIdx.y;
+    int unit = blockIdx.x;
+    if (!LIST && p.turn) {
+        unit += split % 8;
+        if (unit >= p.turn) unit -= p.turn;
+    }
+    const int head = unit % p.kv_heads, slot = unit / p.kv_heads;
 
     // the tile: rows of a sequence, or of a token
     Sequence seq;
@@ -498,7 +508,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
                                   : (top + __builtin_log2f(l)) * 0.69314718055994531f;
     };
     typedef Part<D, kRows> P;
-    float *part = p.part + (int64_t)blockIdx.x * gridDim.y * P::kFloats;
+    float *part = p.part + (int64_t)unit * gridDim.y * P::kFloats;
     float *my = part + (int64_t)split * P::kFloats;
     for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
         const int r = x & ((1 << shift) - 1), quad = x >> shift;
@@ -532,7 +542,7 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (threadIdx.x == 0)
-        sh.last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
+        sh.last = last_of(p.tickets + (int64_t)unit * kTicketStride, splits);
     __syncthreads();
     if (!sh.last) return;
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");

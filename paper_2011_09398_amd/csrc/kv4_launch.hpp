@@ -41,6 +41,7 @@ struct AttendParams : QueryParams {
     float *lse;                                          // or null
     float *part;                                         // workspace: partial results
     float scale_log2;
+    int turn;                                            // grid width if splits turn, or 0
 };
 
 struct SelectParams : QueryParams {

@@ -270,6 +270,28 @@ def test_many_sequences_and_long_ones(dtype, rows):
     attend(b, max_len=1900)
 
 
+@pytest.mark.parametrize("kv_heads,lengths", [
+    (1, [700, 64, 1, 3000, 65, 128, 900, 2]),
+    (1, [5000] + [7] * 6 + [64] * 8 + [400]),
+    (2, [2100, 30, 1, 640]),
+    (4, [1900, 3000])])
+@pytest.mark.parametrize("q_len", [1, 3])
+@pytest.mark.parametrize("chunk", [0, 1, 5])
+def test_splits_of_a_few_heads_of_ragged_sequences(kv_heads, lengths, q_len, chunk):
+    q_lens = [min(q_len, n) for n in lengths]
+    b = Batch(71, lengths, q_lens, 4 * kv_heads, kv_heads, 128, "bf16")
+    with lce.tuning(kv4_chunk=chunk):
+        attend(b)
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "bf16"), (128, "f16")])
+def test_many_short_prompts_and_ones_on_a_past(dim, dtype):
+    rng = np.random.default_rng(72)
+    lengths = [int(x) for x in rng.integers(60, 400, 10)]
+    attend(Batch(73, lengths, [min(n, 128) for n in lengths], 32, 8, dim, dtype))
+    attend(Batch(74, [700, 3, 1000, 64], [700, 3, 900, 64], 32, 4, dim, dtype))
+
+
 def test_hints_that_are_wrong_cost_no_result():
     b = Batch(9, [700, 20], [3, 20], 8, 2, 128, "bf16")
     for max_q, max_len in ((1, 1), (1, 64), (4000, 10 ** 6), (None, None)):
