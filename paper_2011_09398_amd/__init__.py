@@ -749,6 +749,7 @@ class KV4Cache:
         self._uint8, self._float32 = torch.uint8, torch.float32
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
         self._scale = head_dim ** -0.5
+        self._empty, self._empty_like, self._device = torch.empty, torch.empty_like, data.device
 
     @property
     def data(self):
@@ -847,7 +848,7 @@ def kv4_read(cache: KV4Cache, slots, *, dtype=None, out=None):
         if dtype is None:
             dtype = torch.bfloat16
         code = _float_type(dtype, "dtype")
-        k = slots.new_empty((n, cache.kv_heads, cache.head_dim), dtype=dtype)
+        k = torch.empty((n, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache._device)
         v = torch.empty_like(k)
     else:
         k, v = out
@@ -944,12 +945,13 @@ def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optiona
     d = _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, max_len,
                    cache._scale if scale is None else scale)
     if out is None:
-        out = q.new_empty(q.shape)
+        out = cache._empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
     else:
         _require_like(out, q.dtype, q.device, "out")
         if out.shape != q.shape:
             raise ValueError(f"out must be {list(q.shape)}, got {list(out.shape)}")
-    lse = q.new_empty(q.shape[:2], dtype=cache._float32) if return_lse else None
+    lse = (cache._empty(q.shape[:2], dtype=cache._float32, device=cache._device) if return_lse
+           else None)
     if workspace is None or not cache._holds(workspace, cache._uint8):
         workspace = _workspace(workspace, cache, q, table)
     st = lib().lce_kv4_attention(
