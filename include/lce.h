@@ -1,5 +1,7 @@
 /*
- * lce.h - C ABI of the MI355X (gfx950) bitpacked binary 2-D convolution.
+ * lce.h - C ABI of the MI355X (gfx950) bitpacked binary 2-D convolution, and of
+ * a 4-bit key/value cache with the attention that reads it (its own section
+ * below, "4-bit key/value cache").
  *
  * The operator is LceBConv2d of Larq Compute Engine (arXiv 2011.09398,
  * Section 3.2, "Operator implementations"), preceded by the sign
@@ -22,7 +24,8 @@
  * Conventions shared by every entry point:
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The
  *     library never allocates, frees or synchronizes; all work is enqueued
- *     asynchronously on `stream` (NULL = the default stream).
+ *     asynchronously on `stream` (NULL = the default stream).  Entry points
+ *     that need scratch memory take it as a workspace argument.
  *   - Activations are NHWC, filters OHWI (the TensorFlow Lite orders), and a
  *     bitpacked tensor stores ceil(C/32) int32 words per pixel (or filter
  *     tap) with its packed-channel axis innermost.  Bits beyond the real
@@ -495,7 +498,8 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
 /* ---- Schedule overrides, for tests and tuning ----------------------------
  *
  * Every convolution picks its work split by itself.  These process-wide
- * overrides force one instead; each choice gives the identical output, only
+ * overrides force one instead; each choice gives the identical output (of
+ * lce_kv4_attention: the same but for the order of its float32 sums), only
  * the speed changes.  0 (the initial value of every key) restores the
  * library's own choice.  Callers are tests, benchmarks and tuning scripts,
  * not production code.  Values are read once per launch with atomic loads,
