@@ -457,7 +457,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     if (threadIdx.x == 0) last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
     __syncthreads();
     if (!last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     for (int x = threadIdx.x; x < kRows * (D / 4); x += kThreads) {
         const int rr = x % kRows, quad = x / kRows;
         if (rr >= valid) continue;

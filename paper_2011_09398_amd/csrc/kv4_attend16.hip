@@ -553,7 +553,6 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         sh.last = last_of(p.tickets + (int64_t)unit * kTicketStride, splits);
     __syncthreads();
     if (!sh.last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
         const int r = x & ((1 << shift) - 1), quad = x >> shift;
         if (r >= valid) continue;

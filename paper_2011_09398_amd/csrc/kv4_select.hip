@@ -326,9 +326,11 @@ __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p) {
         if (threadIdx.x == 0) last = last_of(p.tickets + (int64_t)blockIdx.x * kTicketStride, splits);
         __syncthreads();
         if (!last) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
         if (pages <= kHeld)
-            for (int i = threadIdx.x; i < pages; i += kThreads) held[i] = ranks[i];
+            for (int i = threadIdx.x; i < pages; i += kThreads)
+                held[i] = __hip_atomic_load(ranks + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        else
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     }
     __syncthreads();
     if (pages <= kHeld)
