@@ -136,24 +136,28 @@ struct Split {
     int splits;   // workgroups that share a unit, at most
 };
 
-// `pages` pages of each of `units` units of work, `step` microseconds for a wave to
-// take one: how many workgroups (of four waves) share a unit.  Sharing costs
-// about `fixed` microseconds for the partial states, the ticket and the joining,
-// and 0.06 for each state joined, so a unit is divided only where its pages take
-// longer, and no further than `most` workgroups in all.
-Split split_pages(int64_t units, int64_t pages, double step, double fixed, int64_t most,
-                  int64_t parts) {
-    const int64_t some = std::max<int64_t>(units, 1);
-    const int64_t room =
-        std::min<int64_t>(std::max<int64_t>(parts / some, 1), lce::kv4::kMostSplits);
+// `pages` pages of each of `likely` units of work (the grid has room for `units`),
+// `step` microseconds for a wave to take one: how many workgroups (of four waves)
+// share a unit.  Sharing costs about `fixed` microseconds for the partial states,
+// the ticket and the joining, and 0.06 for each state joined, so a unit is divided
+// only where its pages take longer, and no further than `most` workgroups in all and
+// `parts` states in the workspace.  `each`: the number of pages that a workgroup takes
+// is a multiple of it, so that all waves are busy to the end.
+Split split_pages(int64_t units, int64_t likely, int64_t pages, double step, double fixed,
+                  int64_t most, int64_t parts, int64_t each) {
+    const int64_t some = std::max<int64_t>(std::min(units, likely), 1);
+    const int64_t room = std::min<int64_t>(
+        std::max<int64_t>(parts / std::max<int64_t>(units, 1), 1), lce::kv4::kMostSplits);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV4_CHUNK)) {
         chunk = std::max<int64_t>(t > 0 ? t : 1, (pages + room - 1) / room);
     } else {
         const double whole = pages * step / 4;
         // the least of whole / z + fixed + 0.06 z
-        const int64_t z = std::min<int64_t>({room, most / some, (int64_t)std::sqrt(whole / 0.06)});
-        if (z > 1 && whole / z + fixed + 0.06 * z < whole) chunk = (pages + z - 1) / z;
+        const double z = std::min(std::min((double)room, (double)most / some),
+                                  std::sqrt(whole / 0.06));
+        if (z > 1 && whole / z + fixed + 0.06 * z < whole)
+            chunk = ((int64_t)std::ceil(pages / z) + each - 1) / each * each;
     }
     Split s;
     s.chunk = (int)chunk;
@@ -269,35 +273,44 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     const int rows = tile_rows(*desc, *query);
     const int64_t units = tiles(*desc, *query, rows, list) * desc->kv_heads;
     const double size = desc->head_dim / 128.0;
-    // Lists and windows are mostly of one length: 512 workgroups, two a CU, keep as many
-    // loads in flight as the memory answers.  Sequences are of different lengths, of
-    // which the call knows the longest: up to 1500, so that the long ones do not run
-    // alone at the end.  Where a sequence has several tiles already, 768, and states of
-    // all their rows to store and join.  Measured (us, heads of 128, 32 on 8, or lists):
-    //   pages a workgroup                  8     12     16     24     32     64    all
-    //   1 sequence of 20001              13.6   12.0   12.4   13.4   15.2   22.8   80
-    //   32 of up to 8192                                      25.9          29.2  43.5
-    //   4 of up to 65536                                      28.2          33.4   -
-    //   64 of up to 8192, 64 heads       64.1   64.1   64.1   64.0   64.1   63.4  59.5
-    //   128 lists of 64                  20.6   18.0   17.3   18.0   19.3   22.5  22.5
-    //   120 lists of 24, heads of 256    20.3   19.8   20.7   19.2   19.2   19.2  19.2
-    //   2 of up to 359 on 5025, 8 heads                30.5   28.0                23.2
-    const int64_t most = list ? query->list : most_pages(*query);
-    const bool several = !list && query_rows(*desc, *query) > 64;
+    const int64_t slots = desc->head_dim > 128 ? 512 : 768;   // workgroups that run at a time
+    // Lists are of one length: half of the workgroups that run at a time, each with more
+    // pages to hide latencies behind; windows mostly: all of them.  Sequences are of
+    // different lengths, of which the call knows the longest: if they were all as long,
+    // 7/4 of what runs at a time, which is about all of it when they are not.  Where a sequence has several tiles
+    // already, 512, and states of all their rows to store and join.  Measured in graphs
+    // (us, heads of 128, 32 on 8, or lists, if not said otherwise):
+    //   pages a workgroup                  8     12     16     24     32     48     64    all
+    //   1 sequence of 20001              15.2   13.3   13.6   14.4   16.2          23.9   84
+    //   32 of up to 8192                 32.0   30.5   29.3   25.8   27.5          30.0   43.4
+    //   4 of up to 65536                 38.4   36.3   32.3   29.6   29.9          33.9  297
+    //   64 of up to 8192, 64 heads       47.0   46.6   46.5   46.4   45.6   42.9   45.4   50.1
+    //   48 of up to 12000, 64 heads                           52.0   50.3   46.3   47.8   67.8
+    //   128 lists of 64                  21.6   18.9   17.5   17.7   18.2          24.2   24.3
+    //   120 lists of 24, heads of 256    21.5   18.7   20.1   20.2   20.2   20.2   20.2   20.2
+    //   2 of up to 359 on 5025, 8 heads  38.8   31.7   30.3   27.1   27.5          25.0   23.3
+    //   16 of 5 on 4096, 24 on 4 of 64   18.0   15.5   16.7   15.6   17.6          21.8   20.9
+    const int64_t seen = most_pages(*query);
+    const int64_t most = list ? std::min<int64_t>(query->list, seen) : seen;
+    const int64_t each = query_rows(*desc, *query);
+    const bool several = !list && each > 64;
+    // the grid has room for sequences that share a tile's rows; mostly none do
+    const int64_t likely = (int64_t)(list ? query->tokens : query->seqs) *
+                           ((each + rows - 1) / rows) * desc->kv_heads;
     const Split s =
         rows == 128
-            ? split_pages(units, most, 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8)
-            : split_pages(units, most, 0.25 + 0.4 * size,
-                          (1 + 2.5 * size) * (several ? 2.5 : 1.0),
-                          list || query->window ? 512 : several ? 768 : 1500,
-                          kMostParts * 16 / rows);
+            ? split_pages(units, likely, most, 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8, 1)
+            : split_pages(units, likely, most, 0.4 + 0.4 * size,
+                          (0.5 + 1.3 * size) * (several ? 2.5 : 1.0),
+                          list ? slots / 2 : query->window ? slots : several ? 512 : 7 * slots / 4,
+                          kMostParts * 16 / rows, 4);
     // Loads past the caches where no other tile reads the same pages and the whole keeps
     // the memory busy: 64 sequences of up to 8192 tokens, 64 heads of 128 on 8 (238 MB),
     // 59.5 -> 52.6 us; 512 lists of 64 pages (143 MB) 39.5 -> 36.1; but where latency
     // counts (32 sequences of up to 53109, 16 heads on one, 76 MB: 44 -> 53) or lines are
     // read in two halves (other head sizes) they are slower.  The bounds are of what the
     // call could read, which for sequences is a few times what it does.
-    const bool once = query_rows(*desc, *query) <= 16 &&
+    const bool once = each <= 16 &&
                       68.0 * desc->head_dim * most * units >= (list ? 256 << 20 : 768 << 20);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
@@ -351,7 +364,7 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
     // a window hides pages but does not renumber them: all up to the last count
     lce_kv4_query_desc all = *query;
     all.window = 0;
-    const Split s = split_pages(units, most_pages(all), 0.5, 2, 2048, kMostParts);
+    const Split s = split_pages(units, units, most_pages(all), 0.5, 2, 2048, kMostParts, 1);
     lce::kv4::SelectParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.keep_first = keep_first, p.keep_last = keep_last;
