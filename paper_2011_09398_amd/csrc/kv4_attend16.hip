@@ -330,9 +330,9 @@ struct Shared {
 // Bound by memory where a call reads much, by the latencies in a row (launch,
 // lengths, table, a page, the states out, the ticket, the states in) where it does
 // not.  Measured, us: 64 sequences of up to 8192 tokens, 64 heads of 128 on 8, bfloat16
-// (238 MB) 52.4, 4.6 TB/s with the launch; one sequence of 20001, 32 heads on 8
-// (22 MB) 12.1, of which the joining of the splits takes more than 2; 128 lists of 64 pages
-// (61 MB) 17.1.  Loads of a page's keys and values are 16 bytes a lane, and one page
+// (238 MB) 52.3, 4.6 TB/s with the launch; one sequence of 20001, 32 heads on 8
+// (22 MB) 12.0, of which the joining of the splits takes 3; 128 lists of 64 pages
+// (61 MB) 15.9.  Loads of a page's keys and values are 16 bytes a lane, and one page
 // is on its way while another is worked on: 12 waves of a CU hide the rest.
 template <typename E, int D, bool LIST, int C, bool ONCE>
 __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16_kernel(
@@ -483,8 +483,12 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
 #pragma unroll
         for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], p.scale_log2);
         if (more) keys.template load<ONCE>(rec, n, g);
+        // ahead of the other waves' scores: 1 to 3 % (heads of 256, 128 rows on 65536
+        // tokens: 386 -> 376 us)
+        __builtin_amdgcn_s_setprio(1);
         add_values<E, D, C, 0, 0>(st, values, w);
         add_values<E, D, C, 1, 0>(st, values, w);
+        __builtin_amdgcn_s_setprio(0);
         if (more) values.template load<ONCE>(rec, n, g);
     }
 #pragma unroll

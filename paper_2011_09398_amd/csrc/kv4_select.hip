@@ -152,9 +152,9 @@ __device__ __forceinline__ void choose(const uint16_t *ranks, int pages, const S
 // chosen pages in order.
 //
 // Bound by memory where contexts are long: 32 sequences of up to 32768 tokens, 64 heads
-// of 128 on 8 (50 MB of signs) take 22.3 us, of which the scores take 10 (5 TB/s), the
+// of 128 on 8 (50 MB of signs) take 22.1 us, of which the scores take 10 (5 TB/s), the
 // ticket and the choice 3.7, and the launch and all before the first page the rest.
-// Small calls are launches: 8 sequences of up to 8192 tokens, 32 heads on 8, 8.4 us.
+// Small calls wait for the host: 8 sequences of up to 8192 tokens, 32 heads on 8, 7.6 us.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void select_kernel(SelectParams p) {
     constexpr int W = D / 32, U = 4;
