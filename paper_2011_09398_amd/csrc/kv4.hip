@@ -145,7 +145,7 @@ struct Split {
 // is a multiple of it, so that all waves are busy to the end.
 Split split_pages(int64_t units, int64_t likely, int64_t pages, double step, double fixed,
                   int64_t most, int64_t parts, int64_t each) {
-    const int64_t some = std::max<int64_t>(std::min(units, likely), 1);
+    const int64_t some = std::max<int64_t>(likely, 1);
     const int64_t room = std::min<int64_t>(
         std::max<int64_t>(parts / std::max<int64_t>(units, 1), 1), lce::kv4::kMostSplits);
     int64_t chunk = std::max<int64_t>(pages, 1);
@@ -294,9 +294,10 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     const int64_t most = list ? std::min<int64_t>(query->list, seen) : seen;
     const int64_t each = query_rows(*desc, *query);
     const bool several = !list && each > 64;
-    // the grid has room for sequences that share a tile's rows; mostly none do
-    const int64_t likely = (int64_t)(list ? query->tokens : query->seqs) *
-                           ((each + rows - 1) / rows) * desc->kv_heads;
+    // the grid has a tile to spare for each sequence; most calls have fewer (counted in
+    // floating point: max_q is the caller's word)
+    const double spread = (list ? query->tokens : query->seqs) * (double)desc->kv_heads;
+    const int64_t likely = (int64_t)std::min((double)units, spread * ((each + rows - 1) / rows));
     const Split s =
         rows == 128
             ? split_pages(units, likely, most, 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8, 1)

@@ -298,6 +298,14 @@ def test_hints_that_are_wrong_cost_no_result():
         attend(b, max_q=max_q, max_len=max_len)
 
 
+@pytest.mark.parametrize("window", [0, 30])
+def test_hints_at_the_ends_of_their_range(window):
+    b = Batch(75, [900, 64, 1, 200], [1, 2, 1, 3], 8, 2, 128, "bf16")
+    for max_q in (1, 2 ** 31 - 1):
+        for max_len in (1, 2 ** 31 - 1):
+            attend(b, window=window, max_q=max_q, max_len=max_len)
+
+
 def test_strided_queries_and_scale():
     b = Batch(10, [100, 50], [3, 50], 6, 3, 64, "bf16")
     cache, q, table, start, lengths = b.device(lce)
