@@ -465,7 +465,9 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  *   lse     float32 [tokens][q_heads] or NULL
  *   workspace, workspace_bytes: see lce_kv4_workspace_size
  * A query row that holds an infinity or a NaN gives NaN.  With LCE_FLOAT16,
- * cached values of 65536 and more count as infinities, as in lce_kv4_read.
+ * cached values of 65536 and more count as 65504, the largest float16 (and
+ * -65536 and less as -65504), not as the infinities that lce_kv4_read makes of
+ * them; what shares a scale with them is not affected.
  * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
  *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
  *         table_width over 2^24, more rows or tiles than a grid holds),

@@ -14,10 +14,7 @@ struct Bf16 {
     typedef bf16x8 T8;
     // pieces of 4 significant bits (and a sign each) that hold any bfloat16
     static constexpr int kPieces = 2;
-    // the largest scale byte a finite value can have, for tokens that a row
-    // does not see (their weight is 0, and 0 times what the bytes decode to has
-    // to be 0): 6 * 2^125 is finite in bfloat16
-    static constexpr uint32_t kMaxScale = 252;
+    static constexpr bool kSaturates = false;   // holds every finite cached value
     static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
@@ -31,7 +28,7 @@ struct F16 {
     typedef f16x2 T2;
     typedef f16x8 T8;
     static constexpr int kPieces = 3;
-    static constexpr uint32_t kMaxScale = 140;   // 6 * 2^13 is finite in float16
+    static constexpr bool kSaturates = true;    // cached values of 65536 and more: see below
     static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
@@ -40,14 +37,49 @@ struct F16 {
     }
 };
 
-// Two codes (byte BYTE of c) as a packed pair of E::T, times a power of two.
-template <typename E, int BYTE>
+// The largest scale byte of a finite value: 6 * 2^125.
+constexpr uint32_t kMaxScale = 252;
+
+// Two codes (byte BYTE of c) as a packed pair of E::T, times a power of two; SAT: of
+// float16's range, the nearest to it.
+template <typename E, int BYTE, bool SAT = false>
 __device__ __forceinline__ uint32_t decode_pair(uint32_t c, float s) {
-    if constexpr (__is_same(typename E::T, __bf16))
+    if constexpr (__is_same(typename E::T, __bf16)) {
         return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, BYTE));
-    else
-        return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, BYTE));
+    } else {
+        f16x2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, BYTE);
+        if constexpr (SAT) {
+            constexpr f16x2 most = {(_Float16)65504.0f, (_Float16)65504.0f};
+            x = __builtin_elementwise_max(__builtin_elementwise_min(x, most), -most);
+        }
+        return bits_as<uint32_t>(x);
+    }
 }
+
+// What the scale bytes of the values of tokens first .. first + 3 (byte i: first + i)
+// become on a page that not every row sees whole, [lo, hi) being what some row sees: a
+// hidden token's weight is 0, and 0 times its values has to be 0.  Tokens that no row
+// sees stand for next to nothing, whatever their bytes are, and those that some row
+// sees for what they are; a group that is not finite has codes 0, and its key the NaN.
+__device__ __forceinline__ uint32_t settled(uint32_t scale, int first, int lo, int hi) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (first + i >= lo && first + i < hi)
+            w |= min(scale >> (8 * i) & 255u, kMaxScale) << (8 * i);
+    return w;
+}
+
+// The highest bit of those of four scale bytes that are past 140, the largest with which
+// every code is finite in float16: 6 * 2^13.  The values under such a scale are decoded
+// with saturation (an infinity times a weight of 0 would be NaN), the others are spared
+// its two instructions a pair.
+__device__ __forceinline__ uint32_t past_float16(uint32_t scale) {
+    return ((scale & 0x7F7F7F7Fu) + 0x73737373u) & scale & 0x80808080u;
+}
+
+// All bits of the bytes whose highest bit is set.
+__device__ __forceinline__ uint32_t whole_bytes(uint32_t top) { return (top - (top >> 7)) | top; }
 
 template <typename E>
 __device__ __forceinline__ uint32_t pack_pair(float a, float b) {

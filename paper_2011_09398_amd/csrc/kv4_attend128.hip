@@ -67,18 +67,19 @@ struct Page {
     u32x4 unit[4][2][D];
 };
 
-template <typename E, int D, int B>
+template <typename E, int D, int B, bool SAT = false>
 __device__ __forceinline__ void store_values(Page<D> &page, const Values<D> &x, int quarter, int r,
                                              int g) {
     if constexpr (B < D / 32) {
         constexpr int G = D / 32;   // bytes of a token
         const uint32_t w = x.scale;
-        const uint32_t x0 = decode_pair<E, B % 4>(x.v[B / 4], bits_as<float>(w << 23));
-        const uint32_t x1 = decode_pair<E, (G + B) % 4>(x.v[(G + B) / 4], bits_as<float>(w << 15));
+        const uint32_t x0 = decode_pair<E, B % 4, SAT>(x.v[B / 4], bits_as<float>(w << 23));
+        const uint32_t x1 =
+            decode_pair<E, (G + B) % 4, SAT>(x.v[(G + B) / 4], bits_as<float>(w << 15));
         const uint32_t x2 =
-            decode_pair<E, (2 * G + B) % 4>(x.v[(2 * G + B) / 4], bits_as<float>(w << 7));
+            decode_pair<E, (2 * G + B) % 4, SAT>(x.v[(2 * G + B) / 4], bits_as<float>(w << 7));
         const uint32_t x3 =
-            decode_pair<E, (3 * G + B) % 4>(x.v[(3 * G + B) / 4], bits_as<float>(w >> 1));
+            decode_pair<E, (3 * G + B) % 4, SAT>(x.v[(3 * G + B) / 4], bits_as<float>(w >> 1));
         // two tokens of a channel side by side
         const u32x2 even = {__builtin_amdgcn_perm(x1, x0, 0x05040100u),
                             __builtin_amdgcn_perm(x3, x2, 0x05040100u)};
@@ -87,7 +88,7 @@ __device__ __forceinline__ void store_values(Page<D> &page, const Values<D> &x, 
         u32x2 *to = reinterpret_cast<u32x2 *>(&page.unit[quarter][g % 2][r]) + g / 2;
         to[2 * 16 * (2 * B)] = even;
         to[2 * 16 * (2 * B + 1)] = odd;
-        store_values<E, D, B + 1>(page, x, quarter, r, g);
+        store_values<E, D, B + 1, SAT>(page, x, quarter, r, g);
     }
 }
 
@@ -289,16 +290,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         keys.load(rec, n, h);
         values.load(rec, wave, r, g);
     };
-    // what the scales of tokens that some row does not see stand for is made finite:
-    // their weight is 0, whatever the bytes are
     const auto settle = [&](int of) {
-        if (of * kPage < z.lo || of * kPage + kPage > a.hi) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                w |= min(values.scale >> (8 * k) & 255u, E::kMaxScale) << (8 * k);
-            values.scale = w;
-        }
+        const int t0 = of * kPage;
+        if (t0 < z.lo || t0 + kPage > a.hi)
+            values.scale = settled(values.scale, 16 * wave + 4 * g, a.lo - t0, z.hi - t0);
+    };
+    // whether the wave's quarter of a page has values past float16's range; it is then
+    // stored once more, behind the ordinary place, the order of which a branch would break
+    const auto past_range = [&]() {
+        if constexpr (!E::kSaturates) return false;
+        return __builtin_amdgcn_ballot_w64(past_float16(values.scale) != 0) != 0;
+    };
+    bool past = false;
+    const auto saturate = [&](Page<D> &page) {
+        if (__builtin_expect(past, 0)) store_values<E, D, 0, E::kSaturates>(page, values, wave, r, g);
     };
     // weights of 16 scores, two second operands of 16 tokens each
     f32x16 s[2];
@@ -334,6 +339,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         load(number);
         settle(number);
         store_values<E, D, 0>(pages[0], values, wave, r, g);
+        past = past_range();
+        saturate(pages[0]);
         s[0] = scores<E, D, 0>(keys, q, n);
         s[1] = scores<E, D, 1>(keys, q, n);
         fetch();
@@ -346,12 +353,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         if (more) settle(following);
         if (t0 < wz.hi && t0 + kPage > wa.lo) {
             if (t0 < wz.lo || t0 + kPage > wa.hi) {
-                const int lo = span.lo - t0, hi = span.hi - t0;
+                const int lo = span.lo - t0 - 4 * h, hi = span.hi - t0 - 4 * h;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const int j = 32 * t + 8 * (k / 4) + 4 * h + k % 4;
+                        const int j = 32 * t + 8 * (k / 4) + k % 4;
                         s[t][k] = j >= lo && j < hi ? s[t][k] : -__builtin_inff();
                     }
             }
@@ -390,6 +397,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
             interleave<D / 16 + Keys<D>::kChunks * E::kPieces, 6>();
             __builtin_amdgcn_sched_barrier(0);
             add(1);
+            past = past_range();
             s[1] = scores<E, D, 1>(keys, q, n);
             store_values<E, D, 0>(pages[now ^ 1], values, wave, r, g);
             interleave<D / 16 + Keys<D>::kChunks * E::kPieces, 4>();
@@ -398,8 +406,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         } else {
             s[0] = scores<E, D, 0>(keys, q, n);
             s[1] = scores<E, D, 1>(keys, q, n);
+            past = past_range();
             store_values<E, D, 0>(pages[now ^ 1], values, wave, r, g);
         }
+        saturate(pages[now ^ 1]);
         if (!more) break;
         now ^= 1;
         number = following;

@@ -200,32 +200,32 @@ struct RowState {
 
 // The values of token pairs: byte B of a token's codes holds its channels 2B
 // and 2B+1; a product wants two tokens of one channel side by side.
-template <typename E, int D, int TAU, int B>
+template <typename E, int D, int TAU, int B, bool SAT>
 __device__ __forceinline__ void decode_values(const Values<D> &r, uint32_t (&even)[2],
                                               uint32_t (&odd)[2]) {
     constexpr int G = D / 32;
     // the bits beside the exponent's do not count: a shift makes a scale's byte one
     const uint32_t w = r.scale[TAU];
-    const uint32_t x0 = decode_pair<E, B % 4>(r.v[TAU][B / 4], bits_as<float>(w << 23));
+    const uint32_t x0 = decode_pair<E, B % 4, SAT>(r.v[TAU][B / 4], bits_as<float>(w << 23));
     const uint32_t x1 =
-        decode_pair<E, (G + B) % 4>(r.v[TAU][(G + B) / 4], bits_as<float>(w << 15));
+        decode_pair<E, (G + B) % 4, SAT>(r.v[TAU][(G + B) / 4], bits_as<float>(w << 15));
     const uint32_t x2 =
-        decode_pair<E, (2 * G + B) % 4>(r.v[TAU][(2 * G + B) / 4], bits_as<float>(w << 7));
+        decode_pair<E, (2 * G + B) % 4, SAT>(r.v[TAU][(2 * G + B) / 4], bits_as<float>(w << 7));
     const uint32_t x3 =
-        decode_pair<E, (3 * G + B) % 4>(r.v[TAU][(3 * G + B) / 4], bits_as<float>(w >> 1));
+        decode_pair<E, (3 * G + B) % 4, SAT>(r.v[TAU][(3 * G + B) / 4], bits_as<float>(w >> 1));
     even[0] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
     odd[0] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
     even[1] = __builtin_amdgcn_perm(x3, x2, 0x05040100u);
     odd[1] = __builtin_amdgcn_perm(x3, x2, 0x07060302u);
 }
 
-template <typename E, int D, int C, int U, int B>
+template <typename E, int D, int C, int U, int B, bool SAT>
 __device__ __forceinline__ void add_values(RowState<D> (&st)[C], const Values<D> &r,
                                            const u32x4 (&p)[C][2]) {
     if constexpr (B < D / 32) {
         uint32_t e0[2], o0[2], e1[2], o1[2];
-        decode_values<E, D, 2 * U, B>(r, e0, o0);
-        decode_values<E, D, 2 * U + 1, B>(r, e1, o1);
+        decode_values<E, D, 2 * U, B, SAT>(r, e0, o0);
+        decode_values<E, D, 2 * U + 1, B, SAT>(r, e1, o1);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             st[c].o[2 * B] =
@@ -233,34 +233,35 @@ __device__ __forceinline__ void add_values(RowState<D> (&st)[C], const Values<D>
             st[c].o[2 * B + 1] =
                 E::mfma16(u32x4{o0[0], o0[1], o1[0], o1[1]}, p[c][U], st[c].o[2 * B + 1]);
         }
-        add_values<E, D, C, U, B + 1>(st, r, p);
+        add_values<E, D, C, U, B + 1, SAT>(st, r, p);
     }
 }
 
-// Hides the tokens outside [lo, hi) (this row's visible ones, counted from the
-// page's first).
-__device__ __forceinline__ void hide(f32x4 (&s)[4], int lo, int hi, int g) {
+// Hides the tokens outside [lo, hi) (this row's visible ones, counted from the lane's
+// first: 4g on the page, so that constants are compared with two registers).
+__device__ __forceinline__ void hide(f32x4 (&s)[4], int lo, int hi) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int j = 16 * t + 4 * g + i;
+            const int j = 16 * t + i;
             s[t][i] = j >= lo && j < hi ? s[t][i] : -__builtin_inff();
         }
 }
 
-// Makes what the scales of tokens stand for finite: a hidden token's weight is 0,
-// and 0 times its values has to be 0 whatever the page's unwritten bytes are.
+// Takes the values past the type's range out of a page (their scale to almost nothing);
+// whether some lane had one.
 template <typename E, int D>
-__device__ __forceinline__ void settle(Values<D> &r) {
+__device__ __forceinline__ bool take_past_range(Values<D> &r) {
+    if constexpr (!E::kSaturates) return false;
+    const uint32_t any = past_float16(r.scale[0]) | past_float16(r.scale[1]) |
+                         past_float16(r.scale[2]) | past_float16(r.scale[3]);
+    const bool past = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+    if (__builtin_expect(past, 0)) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w |= min(r.scale[t] >> (8 * i) & 255u, E::kMaxScale) << (8 * i);
-        r.scale[t] = w;
+        for (int t = 0; t < 4; ++t) r.scale[t] &= ~whole_bytes(past_float16(r.scale[t]));
     }
+    return past;
 }
 
 // A page's scores into the rows' maximum and sum; its weights, ready to be
@@ -449,12 +450,18 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     Keys<D> keys;
     Values<D> values;
     int number = 0;
+    const uint8_t *now = nullptr;
     const bool any = todo != 0;
     if (any) {
-        const uint8_t *rec = next(number);
-        keys.template load<ONCE>(rec, n, g);
-        values.template load<ONCE>(rec, n, g);
+        now = next(number);
+        keys.template load<ONCE>(now, n, g);
+        values.template load<ONCE>(now, n, g);
     }
+    const auto settle = [&](Values<D> &v, int t0) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            v.scale[t] = settled(v.scale[t], 16 * t, a.lo - t0 - 4 * g, z.hi - t0 - 4 * g);
+    };
     Queries<E, D> q[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) make_pieces<E, D>(q[c], raw[c], g);
@@ -476,20 +483,32 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         if (more) rec = next(number);
         if (masked) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) hide(s[c], span[c].lo - t0, span[c].hi - t0, g);
-            settle<E, D>(values);
+            for (int c = 0; c < C; ++c) hide(s[c], span[c].lo - t0 - 4 * g, span[c].hi - t0 - 4 * g);
+            settle(values, t0);
         }
         u32x4 w[C][2];
 #pragma unroll
         for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], p.scale_log2);
         if (more) keys.template load<ONCE>(rec, n, g);
+        const bool past = take_past_range<E, D>(values);
         // ahead of the other waves' scores: 1 to 3 % (heads of 256, 128 rows on 65536
         // tokens: 386 -> 376 us)
         __builtin_amdgcn_s_setprio(1);
-        add_values<E, D, C, 0, 0>(st, values, w);
-        add_values<E, D, C, 1, 0>(st, values, w);
+        add_values<E, D, C, 0, 0, false>(st, values, w);
+        add_values<E, D, C, 1, 0, false>(st, values, w);
         __builtin_amdgcn_s_setprio(0);
+        // the values past the range from memory once more, and saturated: a second set of
+        // them here would cost registers everywhere
+        if (__builtin_expect(past, 0)) {
+            values.template load<ONCE>(now, n, g);
+            if (masked) settle(values, t0);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) values.scale[t] &= whole_bytes(past_float16(values.scale[t]));
+            add_values<E, D, C, 0, 0, E::kSaturates>(st, values, w);
+            add_values<E, D, C, 1, 0, E::kSaturates>(st, values, w);
+        }
         if (more) values.template load<ONCE>(rec, n, g);
+        now = rec;
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {

@@ -1,0 +1,107 @@
+"""Attention over the 4-bit cache at the ends of its types' ranges, against the definition in
+64 bits (kv4_util)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2011_09398_amd as lce
+from tests.kv4_util import PAGE, Batch
+
+pytestmark = pytest.mark.gpu
+
+MOST = 65504.0        # the largest float16
+
+
+def check(b, out, lse, scale, causal=True, window=0, pages=None):
+    want, want_lse, bound, lse_bound = b.attention(scale, causal, window, pages)
+    off = np.abs(out.cpu().double().numpy() - want)
+    assert (off <= bound).all(), (np.argwhere(~(off <= bound))[:5], np.nanmax(off / bound))
+    got = lse.cpu().double().numpy()
+    empty = np.isinf(want_lse)
+    assert np.array_equal(np.isneginf(got), empty)
+    assert (np.abs(got[~empty] - want_lse[~empty]) <= lse_bound[~empty]).all()
+
+
+def attend(b, causal=True, window=0, pages=None, scale=None):
+    scale = b.dim ** -0.5 if scale is None else scale
+    dev = None if pages is None else torch.from_numpy(pages).cuda()
+    return lce.kv4_attention(*b.device(lce), scale=scale, causal=causal, window=window, pages=dev,
+                             return_lse=True)
+
+
+# ---- float16 queries over values that float16 does not hold: they count as +-65504, on
+# ---- whole pages and on others, and what shares their scales keeps its own values
+
+def large_values(seed, lengths, dim, heads):
+    """Every ninth token of a head has a group of values around 2^14 to 2^18, with small ones
+    among them (code 1 of a scale of 2^14 to 2^17), a few tokens around 2^60."""
+    rng = np.random.default_rng(seed)
+    odd = []
+    for b, n in enumerate(lengths):
+        for h in range(heads):
+            for j in range(h, n, 9):
+                g = int(rng.integers(0, dim // 32))
+                up = 2.0 ** (60 if j % 5 == 0 else int(rng.integers(13, 17)))
+                x = rng.uniform(-4, 4, 32) * np.where(rng.random(32) < 0.5, 0.2, 1.0)
+                odd += [(b, j, h, 32 * g + c, "v", x[c] * up) for c in range(32)]
+    return odd
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 70)])
+def test_values_past_float16(dim, rows, causal, window):
+    lengths, queries = [200, 128, 77, 130], [1, 90, 5, 130]
+    b = Batch(31, lengths, queries, 4, 2, dim, "f16", odd=large_values(dim, lengths, dim, 2))
+    assert max(np.abs(v).max() for v in b.v) > MOST
+    b.v = [np.clip(v, -MOST, MOST) for v in b.v]
+    for chunk in (0, 1):
+        with lce.tuning(kv4_rows=rows, kv4_chunk=chunk):
+            out, lse = attend(b, causal, window)
+        check(b, out, lse, dim ** -0.5, causal, window)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_values_past_float16_in_lists(dim):
+    lengths, queries = [300, 70], [2, 1]
+    b = Batch(32, lengths, queries, 8, 2, dim, "f16", odd=large_values(7, lengths, dim, 2))
+    b.v = [np.clip(v, -MOST, MOST) for v in b.v]
+    pages = np.full((3, 2, 4), -1, np.int32)
+    pages[:2, 0, :3], pages[:2, 1, :4], pages[2, :, :2] = [0, 2, 4], [4, 1, 3, 0], [0, 1]
+    out, lse = attend(b, pages=pages)
+    check(b, out, lse, dim ** -0.5, pages=pages)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+def test_float16_results_do_not_depend_on_the_page_being_whole(dim, rows):
+    """One token of 65536 beside 16384 in one group: alone on its page, and with 64 tokens."""
+    odd = [(0, 0, 0, 0, "v", 65536.0), (0, 0, 0, 1, "v", 16384.0), (0, 0, 0, 2, "v", -2.0 ** 17)]
+    with lce.tuning(kv4_rows=rows):
+        for n in (1, PAGE):
+            b = Batch(33, [n], [1], 1, 1, dim, "f16", odd=odd)
+            b.k[0][:] = 0                              # equal scores: the mean of the values
+            b.q[:] = 0
+            b.v = [np.clip(v, -MOST, MOST) for v in b.v]
+            out, lse = attend(b)
+            check(b, out, lse, dim ** -0.5)
+            if n == 1:
+                assert out[0, 0, :3].tolist() == [MOST, 16384.0, -MOST]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("byte", [141, 252, 254])
+def test_bytes_of_slots_never_written_do_not_count(dtype, dim, rows, byte):
+    """Codes 6 and scales of any size past the sequences' ends leave no trace."""
+    b = Batch(34, [100, 70, 3], [40, 2, 1], 4, 2, dim, dtype)
+    with lce.tuning(kv4_rows=rows):
+        clean = attend(b)
+        for s, n in enumerate(b.lengths):
+            for t in range(n % PAGE, PAGE):
+                rec = b.cache.data[b.table[s, n // PAGE]]
+                for part, fill in zip(b.cache.places(t), (0x77, 0x77, byte, byte, 0x55)):
+                    rec[:, part] = fill
+        junk = attend(b)
+    assert torch.equal(clean[0], junk[0]) and torch.equal(clean[1], junk[1])
