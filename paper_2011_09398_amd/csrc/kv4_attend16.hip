@@ -276,8 +276,9 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)
     top *= c;
     // The maximum that weights are taken against follows the true one only when
     // that has passed it by 2^8: weights up to 256 cost no precision, and most
-    // pages then need neither the exchange between lanes nor the rescaling.
-    if (__builtin_amdgcn_ballot_w64(top > st.m + 8.0f)) {
+    // pages then need neither the exchange between lanes nor the rescaling.  (Of large
+    // maxima, the difference is exact where the sum is not.)
+    if (__builtin_amdgcn_ballot_w64(top - st.m > 8.0f)) {
         const float all =
             fmaxf(st.m, across_rows(top, [](float a, float b) { return fmaxf(a, b); }));
         const float f = __builtin_amdgcn_exp2f(st.m - all);

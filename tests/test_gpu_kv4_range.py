@@ -105,3 +105,38 @@ def test_bytes_of_slots_never_written_do_not_count(dtype, dim, rows, byte):
                     rec[:, part] = fill
         junk = attend(b)
     assert torch.equal(clean[0], junk[0]) and torch.equal(clean[1], junk[1])
+
+
+# ---- weights and scores at the ends of their ranges
+
+def fill(cache, keys, values):
+    """keys, values [tokens, dim] of the cache's only head, in pages in order; the call's
+    table, q_start and lengths for one sequence with one new token."""
+    n = keys.shape[0]
+    lce.kv4_append(cache, keys.cuda().bfloat16()[:, None].contiguous(),
+                   values.cuda().bfloat16()[:, None].contiguous(), torch.arange(n).cuda())
+    return (torch.arange(cache.pages, dtype=torch.int32).cuda()[None].contiguous(),
+            torch.tensor([0, 1], dtype=torch.int32).cuda(),
+            torch.tensor([n], dtype=torch.int32).cuda())
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+def test_scores_whose_last_place_is_sixteen(dtype, rows):
+    """Scores of 2^27 + 16, then of 2^27 + 32 (log2): adjacent float32, 16 apart.  Weights
+    of 2^16 would be past float16."""
+    scale = np.float32(1 / np.log2(np.e))
+    while scale * np.float32(np.log2(np.e)) != 1:
+        scale = np.nextafter(scale, np.float32(0))
+    keys, values = torch.zeros(300, 64), torch.ones(300, 64)
+    keys[:, 0], keys[:, 32], keys[256:, 32], values[256:] = 2.0 ** 27, 16, 32, 2
+    q = torch.zeros(1, 1, 64, dtype=dtype)
+    q[..., 0] = q[..., 32] = 1
+    cache = lce.KV4Cache(1, 64, pages=5)
+    with lce.tuning(kv4_rows=rows, kv4_chunk=5):
+        out, lse = lce.kv4_attention(cache, q.cuda(), *fill(cache, keys, values),
+                                     scale=float(scale), return_lse=True)
+    # 44 tokens of 2, and 256 of 1 that weigh 2^-16 each: within 4e-5 of 2
+    assert (out == 2).all()
+    # the maximum and the sum's logarithm (6), in a last place of 16; then of 8
+    assert abs(lse.item() - (2.0 ** 27 + 32 + np.log2(44)) * np.log(2)) <= 8 + 4 + 8
