@@ -305,18 +305,22 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     const auto saturate = [&](Page<D> &page) {
         if (__builtin_expect(past, 0)) store_values<E, D, 0, E::kSaturates>(page, values, wave, r, g);
     };
-    // weights of 16 scores, two second operands of 16 tokens each
+    // weights of 16 scores, two second operands of 16 tokens each; summed by themselves:
+    // a long sequence's many small ones would be rounded one by one to the last place of
+    // a large sum
     f32x16 s[2];
     u32x4 w[4];
     const auto weigh = [&](int t, float c) {
+        float sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < 16; k += 2) {
             const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k], c, -top));
             const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k + 1], c, -top));
-            l += x;
-            l += y;
+            sum += x;
+            sum += y;
             w[2 * t + k / 8][k % 8 / 2] = pack_pair<E>(x, y);
         }
+        l += sum;
     };
     const auto add = [&](int t) {
 #pragma unroll

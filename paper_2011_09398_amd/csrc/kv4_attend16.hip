@@ -294,17 +294,21 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)
         for (int t = 0; t < 4; ++t) s[t] *= c;
         c = 1.0f;
     }
+    // a page's weights are summed by themselves: a long sequence's many small ones would
+    // be rounded one by one to the last place of a large sum
+    float sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         float w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, -st.m));
-            st.l += w[i];
+            sum += w[i];
         }
         p[t / 2][t % 2 * 2] = pack_pair<E>(w[0], w[1]);
         p[t / 2][t % 2 * 2 + 1] = pack_pair<E>(w[2], w[3]);
     }
+    st.l += sum;
 }
 
 // The waves' states, where they are joined: sums four channels at a time, rows next

@@ -140,3 +140,27 @@ def test_scores_whose_last_place_is_sixteen(dtype, rows):
     assert (out == 2).all()
     # the maximum and the sum's logarithm (6), in a last place of 16; then of 8
     assert abs(lse.item() - (2.0 ** 27 + 32 + np.log2(44)) * np.log(2)) <= 8 + 4 + 8
+
+
+def one_large(gap, dtype, rows, n=65536):
+    """Attention over one token in each of the first four pages that weighs e^gap times as
+    much as each of n - 4 others, whose values are 1; what the others weigh together."""
+    keys, values = torch.zeros(n, 64), torch.ones(n, 64)
+    keys[0:256:64, 0], values[0:256:64] = 1, 0
+    q = torch.zeros(1, 1, 64, dtype=dtype)
+    q[..., 0] = 1
+    cache = lce.KV4Cache(1, 64, pages=n // PAGE)
+    with lce.tuning(kv4_rows=rows, kv4_chunk=n // PAGE):
+        out, lse = lce.kv4_attention(cache, q.cuda(), *fill(cache, keys, values), scale=gap,
+                                     return_lse=True)
+    return out.cpu().double().numpy(), lse.item(), (n - 4) * np.exp(-gap)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("gap", [5.0, 16.0, 17.0, 17.4])
+def test_sums_of_many_small_weights_beside_a_large_one(dtype, rows, gap):
+    """Sums of weights lose 2^-24 of the largest term at each of at most 4096 additions (16
+    of a page, 1024 pages)."""
+    _, lse, small = one_large(gap, dtype, rows)
+    assert abs(lse - (gap + np.log(4 + small))) <= 4096 * 2.0 ** -24 + 2.0 ** -18
