@@ -448,7 +448,8 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)
  * with k and v as the cache holds them.  Products are exact and sums, the
  * running maximum and the running sum are float32; softmax weights are rounded
- * to `type` where they multiply the values, and out is rounded to it once.
+ * to `type` where they multiply the values (float16: with a last place of at
+ * most 2^-31 of a row's largest weight), and out is rounded to it once.
  * A row that sees nothing is 0 with lse -infinity.
  *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
  *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a

@@ -65,8 +65,8 @@ __device__ __forceinline__ float across_rows(float x, F f) {
 // token exp2(-infinity - kNone) = 0.
 constexpr float kNone = -3.402823466e38f;
 
-// Scores (log2) from which half a last place passes a half.
-constexpr float kLarge = 16777216.0f;
+// Scores (log2) up to which half a last place is at most a half, 2^kLag more included.
+constexpr float kLarge = 8388608.0f;
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 

@@ -15,6 +15,7 @@ struct Bf16 {
     // pieces of 4 significant bits (and a sign each) that hold any bfloat16
     static constexpr int kPieces = 2;
     static constexpr bool kSaturates = false;   // holds every finite cached value
+    static constexpr float kLift = 0.0f;
     static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
@@ -29,6 +30,10 @@ struct F16 {
     typedef f16x8 T8;
     static constexpr int kPieces = 3;
     static constexpr bool kSaturates = true;    // cached values of 65536 and more: see below
+    // Weights are taken against 2^-7 of the largest score's, so that they are at most
+    // 2^15 (see kLag) and the small ones lose no bits above 2^-21 of the largest and
+    // are not dropped above 2^-32, of which a long context has many.
+    static constexpr float kLift = 7.0f;
     static __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
@@ -36,6 +41,11 @@ struct F16 {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(bits_as<T8>(a), bits_as<T8>(b), c, 0, 0, 0);
     }
 };
+
+// Weights are taken against a maximum that follows the true one only when that has
+// passed it by 2^kLag (beyond kLift): they cost no precision, and most pages then need
+// neither the exchange between lanes nor the rescaling.
+constexpr float kLag = 8.0f;
 
 // The largest scale byte of a finite value: 6 * 2^125.
 constexpr uint32_t kMaxScale = 252;

@@ -372,10 +372,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
 #pragma unroll
                 for (int k = 0; k < 16; ++k) high = fmaxf(high, s[t][k]);
             high *= p.scale_log2;
-            // weights are taken against a maximum that follows the true one when it is
-            // 2^8 behind (the difference of large ones is exact where the sum is not)
-            if (__builtin_amdgcn_ballot_w64(high - top > 8.0f)) {
-                const float all = fmaxf(top, across_halves(high, false));
+            // (of large maxima, the difference is exact where a sum is not)
+            if (__builtin_amdgcn_ballot_w64(high - top > kLag + E::kLift)) {
+                const float all = fmaxf(top, across_halves(high, false) - E::kLift);
                 const float f = __builtin_amdgcn_exp2f(top - all);
                 top = all;
                 l *= f;

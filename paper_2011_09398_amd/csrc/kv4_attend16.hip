@@ -274,13 +274,10 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
     top *= c;
-    // The maximum that weights are taken against follows the true one only when
-    // that has passed it by 2^8: weights up to 256 cost no precision, and most
-    // pages then need neither the exchange between lanes nor the rescaling.  (Of large
-    // maxima, the difference is exact where the sum is not.)
-    if (__builtin_amdgcn_ballot_w64(top - st.m > 8.0f)) {
-        const float all =
-            fmaxf(st.m, across_rows(top, [](float a, float b) { return fmaxf(a, b); }));
+    // (Of large maxima, the difference is exact where a sum is not.)
+    if (__builtin_amdgcn_ballot_w64(top - st.m > kLag + E::kLift)) {
+        const float all = fmaxf(
+            st.m, across_rows(top, [](float a, float b) { return fmaxf(a, b); }) - E::kLift);
         const float f = __builtin_amdgcn_exp2f(st.m - all);
         st.m = all;
         st.l *= f;
@@ -288,7 +285,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)
         for (int m = 0; m < D / 16; ++m) st.o[m] *= f;
     }
     // The fused product below differs from the rounded one that the maximum is; where
-    // that could show (scores past 2^24), round the scores' products too.
+    // that could show (scores past kLarge), round the scores' products too.
     if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(st.m) > kLarge)) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] *= c;

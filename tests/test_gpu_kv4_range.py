@@ -164,3 +164,19 @@ def test_sums_of_many_small_weights_beside_a_large_one(dtype, rows, gap):
     of a page, 1024 pages)."""
     _, lse, small = one_large(gap, dtype, rows)
     assert abs(lse - (gap + np.log(4 + small))) <= 4096 * 2.0 ** -24 + 2.0 ** -18
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("gap", [5.0, 16.0, 17.0, 17.4])
+def test_many_small_weights_beside_a_large_one(dtype, rows, gap):
+    """A weight is rounded to half a last place of its type, in float16 to half of 2^-24 at
+    least, of which the largest is 2^7 times 2^24; so is the result; and sums lose 2^-24 of
+    the largest term at each of 4096 additions."""
+    out, _, small = one_large(gap, dtype, rows)
+    want = small / (4 + small)
+    ulp = 2.0 ** (-11 if dtype == torch.float16 else -8)
+    bound = want * (2 * ulp + 4096 * 2.0 ** -24)
+    if dtype == torch.float16:
+        bound += 65532 * 2.0 ** -32 / (4 + small) + 2.0 ** -25
+    assert np.abs(out - want).max() <= bound
