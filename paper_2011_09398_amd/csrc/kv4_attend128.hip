@@ -372,9 +372,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
 #pragma unroll
                 for (int k = 0; k < 16; ++k) high = fmaxf(high, s[t][k]);
             high *= p.scale_log2;
-            // (of large maxima, the difference is exact where a sum is not)
+            // (of large maxima, the difference is exact where a sum is not; each row goes by
+            // its own maximum, so that no bit of it depends on the rows beside it)
             if (__builtin_amdgcn_ballot_w64(high - top > kLag + E::kLift)) {
-                const float all = fmaxf(top, across_halves(high, false) - E::kLift);
+                high = across_halves(high, false);
+                const float all = high - top > kLag + E::kLift ? high - E::kLift : top;
                 const float f = __builtin_amdgcn_exp2f(top - all);
                 top = all;
                 l *= f;
@@ -384,10 +386,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
             // the fused product differs from the rounded one that the maximum is: where
             // that could show, round the scores' products too
             float c = p.scale_log2;
-            if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(top) > kLarge)) {
-                s[0] *= c;
-                s[1] *= c;
-                c = 1.0f;
+            const bool large = __builtin_fabsf(top) > kLarge;
+            if (__builtin_amdgcn_ballot_w64(large)) {
+                s[0] = large ? s[0] * c : s[0];
+                s[1] = large ? s[1] * c : s[1];
+                c = large ? 1.0f : c;
             }
             weigh(0, c);
             __builtin_amdgcn_sched_barrier(0);

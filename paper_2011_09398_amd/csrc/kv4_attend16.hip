@@ -274,10 +274,11 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
     top *= c;
-    // (Of large maxima, the difference is exact where a sum is not.)
+    // (Of large maxima, the difference is exact where a sum is not.  Each row goes by
+    // its own maximum, so that no bit of it depends on the rows beside it.)
     if (__builtin_amdgcn_ballot_w64(top - st.m > kLag + E::kLift)) {
-        const float all = fmaxf(
-            st.m, across_rows(top, [](float a, float b) { return fmaxf(a, b); }) - E::kLift);
+        const float high = across_rows(top, [](float a, float b) { return fmaxf(a, b); });
+        const float all = high - st.m > kLag + E::kLift ? high - E::kLift : st.m;
         const float f = __builtin_amdgcn_exp2f(st.m - all);
         st.m = all;
         st.l *= f;
@@ -286,10 +287,11 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[4], u32x4 (&p)
     }
     // The fused product below differs from the rounded one that the maximum is; where
     // that could show (scores past kLarge), round the scores' products too.
-    if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(st.m) > kLarge)) {
+    const bool large = __builtin_fabsf(st.m) > kLarge;
+    if (__builtin_amdgcn_ballot_w64(large)) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) s[t] *= c;
-        c = 1.0f;
+        for (int t = 0; t < 4; ++t) s[t] = large ? s[t] * c : s[t];
+        c = large ? 1.0f : c;
     }
     // a page's weights are summed by themselves: a long sequence's many small ones would
     // be rounded one by one to the last place of a large sum

@@ -180,3 +180,38 @@ def test_many_small_weights_beside_a_large_one(dtype, rows, gap):
     if dtype == torch.float16:
         bound += 65532 * 2.0 ** -32 / (4 + small) + 2.0 ** -25
     assert np.abs(out - want).max() <= bound
+
+
+# ---- rows that have nothing to do with each other
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+def test_a_channel_without_a_number_takes_its_row_alone(value, dtype, dim, rows):
+    b = Batch(44, [70], [2], 4, 2, dim, dtype)
+    with lce.tuning(kv4_rows=rows):
+        clean = attend(b)
+        for c in range(5, dim, 32):
+            q = b.q.clone()
+            b.q[1, 2, c] = value
+            out, lse = attend(b)
+            b.q = q
+            assert out[1, 2].isnan().all() and lse[1, 2].isnan()
+            out[1, 2], lse[1, 2] = clean[0][1, 2], clean[1][1, 2]
+            assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+def test_no_bit_of_a_row_depends_on_the_rows_beside_it(dtype, dim, rows):
+    """A row whose scores grow from page to page, or are past 2^23, among ordinary ones."""
+    b = Batch(45, [400], [2], 4, 1, dim, dtype)
+    with lce.tuning(kv4_rows=rows, kv4_chunk=7):
+        clean = attend(b)
+        for up in (2.0 ** 6, 2.0 ** 15):
+            b.q[1, 2] = (b.q[1, 2].double() / b.q[1, 2].abs().max().double() * up).to(b.q.dtype)
+            out, lse = attend(b)
+            out[1, 2], lse[1, 2] = clean[0][1, 2], clean[1][1, 2]
+            assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
