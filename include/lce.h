@@ -446,10 +446,13 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
 /* Attention of new tokens over the cache: per token and query head
  *     s_j = scale * (q . k_j) over the visible tokens j,
  *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)
- * with k and v as the cache holds them.  Products are exact and sums, the
- * running maximum and the running sum are float32; softmax weights are rounded
- * to `type` where they multiply the values (float16: with a last place of at
- * most 2^-31 of a row's largest weight), and out is rounded to it once.
+ * with k and v as the cache holds them.  Products of queries and keys are exact
+ * of channels that are at least 2^-13 of the largest |q| of their group (of 32
+ * channels, as they share a scale in a key); smaller ones are held to 2^-21 of
+ * it (float16: 2^-25).  Sums, the running maximum and the running sum are
+ * float32; softmax weights are rounded to `type` where they multiply the values
+ * (float16: with a last place of at most 2^-31 of a row's largest weight), and
+ * out is rounded to it once.
  * A row that sees nothing is 0 with lse -infinity.
  *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
  *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a

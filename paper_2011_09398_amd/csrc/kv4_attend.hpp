@@ -97,26 +97,48 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
     return bits_as<uint32_t>(v);
 }
 
-// A row's scale and the next piece of its values: a query row is multiplied in
-// 8-bit floats (e4m3) against the 4-bit keys.  With E = floor(log2 max|q|) the
-// first piece is q * 2^(7-E) rounded to 4 significant bits, the next ones what
-// is left, times 16 each: two hold a bfloat16's 8 bits exactly, three a
-// float16's 11 (of a row's small values, to 2^-21 and 2^-25 of its largest).
-// The matrix cores multiply the pieces' products by the pieces' scales and the
-// key groups' own, so that every product is exact.
-struct RowScale {
+// A query is multiplied in 8-bit floats (e4m3) against the 4-bit keys, in groups of
+// the same 32 channels that share a scale in a key.  With E = floor(log2 max|q|) of a
+// group, the first piece is q * 2^(7-E) rounded to 4 significant bits, the next ones
+// what is left, times 16 each: two hold a bfloat16's 8 bits exactly, three a float16's
+// 11, of values down to 2^-13 of the group's largest, and smaller ones to 2^-21 and
+// 2^-25 of it.  The matrix cores multiply the pieces' products by the pieces' scales and
+// the key groups' own, so that products are exact but for that.
+struct GroupScale {
     float up;         // 2^(7-E)
-    uint32_t byte;    // biased exponent of 2^(E-7); 255 (NaN) for a row that is not finite
+    uint32_t bytes;   // byte p: biased exponent of piece p, 2^(E-7-4p); 255 (NaN) for a
+                      // group that is not finite
 };
 
-__device__ __forceinline__ RowScale row_scale(float top) {
+template <typename E>
+__device__ __forceinline__ GroupScale group_scale(float top) {
     const uint32_t t = bits_as<uint32_t>(top);
-    RowScale r;
-    // rows below 2^-100 are scaled as if they reached it
-    const int e = max((int)(t >> 23), 27);   // biased E
+    GroupScale r;
+    // the smallest for which every piece's scale has an exponent; of bfloat16's groups
+    // below it (2^-115), whose values are multiples of 2^-133, two pieces hold all bits
+    constexpr int kLeast = 8 + 4 * (E::kPieces - 1);
+    const int e = max((int)(t >> 23), kLeast);   // biased E
     r.up = bits_as<float>((uint32_t)(254 + 7 - e) << 23);
-    r.byte = t >= 0x7F800000u ? 255u : (uint32_t)(e - 7);
+    r.bytes = 0;
+#pragma unroll
+    for (int p = 0; p < E::kPieces; ++p) r.bytes |= (uint32_t)(e - 7 - 4 * p) << (8 * p);
+    if (t >= 0x7F800000u) r.bytes = ~0u;
     return r;
+}
+
+// The largest absolute value of those whose bits (without signs) `bits` is the largest
+// of: bits are in the order of the values, infinities and NaN last.
+template <typename E>
+__device__ __forceinline__ float top_of(uint32_t bits) {
+    const float top = (float)bits_as<typename E::T>((uint16_t)bits);
+    return top < __builtin_inff() ? top : __builtin_inff();
+}
+
+// x of the lanes l and l^32: [0] is that of the one below 32.
+__device__ __forceinline__ f32x2 both_halves(float x) {
+    const auto a =
+        __builtin_amdgcn_permlane32_swap(bits_as<uint32_t>(x), bits_as<uint32_t>(x), false, false);
+    return f32x2{bits_as<float>((uint32_t)a[0]), bits_as<float>((uint32_t)a[1])};
 }
 
 // Four values -> four e4m3 bytes, and what the rounding left of them, times 16.

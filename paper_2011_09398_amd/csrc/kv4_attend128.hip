@@ -98,17 +98,15 @@ template <typename E, int D>
 struct Queries {
     static constexpr int kChunks = D / 64;
     i32x8 piece[E::kPieces][kChunks];
-    uint32_t scale[E::kPieces];
+    uint32_t scale[kChunks];   // byte p: the scale of piece p of group 2c + h
 };
 
 template <typename E, int D>
 __device__ __forceinline__ void load_queries(Queries<E, D> &q, const typename E::T *row, bool valid,
                                              int h) {
-    constexpr int kChunks = D / 64;
-    u32x4 w[kChunks][2][2];
-    uint32_t bits = 0;
+    u32x4 w[D / 64][2][2];
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c)
+    for (int c = 0; c < D / 64; ++c)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             w[c][k][0] = w[c][k][1] = u32x4{0, 0, 0, 0};
@@ -117,35 +115,47 @@ __device__ __forceinline__ void load_queries(Queries<E, D> &q, const typename E:
                     reinterpret_cast<const u32x4 *>(row + 64 * c + 32 * k + 16 * h);
                 w[c][k][0] = at[0], w[c][k][1] = at[1];
             }
+        }
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+        float tops[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint32_t bits = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t x = w[c][k][i / 4][i % 4];
                 bits = max(bits, max(x & 0x7FFFu, x >> 16 & 0x7FFFu));
             }
-        }
-    float top = (float)bits_as<typename E::T>((uint16_t)bits);
-    if (!(top < __builtin_inff())) top = __builtin_inff();
-    const auto other =
-        __builtin_amdgcn_permlane32_swap(bits_as<uint32_t>(top), bits_as<uint32_t>(top), false, false);
-    top = fmaxf(bits_as<float>((uint32_t)other[0]), bits_as<float>((uint32_t)other[1]));
-    const RowScale s = row_scale(top);
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
+            const f32x2 both = both_halves(top_of<E>(bits));
+            tops[k] = fmaxf(both[0], both[1]);
+            const float up = group_scale<E>(tops[k]).up;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float y[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const auto pair = bits_as<typename E::T2>((uint32_t)w[c][k][i / 2][i % 2 * 2 + j / 2]);
-                    y[j] = (float)pair[j % 2] * s.up;
+                    y[j] = (float)pair[j % 2] * up;
                 }
 #pragma unroll
                 for (int p = 0; p < E::kPieces; ++p) q.piece[p][c][4 * k + i] = (int)next_piece(y);
             }
-#pragma unroll
-    for (int p = 0; p < E::kPieces; ++p) q.scale[p] = s.byte == 255u ? 255u : s.byte - 4u * p;
+        }
+        q.scale[c] = group_scale<E>(h ? tops[1] : tops[0]).bytes;
+    }
+}
+
+// A chunk's products of piece P, and those of the pieces after it.
+template <typename E, int D, int T, int P>
+__device__ __forceinline__ f32x16 multiply(const i32x8 &k, uint32_t scale, const Queries<E, D> &q,
+                                           int c, f32x16 s) {
+    if constexpr (P < E::kPieces) {
+        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q.piece[P][c], s, 4, 0, 2 * T,
+                                                            (int)scale, P, (int)q.scale[c]);
+        return multiply<E, D, T, P + 1>(k, scale, q, c, s);
+    }
+    return s;
 }
 
 // Scores of tokens 32T .. 32T + 31 of a page: s[i] of lane (n, h) is row n against
@@ -158,21 +168,15 @@ __device__ __forceinline__ f32x16 scores(const Keys<D> &r, const Queries<E, D> &
 #pragma unroll
     for (int c = 0; c < Keys<D>::kChunks; ++c) {
         const u32x4 k = r.k[T][c];
-        const uint32_t scale = r.scale[c] >> (n / 16 * 8);
-        const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-#pragma unroll
-        for (int p = 0; p < E::kPieces; ++p)
-            s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q.piece[p][c], s, 4, 0, 2 * T,
-                                                                (int)scale, 0, (int)q.scale[p]);
+        s = multiply<E, D, T, 0>(i32x8{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0},
+                                 r.scale[c] >> (n / 16 * 8), q, c, s);
     }
     return s;
 }
 
 __device__ __forceinline__ float across_halves(float x, bool sum) {
-    const auto a =
-        __builtin_amdgcn_permlane32_swap(bits_as<uint32_t>(x), bits_as<uint32_t>(x), false, false);
-    const float u = bits_as<float>((uint32_t)a[0]), v = bits_as<float>((uint32_t)a[1]);
-    return sum ? u + v : fmaxf(u, v);
+    const f32x2 both = both_halves(x);
+    return sum ? both[0] + both[1] : fmaxf(both[0], both[1]);
 }
 
 // Orders what stands since the last scheduling barrier: four LDS reads, then COUNT

@@ -84,7 +84,7 @@ struct Queries {
     // two pieces, in its two halves)
     static constexpr int kSteps = D < 128 ? (E::kPieces + 1) / 2 : E::kPieces;
     i32x8 piece[kSteps][kChunks];
-    uint32_t scale[kSteps];
+    uint32_t scale[kChunks];   // byte st: the scale of the lane's group in product st
 };
 
 // The same channels as they come from memory: on their way while the page
@@ -109,68 +109,80 @@ struct RawQueries {
     }
 };
 
+// Lane (n, g) holds half of channel group g / 2, and of group 2 + g / 2 in its second
+// half, and gives the products the scale of group g: heads of 64 channels, of which
+// a product takes two pieces, that of group g % 2 for piece g / 2.
 template <typename E, int D>
 __device__ __forceinline__ void make_pieces(Queries<E, D> &q, const RawQueries<D> &raw, int g) {
     constexpr int kChunks = Keys<D>::kChunks, kHalves = RawQueries<D>::kHalves;
-    float x[kChunks][kHalves][16];
-    uint32_t bits = 0;   // of the largest absolute value: as whole numbers, in the
-                         // order of the values, infinities and NaN last
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c)
+    for (int c = 0; c < kChunks; ++c) {
+        uint32_t bytes[E::kPieces][kHalves][4];
+        f32x2 tops[kHalves];
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
+        for (int h = 0; h < kHalves; ++h) {
+            float x[16];
+            uint32_t bits = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t w = raw.w[c][h][i / 4][i % 4];
                 bits = max(bits, max(w & 0x7FFFu, w >> 16 & 0x7FFFu));
                 const typename E::T2 pair = bits_as<typename E::T2>(w);
-                x[c][h][2 * i] = (float)pair[0];
-                x[c][h][2 * i + 1] = (float)pair[1];
+                x[2 * i] = (float)pair[0];
+                x[2 * i + 1] = (float)pair[1];
             }
-    float top = (float)bits_as<typename E::T>((uint16_t)bits);
-    if (!(top < __builtin_inff())) top = __builtin_inff();
-    top = across_rows(top, [](float a, float b) { return fmaxf(a, b); });
-    const RowScale s = row_scale(top);
-    uint32_t bytes[E::kPieces][kChunks][kHalves][4];
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h)
+            const uint32_t own = bits_as<uint32_t>(top_of<E>(bits));
+            const auto a = __builtin_amdgcn_permlane16_swap(own, own, false, false);
+            const float top =
+                fmaxf(bits_as<float>((uint32_t)a[0]), bits_as<float>((uint32_t)a[1]));
+            tops[h] = both_halves(top);
+            const float up = group_scale<E>(top).up;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float y[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = x[c][h][4 * i + j] * s.up;
+                for (int j = 0; j < 4; ++j) y[j] = x[4 * i + j] * up;
 #pragma unroll
-                for (int p = 0; p < E::kPieces; ++p) bytes[p][c][h][i] = next_piece(y);
+                for (int p = 0; p < E::kPieces; ++p) bytes[p][h][i] = next_piece(y);
             }
-    // the scale of piece p: 16^-p
-    const auto scale = [&](int p) { return s.byte == 255u ? 255u : s.byte - 4u * p; };
-    if constexpr (D < 128) {
-#pragma unroll
-        for (int st = 0; st < Queries<E, D>::kSteps; ++st) {
-            const int p0 = 2 * st, p1 = 2 * st + 1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                q.piece[st][0][i] = (int)bytes[p0][0][0][i];
-                q.piece[st][0][4 + i] = p1 < E::kPieces ? (int)bytes[p1 < E::kPieces ? p1 : 0][0][0][i] : 0;
-            }
-            // scales go by the product's groups of 32: its second half is piece p1
-            q.scale[st] = g < 2 ? scale(p0) : scale(p1 < E::kPieces ? p1 : p0);
         }
-    } else {
+        if constexpr (D < 128) {
+            const uint32_t scales = group_scale<E>(g % 2 ? tops[0][1] : tops[0][0]).bytes;
+            q.scale[c] = 0;
 #pragma unroll
-        for (int p = 0; p < E::kPieces; ++p) {
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
+            for (int st = 0; st < Queries<E, D>::kSteps; ++st) {
+                const int p0 = 2 * st, p1 = 2 * st + 1 < E::kPieces ? 2 * st + 1 : p0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    q.piece[p][c][i] = (int)bytes[p][c][0][i];
-                    q.piece[p][c][4 + i] = (int)bytes[p][c][kHalves - 1][i];
+                    q.piece[st][c][i] = (int)bytes[p0][0][i];
+                    q.piece[st][c][4 + i] = p1 == p0 ? 0 : (int)bytes[p1][0][i];
                 }
-            q.scale[p] = scale(p);
+                q.scale[c] |= (scales >> (g < 2 ? 8 * p0 : 8 * p1) & 255u) << (8 * st);
+            }
+        } else {
+            const f32x2 top = tops[g < 2 ? 0 : kHalves - 1];
+            q.scale[c] = group_scale<E>(g % 2 ? top[1] : top[0]).bytes;
+#pragma unroll
+            for (int p = 0; p < E::kPieces; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    q.piece[p][c][i] = (int)bytes[p][0][i];
+                    q.piece[p][c][4 + i] = (int)bytes[p][kHalves - 1][i];
+                }
         }
     }
+}
+
+// A chunk's product of step ST, and those of the steps after it.
+template <typename E, int D, int T, int ST>
+__device__ __forceinline__ f32x4 multiply(const i32x8 &k, uint32_t scale, const Queries<E, D> &q,
+                                          int c, f32x4 s) {
+    if constexpr (ST < Queries<E, D>::kSteps) {
+        s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q.piece[ST][c], s, 4, 0, T,
+                                                             (int)scale, ST, (int)q.scale[c]);
+        return multiply<E, D, T, ST + 1>(k, scale, q, c, s);
+    }
+    return s;
 }
 
 // Scores of a page: s[t][i] of lane (n, g) is row n against token 16t + 4g + i.
@@ -180,11 +192,8 @@ __device__ __forceinline__ f32x4 scores(const Keys<D> &r, const Queries<E, D> &q
 #pragma unroll
     for (int c = 0; c < Keys<D>::kChunks; ++c) {
         const u32x4 k = r.k[T][c];
-        const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-#pragma unroll
-        for (int st = 0; st < Queries<E, D>::kSteps; ++st)
-            s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.piece[st][c], s, 4, 0, T,
-                                                                 (int)r.scale[c], 0, (int)q.scale[st]);
+        s = multiply<E, D, T, 0>(i32x8{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0},
+                                 r.scale[c], q, c, s);
     }
     return s;
 }

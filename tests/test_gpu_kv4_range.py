@@ -215,3 +215,67 @@ def test_no_bit_of_a_row_depends_on_the_rows_beside_it(dtype, dim, rows):
             out, lse = attend(b)
             out[1, 2], lse[1, 2] = clean[0][1, 2], clean[1][1, 2]
             assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
+
+
+# ---- queries whose channels are of very different sizes
+
+def spread_keys(seed, n, dim, up):
+    """Keys whose groups of 32 channels have scales 2^up[g], as Batch takes them."""
+    rng = np.random.default_rng(seed)
+    k = rng.standard_normal((n, dim)) * np.exp2(np.repeat(up, 32))
+    return [(0, j, 0, c, "k", k[j, c]) for j in range(n) for c in range(dim)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("step", [16, 20, 24])
+def test_groups_of_channels_far_apart(dtype, dim, rows, step):
+    """Groups of a query 2^-step of each other's size, against keys that are as much
+    larger there: each counts as much as the others."""
+    if dtype == "f16":
+        step -= 6                                      # to the ends of its normal numbers
+    down = -step * (np.arange(dim // 32) % 2)
+    b = Batch(41, [90], [3], 2, 1, dim, dtype, odd=spread_keys(41, 90, dim, -down))
+    q = b.q.double() * torch.from_numpy(np.exp2(np.repeat(down, 32)))
+    b.q = q.to(b.q.dtype)
+    with lce.tuning(kv4_rows=rows):
+        out, lse = attend(b)
+    check(b, out, lse, dim ** -0.5)
+
+
+@pytest.mark.parametrize("dtype,left", [("bf16", 2.0 ** -21), ("f16", 2.0 ** -25)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("down", [12, 16, 20])
+def test_channels_of_one_group_far_apart(dtype, left, dim, rows, down):
+    """One loud channel of each group of a query, of which the keys have nothing: the others
+    are off by at most `left` of it."""
+    quiet = np.arange(dim) % 32 != 7
+    odd = [(0, j, 0, c, "k", 0.0) for j in range(90) for c in range(7, dim, 32)]
+    b = Batch(42, [90], [3], 2, 1, dim, dtype, odd=odd)
+    q = b.q.double().numpy()
+    q[..., quiet] *= 2.0 ** -down
+    q[..., ~quiet] = 1.5
+    b.q = torch.from_numpy(q).to(b.q.dtype)
+    scale = 2.0 ** down * dim ** -0.5
+    with lce.tuning(kv4_rows=rows):
+        out, lse = attend(b, scale=scale)
+    want, want_lse, bound, lse_bound = b.attention(scale)
+    score = scale * 1.5 * left * np.abs(b.k[0][:, 0]).sum(-1).max()
+    out, lse = out.cpu().double().numpy(), lse.cpu().double().numpy()
+    bound += np.expm1(2 * score) * np.abs(b.v[0][:, 0]).max()
+    assert (np.abs(out - want) <= bound).all() and (np.abs(lse - want_lse) <= lse_bound + score).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("down", [100, 114, 118, 126, 131])
+def test_bfloat16_queries_down_to_the_smallest(dim, rows, down):
+    b = Batch(43, [90], [3], 2, 1, dim, "bf16", odd=spread_keys(43, 90, dim, np.full(dim // 32, 100)))
+    b.q = (b.q.double() * 2.0 ** -down).to(b.q.dtype)
+    assert b.q.any()
+    scale = 2.0 ** (down - 100) * dim ** -0.5
+    with lce.tuning(kv4_rows=rows):
+        out, lse = attend(b, scale=scale)
+    check(b, out, lse, scale)
