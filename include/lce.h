@@ -474,7 +474,8 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  * them; what shares a scale with them is not affected.
  * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
  *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
- *         table_width over 2^24, more rows or tiles than a grid holds),
+ *         table_width or a list over 2^24, more rows or tiles than a grid
+ *         holds),
  *         LCE_EALIGN, LCE_EHIP. */
 lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
                              const lce_kv4_query_desc *query, const void *q, const int32_t *table,

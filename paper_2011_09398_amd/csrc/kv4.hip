@@ -70,6 +70,9 @@ lce_status validate_call(const lce_kv4_cache_desc *d, const lce_kv4_query_desc *
     if (q->window < 0 || q->list < 0 || q->max_q < 0 || q->max_len < 0)
         return fail(LCE_EINVAL, "window %d, list %d, max_q %d and max_len %d must be >= 0",
                     q->window, q->list, q->max_q, q->max_len);
+    // kernels count entries, and up to a workgroup's past the last, in 32 bits
+    if (q->list > 1 << 24)
+        return fail(LCE_EUNSUPPORTED, "list %d: more pages than a table has", q->list);
     return LCE_OK;
 }
 
@@ -150,7 +153,7 @@ Split split_pages(int64_t units, int64_t likely, int64_t pages, double step, dou
         std::max<int64_t>(parts / std::max<int64_t>(units, 1), 1), lce::kv4::kMostSplits);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV4_CHUNK)) {
-        chunk = std::max<int64_t>(t > 0 ? t : 1, (pages + room - 1) / room);
+        chunk = std::max(std::clamp<int64_t>(t, 1, chunk), (pages + room - 1) / room);
     } else {
         const double whole = pages * step / 4;
         // the least of whole / z + fixed + 0.06 z
