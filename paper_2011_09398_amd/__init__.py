@@ -740,6 +740,8 @@ class KV4Cache:
         n = ctypes.c_int64()
         _check(lib().lce_kv4_cache_size(ctypes.byref(self.desc), ctypes.byref(n)))
         if data is None:
+            if torch.device(device).type != "cuda":
+                raise ValueError(f"device must be a GPU, got {device}")
             data = torch.empty((pages, kv_heads, 76 * head_dim), dtype=torch.uint8, device=device)
         self._data, self.pages, self.kv_heads, self.head_dim = data, pages, kv_heads, head_dim
         self._ref = ctypes.byref(self.desc)

@@ -16,3 +16,10 @@ def test_lists_longer_than_a_table_can_be(count):
     assert str(count) in lce.last_error()
     assert call_select(q=q) == lce.LCE_EUNSUPPORTED
     assert str(count) in lce.last_error()
+
+
+def test_a_cache_is_on_a_device():
+    """Its tensors' addresses go to kernels: a buffer on the host is refused, as data is."""
+    for device in ("cpu", "meta"):
+        with pytest.raises(ValueError, match="device"):
+            lce.KV4Cache(2, 64, pages=1, device=device)
