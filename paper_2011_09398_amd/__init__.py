@@ -867,6 +867,13 @@ def kv4_read(cache: KV4Cache, slots, *, dtype=None, out=None):
     return k, v
 
 
+def _int32_refused(**sizes):
+    """Raises for a size that an int32 of the C ABI would hold as another one."""
+    for name, value in sizes.items():
+        if not INT32_MIN <= value <= INT32_MAX:
+            raise ValueError(f"{name} must be an int32, got {value}")
+
+
 def _query_refused(cache, q, table, q_start, lengths):
     """Raises for what attention and selection do not take."""
     import torch
@@ -904,8 +911,12 @@ def _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, 
         fine = False
     if not fine:
         _query_refused(cache, q, table, q_start, lengths)
+    max_q, max_len = max_q or 0, max_len or 0
+    if (tokens | heads | seqs | width | window | count | max_q | max_len) >> 31:
+        _int32_refused(tokens=tokens, heads=heads, sequences=seqs, table=width, window=window,
+                       count=count, max_q=max_q, max_len=max_len)
     return KV4QueryDesc(tokens, heads, seqs, width, code, 1 if causal else 0, window, count,
-                        max_q or 0, max_len or 0, scale, strides[0], strides[1])
+                        max_q, max_len, scale, strides[0], strides[1])
 
 
 def kv4_workspace(cache: KV4Cache, q, table):
@@ -982,6 +993,8 @@ def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_
     """The `count` pages of each token and cache head whose key signs agree best with the
     query signs (lce_kv4_select): int32 [tokens, kv_heads, count], ascending, then -1.
     The first keep_first and the last keep_last pages are always among them."""
+    if (keep_first | keep_last) >> 31:
+        _int32_refused(keep_first=keep_first, keep_last=keep_last)
     d = _kv4_query(cache, q, table, q_start, lengths, causal, window, count, None, max_len, 1.0)
     shape = (q.shape[0], cache.kv_heads, count)
     if out is None:

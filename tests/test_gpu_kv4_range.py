@@ -279,3 +279,24 @@ def test_bfloat16_queries_down_to_the_smallest(dim, rows, down):
     with lce.tuning(kv4_rows=rows):
         out, lse = attend(b, scale=scale)
     check(b, out, lse, scale)
+
+
+# ---- arguments past 32 bits
+
+def test_sizes_that_an_int32_would_hold_as_others():
+    """A window of 2^32 + 5 was one of 5."""
+    b = Batch(46, [200], [2], 4, 2, 64, "bf16")
+    args = b.device(lce)
+    for call, kw in ((lce.kv4_attention, dict(window=2 ** 32 + 5)),
+                     (lce.kv4_attention, dict(window=-2 ** 32)),
+                     (lce.kv4_attention, dict(max_q=2 ** 32 + 1)),
+                     (lce.kv4_attention, dict(max_len=2 ** 31)),
+                     (lce.kv4_select, dict(count=2, keep_first=2 ** 32)),
+                     (lce.kv4_select, dict(count=2, keep_last=2 ** 32 + 1)),
+                     (lce.kv4_select, dict(count=2, window=2 ** 32 + 70)),
+                     (lce.kv4_select, dict(count=2 ** 32 + 2))):
+        with pytest.raises(ValueError, match="int32"):
+            call(*args, **kw)
+    for kw in (dict(window=-1), dict(max_q=-1)):
+        with pytest.raises(lce.LceError):
+            lce.kv4_attention(*args, **kw)
