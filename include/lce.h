@@ -433,13 +433,20 @@ typedef struct {
     int64_t q_token_stride, q_head_stride;   /* elements, multiples of 8               */
 } lce_kv4_query_desc;
 
-/* Bytes of workspace that every lce_kv4_attention and lce_kv4_select call with
- * these tokens, q_heads, seqs and table_width can need (the other fields do not
- * matter).  The workspace is 16-byte aligned device memory whose first
- * LCE_KV4_WORKSPACE_ZERO bytes are zero before its first use; each call leaves
- * them zero.  Calls that may run at the same time need one each.
- * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim). */
+/* Bytes of workspace that lce_kv4_attention, lce_kv4_select, or both calls with
+ * these tokens or fewer, q_heads, seqs and table_width can need (the other
+ * fields do not matter): 128 KiB, and for attention at most 36 MB (heads of 64:
+ * 18, of 256: 69) of partial results, for selection 2 bytes for each token, cache
+ * head and page of the table.  The workspace is 16-byte aligned device memory
+ * whose first LCE_KV4_WORKSPACE_ZERO bytes are zero before its first use; each
+ * call leaves them zero.  Calls that may run at the same time need one each.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim, as
+ *         lce_kv4_attention). */
 #define LCE_KV4_WORKSPACE_ZERO 131072
+lce_status lce_kv4_attention_workspace_size(const lce_kv4_cache_desc *desc,
+                                            const lce_kv4_query_desc *query, int64_t *bytes);
+lce_status lce_kv4_select_workspace_size(const lce_kv4_cache_desc *desc,
+                                         const lce_kv4_query_desc *query, int64_t *bytes);
 lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_query_desc *query,
                                   int64_t *bytes);
 
@@ -467,7 +474,7 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  *   out     [tokens][q_heads][head_dim] of query->type, contiguous (device,
  *           16-byte aligned); rows of no sequence are left as they are
  *   lse     float32 [tokens][q_heads] or NULL
- *   workspace, workspace_bytes: see lce_kv4_workspace_size
+ *   workspace, workspace_bytes: see lce_kv4_attention_workspace_size
  * A query row that holds an infinity or a NaN gives NaN.  With LCE_FLOAT16,
  * cached values of 65536 and more count as 65504, the largest float16 (and
  * -65536 and less as -65504), not as the infinities that lce_kv4_read makes of
@@ -493,7 +500,8 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
  * equal ones.  pages int32 [tokens][kv_heads][list] (device) gets the chosen
  * page numbers in ascending order, then -1.  Pages on which the window leaves
  * nothing, or that the table names outside the cache, are not chosen.
- * The other arguments as for lce_kv4_attention.
+ * The other arguments as for lce_kv4_attention (workspace: see
+ * lce_kv4_select_workspace_size).
  * Errors: as lce_kv4_attention, plus LCE_EINVAL (list < 1, keep < 0) and
  *         LCE_EUNSUPPORTED (q_heads / kv_heads * head_dim > 65280). */
 lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,

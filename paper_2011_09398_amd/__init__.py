@@ -47,6 +47,7 @@ EXPORTS = ("lce_packed_words", "lce_bconv2d_out_shape", "lce_bitpack", "lce_bcon
            "lce_dequantize", "lce_bconv2d_mfma_weights_size", "lce_bconv2d_mfma_weights",
            "lce_bconv2d_mfma", "lce_quantize_bconv2d", "lce_quantize_bconv2d_mfma",
            "lce_kv4_cache_size", "lce_kv4_append", "lce_kv4_read", "lce_kv4_workspace_size",
+           "lce_kv4_attention_workspace_size", "lce_kv4_select_workspace_size",
            "lce_kv4_attention", "lce_kv4_select",
            "lce_set_tuning", "lce_get_tuning",
            "lce_last_error", "lce_last_schedule")
@@ -143,8 +144,10 @@ def lib() -> ctypes.CDLL:
         L.lce_kv4_append.restype = ctypes.c_int
         L.lce_kv4_read.argtypes = [cd, vp, vp, i64, i32, vp, vp, vp]
         L.lce_kv4_read.restype = ctypes.c_int
-        L.lce_kv4_workspace_size.argtypes = [cd, qd, ctypes.POINTER(i64)]
-        L.lce_kv4_workspace_size.restype = ctypes.c_int
+        for size in (L.lce_kv4_workspace_size, L.lce_kv4_attention_workspace_size,
+                     L.lce_kv4_select_workspace_size):
+            size.argtypes = [cd, qd, ctypes.POINTER(i64)]
+            size.restype = ctypes.c_int
         L.lce_kv4_attention.argtypes = [cd, vp, qd, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
         L.lce_kv4_attention.restype = ctypes.c_int
         L.lce_kv4_select.argtypes = [cd, vp, qd, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp]
@@ -919,24 +922,34 @@ def _kv4_query(cache, q, table, q_start, lengths, causal, window, count, max_q, 
                         max_q, max_len, scale, strides[0], strides[1])
 
 
-def kv4_workspace(cache: KV4Cache, q, table):
+def kv4_workspace(cache: KV4Cache, q, table, *, only: Optional[str] = None):
     """Workspace (uint8, zeroed) for kv4_attention and kv4_select calls with q's and
-    table's shapes, or with fewer tokens.  Calls that may overlap need one each."""
+    table's shapes, or with fewer tokens; only="attention" or "select": for calls of that
+    kind.  At most 69 MB for attention; for selection 2 bytes for each token, cache head
+    and page of the table.  Calls that may overlap need one each."""
     import torch
     _require_cache(cache)
     _require_heads(q, cache, "q")
+    _require_like(table, torch.int32, cache.data.device, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences, pages]")
+    if only not in (None, "attention", "select"):
+        raise ValueError(f"only must be 'attention', 'select' or None, got {only!r}")
+    _int32_refused(tokens=q.shape[0], heads=q.shape[1], sequences=table.shape[0],
+                   table=table.shape[1])
     d = KV4QueryDesc(q.shape[0], q.shape[1], table.shape[0], table.shape[1])
     n = ctypes.c_int64()
-    _check(lib().lce_kv4_workspace_size(cache._ref, ctypes.byref(d), ctypes.byref(n)))
+    size = getattr(lib(), f"lce_kv4_{only}_workspace_size" if only else "lce_kv4_workspace_size")
+    _check(size(cache._ref, ctypes.byref(d), ctypes.byref(n)))
     ws = torch.empty(n.value, dtype=torch.uint8, device=cache.data.device)
     ws[:KV4_WORKSPACE_ZERO].zero_()
     return ws
 
 
-def _workspace(workspace, cache, q, table):
+def _workspace(workspace, cache, q, table, only):
     import torch
     if workspace is None:
-        return kv4_workspace(cache, q, table)
+        return kv4_workspace(cache, q, table, only=only)
     _require_like(workspace, torch.uint8, cache.data.device, "workspace")
     return workspace
 
@@ -966,7 +979,7 @@ def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optiona
     lse = (cache._empty(q.shape[:2], dtype=cache._float32, device=cache._device) if return_lse
            else None)
     if workspace is None or not cache._holds(workspace, cache._uint8):
-        workspace = _workspace(workspace, cache, q, table)
+        workspace = _workspace(workspace, cache, q, table, "attention")
     st = lib().lce_kv4_attention(
         cache._ref, cache._data.data_ptr(), ctypes.byref(d), q.data_ptr(), table.data_ptr(),
         q_start.data_ptr(), lengths.data_ptr(), None if pages is None else pages.data_ptr(),
@@ -1004,7 +1017,7 @@ def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_
         if out.shape != shape:
             raise ValueError(f"out must be {list(shape)}, got {list(out.shape)}")
     if workspace is None or not cache._holds(workspace, cache._uint8):
-        workspace = _workspace(workspace, cache, q, table)
+        workspace = _workspace(workspace, cache, q, table, "select")
     st = lib().lce_kv4_select(
         cache._ref, cache._data.data_ptr(), ctypes.byref(d), q.data_ptr(), table.data_ptr(),
         q_start.data_ptr(), lengths.data_ptr(), keep_first, keep_last, out.data_ptr(),

@@ -134,6 +134,34 @@ int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
     return most >= 256 && !large && all >= 32 * 1024 ? 32 : 16;
 }
 
+// Most states of one tile, of `units` tiles with room for `parts` states.
+int64_t most_splits(int64_t units, int64_t parts) {
+    return std::min<int64_t>(std::max<int64_t>(parts / std::max<int64_t>(units, 1), 1),
+                             lce::kv4::kMostSplits);
+}
+
+// What states of attention take: with each height of a tile, up to a table's pages of
+// them for each (a list splits no further), or as many as there is room for.  More
+// tokens never take less, so that a workspace serves calls with fewer, too.
+int64_t state_bytes(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
+    const int64_t splits = std::min<int64_t>(q.table_width, lce::kv4::kMostSplits);
+    if (splits < 2) return 0;
+    int64_t most = 0;
+    for (const int rows : {16, 32, 128}) {
+        if (rows > 16 && d.head_dim > 128) break;
+        int64_t units = tiles(d, q, rows, false);
+        if (rows == 16) units = std::max(units, tiles(d, q, rows, true));
+        if (q.tokens == 0) units = 0;
+        most = std::max(most, std::min(kMostParts * 16 / rows, units * d.kv_heads * splits) * rows);
+    }
+    return most * (d.head_dim + 4) * 4;
+}
+
+// What ranks of selection take.
+int64_t rank_bytes(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
+    return (int64_t)q.tokens * d.kv_heads * q.table_width * 2;
+}
+
 struct Split {
     int chunk;    // pages per workgroup
     int splits;   // workgroups that share a unit, at most
@@ -149,8 +177,7 @@ struct Split {
 Split split_pages(int64_t units, int64_t likely, int64_t pages, double step, double fixed,
                   int64_t most, int64_t parts, int64_t each) {
     const int64_t some = std::max<int64_t>(likely, 1);
-    const int64_t room = std::min<int64_t>(
-        std::max<int64_t>(parts / std::max<int64_t>(units, 1), 1), lce::kv4::kMostSplits);
+    const int64_t room = most_splits(units, parts);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV4_CHUNK)) {
         chunk = std::max(std::clamp<int64_t>(t, 1, chunk), (pages + room - 1) / room);
@@ -232,17 +259,28 @@ lce_status lce_kv4_read(const lce_kv4_cache_desc *desc, const void *cache, const
     return check_launch("lce_kv4_read launch");
 }
 
+lce_status lce_kv4_attention_workspace_size(const lce_kv4_cache_desc *desc,
+                                            const lce_kv4_query_desc *query, int64_t *bytes) {
+    if (!bytes) return fail(LCE_EINVAL, "bytes output pointer is NULL");
+    if (const lce_status st = validate_query(desc, query)) return st;
+    *bytes = LCE_KV4_WORKSPACE_ZERO + state_bytes(*desc, *query);
+    return ok();
+}
+
+lce_status lce_kv4_select_workspace_size(const lce_kv4_cache_desc *desc,
+                                         const lce_kv4_query_desc *query, int64_t *bytes) {
+    if (!bytes) return fail(LCE_EINVAL, "bytes output pointer is NULL");
+    if (const lce_status st = validate_query(desc, query)) return st;
+    *bytes = LCE_KV4_WORKSPACE_ZERO + rank_bytes(*desc, *query);
+    return ok();
+}
+
 lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_query_desc *query,
                                   int64_t *bytes) {
     if (!bytes) return fail(LCE_EINVAL, "bytes output pointer is NULL");
     if (const lce_status st = validate_query(desc, query)) return st;
-    const int64_t heads = desc->kv_heads, width = query->table_width;
-    const int64_t units = std::max(tiles(*desc, *query, 16, false), tiles(*desc, *query, 16, true)) *
-                          heads;
-    // a list may be longer than the table, so its splits are bounded by the room
-    const int64_t parts = kMostParts * 16 * (desc->head_dim + 4) * 4;
-    const int64_t ranks = query->tokens * heads * width * 2;
-    *bytes = LCE_KV4_WORKSPACE_ZERO + std::max(units ? parts : 0, ranks);
+    *bytes = LCE_KV4_WORKSPACE_ZERO +
+             std::max(state_bytes(*desc, *query), rank_bytes(*desc, *query));
     return ok();
 }
 
@@ -267,7 +305,7 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     if (query->q_token_stride % 8 || query->q_head_stride % 8)
         return fail(LCE_EALIGN, "q strides must be multiples of 8 elements");
     int64_t need = 0;
-    if (const lce_status st = lce_kv4_workspace_size(desc, query, &need)) return st;
+    if (const lce_status st = lce_kv4_attention_workspace_size(desc, query, &need)) return st;
     if (workspace_bytes < need)
         return fail(LCE_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
                     (long long)need);
@@ -356,7 +394,7 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
     if (query->q_token_stride % 8 || query->q_head_stride % 8)
         return fail(LCE_EALIGN, "q strides must be multiples of 8 elements");
     int64_t need = 0;
-    if (const lce_status st = lce_kv4_workspace_size(desc, query, &need)) return st;
+    if (const lce_status st = lce_kv4_select_workspace_size(desc, query, &need)) return st;
     if (workspace_bytes < need)
         return fail(LCE_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
                     (long long)need);

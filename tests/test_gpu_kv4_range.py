@@ -300,3 +300,36 @@ def test_sizes_that_an_int32_would_hold_as_others():
     for kw in (dict(window=-1), dict(max_q=-1)):
         with pytest.raises(lce.LceError):
             lce.kv4_attention(*args, **kw)
+
+
+# ---- workspaces of the size that a call asks for
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [0, 16, 32, 128])
+@pytest.mark.parametrize("lengths,queries,width", [
+    ([1], [1], None), ([700], [1], None), ([700, 64, 1], [300, 5, 1], None),
+    ([200] * 20, [3] * 20, 9), ([100, 30], [2, 1], 3000)])
+def test_calls_stay_inside_the_workspace_they_ask_for(dim, rows, lengths, queries, width):
+    b = Batch(47, lengths, queries, 4, 2, dim, "bf16", width=width)
+    args = b.device(lce)
+    pages = np.full((b.tokens, 2, 3), -1, np.int32)
+    pages[:, :, 0] = 0
+    guard = 1 << 16
+    with lce.tuning(kv4_rows=rows, kv4_chunk=1):
+        for only in ("attention", "select"):
+            n = lce.kv4_workspace(*args[:3], only=only).numel()
+            ws = torch.full((n + guard,), 0xA5, dtype=torch.uint8, device="cuda")
+            ws[:lce.KV4_WORKSPACE_ZERO] = 0
+            if only == "select":
+                got = lce.kv4_select(*args, 2, workspace=ws[:n])
+                assert np.array_equal(got.cpu().numpy(), b.select(2))
+            else:
+                out, lse = lce.kv4_attention(*args, workspace=ws[:n], return_lse=True)
+                check(b, out, lse, dim ** -0.5)
+                out, lse = lce.kv4_attention(*args, workspace=ws[:n], return_lse=True,
+                                             pages=torch.from_numpy(pages).cuda())
+                check(b, out, lse, dim ** -0.5, pages=pages)
+            assert (ws[n:] == 0xA5).all() and not ws[:lce.KV4_WORKSPACE_ZERO].any()
+            with pytest.raises(lce.LceError):
+                (lce.kv4_select(*args, 2, workspace=ws[:n - 1]) if only == "select"
+                 else lce.kv4_attention(*args, workspace=ws[:n - 1]))
