@@ -562,10 +562,12 @@ int32_t lce_get_tuning(int32_t key);
 /* Message describing the last error on the calling thread ("" if none). */
 const char *lce_last_error(void);
 
-/* What the calling thread's last convolution call that got as far as a launch
- * ran, for tests and tuning: "xor", "xor-generic", "xor-quantize",
- * "filter-stationary", "k-split", "pixel-split", "streaming" or
- * "streaming-stored" (lce_bconv2d on the matrix cores); "" before any. */
+/* What the calling thread's last convolution or lce_kv4_attention call that got
+ * as far as a launch ran, for tests and tuning: "xor", "xor-generic",
+ * "xor-quantize", "filter-stationary", "k-split", "pixel-split", "streaming" or
+ * "streaming-stored" (lce_bconv2d on the matrix cores); "kv4-16", "kv4-32" or
+ * "kv4-128" by the rows of a tile, "kv4-list", each with "-split" behind it where
+ * a tile's pages may be divided; "" before any. */
 const char *lce_last_schedule(void);
 
 #ifdef __cplusplus

@@ -169,7 +169,7 @@ def last_error() -> str:
 
 
 def last_schedule() -> str:
-    """The schedule of this thread's last convolution (lce_last_schedule)."""
+    """The schedule of this thread's last convolution or attention (lce_last_schedule)."""
     return lib().lce_last_schedule().decode()
 
 

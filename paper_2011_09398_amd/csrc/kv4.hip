@@ -365,6 +365,10 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     if (units > kMostGroups)
         return fail(LCE_EUNSUPPORTED, "%lld tiles: too many for one call", (long long)units);
     const dim3 grid((unsigned)units, (unsigned)s.splits);
+    static const char *const kNames[2][4] = {
+        {"kv4-list", "kv4-16", "kv4-32", "kv4-128"},
+        {"kv4-list-split", "kv4-16-split", "kv4-32-split", "kv4-128-split"}};
+    lce::g_last_schedule = kNames[s.splits > 1][list ? 0 : rows == 16 ? 1 : rows == 32 ? 2 : 3];
     if (rows == 128)
         lce::kv4::launch_attend128(p, query->type, desc->head_dim, grid, stream);
     else

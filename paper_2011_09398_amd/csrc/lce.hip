@@ -95,11 +95,10 @@ __global__ __launch_bounds__(256) void mfma_expand_weights_kernel(const uint32_t
 
 namespace {
 
-thread_local const char *g_last_schedule = "";   // of the last convolution launched
-
 using lce::aligned;
 using lce::check_launch;
 using lce::fail;
+using lce::g_last_schedule;
 using lce::ok;
 using lce::tuning;
 

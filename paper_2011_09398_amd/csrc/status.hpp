@@ -38,6 +38,9 @@ inline lce_status check_launch(const char *what) {
     return ok();
 }
 
+// What the calling thread's last convolution or attention launched (lce_last_schedule).
+inline thread_local const char *g_last_schedule = "";
+
 inline bool aligned(const void *p, uintptr_t a) {
     return (reinterpret_cast<uintptr_t>(p) % a) == 0;
 }
