@@ -346,14 +346,26 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
                           (0.5 + 1.3 * size) * (several ? 2.5 : 1.0),
                           list ? slots / 2 : query->window ? slots : several ? 512 : 7 * slots / 4,
                           kMostParts * 16 / rows, 4);
-    // Loads past the caches where no other tile reads the same pages and the whole keeps
-    // the memory busy: 64 sequences of up to 8192 tokens, 64 heads of 128 on 8 (238 MB),
-    // 59.5 -> 52.6 us; 512 lists of 64 pages (143 MB) 39.5 -> 36.1; but where latency
-    // counts (32 sequences of up to 53109, 16 heads on one, 76 MB: 44 -> 53) or lines are
-    // read in two halves (other head sizes) they are slower.  The bounds are of what the
-    // call could read, which for sequences is a few times what it does.
-    const bool once = each <= 16 &&
-                      68.0 * desc->head_dim * most * units >= (list ? 256 << 20 : 768 << 20);
+    // Loads past the caches where no other tile reads the same pages, heads have 128
+    // channels (of others lines are read in two halves) and the whole is long enough.  The
+    // bounds are of what the call could read, all sequences as long as the longest: of
+    // those below, they read half of it or less.  Measured in graphs (us, through the
+    // caches / past them; one token each of n sequences of up to ..., or n lists):
+    //   could read  read, MB
+    //      143         72   16 of 8192, 64 heads on 8       21.9 / 23.9
+    //      214        106   24 of 8192, 64 on 8             31.1 / 31.2
+    //      231        106   32 of 53109, 16 on 1            46.4 / 45.7
+    //      250        118   28 of 8192, 64 on 8             32.6 / 31.6
+    //      285        132   32 of 8192, 64 on 8             36.4 / 34.0
+    //      285        100   128 of 2000, 64 on 8            30.4 / 30.6
+    //      349        175   16 of 20000, 32 on 8            52.6 / 49.4
+    //      570        238   64 of 8192, 64 on 8             58.4 / 53.4
+    //       71         61   16 lists of 64 pages            17.1 / 18.4
+    //      107         95   24 lists of 64                  24.2 / 24.6
+    //      134        135   60 lists of 32                  29.5 / 27.2
+    //      214        192   48 lists of 64                  43.7 / 39.0
+    const bool once = each <= 16 && 68.0 * desc->head_dim * most * likely >=
+                                        (list ? 120 << 20 : 240 << 20);
     lce::kv4::AttendParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.named = list ? pages : nullptr;
