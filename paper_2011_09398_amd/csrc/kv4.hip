@@ -422,7 +422,19 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
     // a window hides pages but does not renumber them: all up to the last count
     lce_kv4_query_desc all = *query;
     all.window = 0;
-    const Split s = split_pages(units, units, most_pages(all), 0.5, 2, 2048, kMostParts, 1);
+    // Measured in graphs (us by pages a workgroup, one token of each sequence, heads of 128
+    // if not said otherwise; * is the choice):
+    //                                         8     16     32     64    128    all
+    //   1 of 20001, 32 heads on 8            8.6*   8.7    8.9   10.0   12.5   19.1
+    //   1 of 100000, 32 on 8                15.1*  15.1   14.5   15.0   17.4   33.3
+    //   8 of up to 8192, 32 on 8             8.1*   8.2    8.2    9.4   10.8   10.8
+    //   32 of up to 2048, 32 on 8            7.2    7.3    6.2*   6.2    6.2    6.2
+    //   60 of up to 3000, 16 on 1 of 256     8.9*   8.9    9.8    9.9    9.8   10.0
+    //   64 of up to 8192, 64 on 8           17.5   17.6   15.5*  15.4   15.4   15.4
+    //   4 of up to 65536, 32 on 2           12.9*  12.7   12.5   14.3   17.2   35.7
+    //   32 of up to 32768, 64 on 8          22.6   22.6   22.6   23.5*  23.8   30.7
+    //   128 of up to 16384, 64 on 8         31.2   31.3   31.4   31.3   33.7*  33.0
+    const Split s = split_pages(units, units, most_pages(all), 0.5, 3.5, 2048, kMostParts, 1);
     lce::kv4::SelectParams p;
     fill_query(p, *desc, cache, *query, q, table, q_start, lengths, s, workspace);
     p.keep_first = keep_first, p.keep_last = keep_last;
