@@ -407,8 +407,8 @@ lce_status lce_kv4_append(const lce_kv4_cache_desc *desc, void *cache, int32_t t
 /* Read tokens back: k and v [tokens][kv_heads][head_dim] of `type`, contiguous
  * (device, 16-byte aligned), get the values that the cache holds for `slots`,
  * zeros for a slot outside the cache.  float32 and bfloat16 hold every value
- * exactly; float16 rounds to nearest those below 2^-24 and has infinities for
- * those of 65536 and more.
+ * exactly; float16 rounds those below 2^-23 to the nearest multiple of 2^-24 and
+ * has infinities for those of 65536 and more.
  * Errors: as lce_kv4_append. */
 lce_status lce_kv4_read(const lce_kv4_cache_desc *desc, const void *cache, const int64_t *slots,
                         int64_t tokens, int32_t type, void *k, void *v, hipStream_t stream);
@@ -478,7 +478,8 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  * A query row that holds an infinity or a NaN gives NaN.  With LCE_FLOAT16,
  * cached values of 65536 and more count as 65504, the largest float16 (and
  * -65536 and less as -65504), not as the infinities that lce_kv4_read makes of
- * them; what shares a scale with them is not affected.
+ * them; what shares a scale with them is not affected.  Those below 2^-23 count
+ * as the nearest multiple of 2^-24.
  * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
  *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
  *         table_width or a list over 2^24, more rows or tiles than a grid

@@ -993,6 +993,7 @@ def kv4_attention(cache: KV4Cache, q, table, q_start, lengths, *, scale: Optiona
 def _list_length(cache, q, pages):
     import torch
     _require_cache(cache)
+    _require_heads(q, cache, "q")
     _require_like(pages, torch.int32, cache.data.device, "pages")
     if pages.dim() != 3 or pages.shape[:2] != (q.shape[0], cache.kv_heads) or not pages.shape[2]:
         raise ValueError(f"pages must be [{q.shape[0]}, {cache.kv_heads}, n], got "

@@ -333,3 +333,17 @@ def test_calls_stay_inside_the_workspace_they_ask_for(dim, rows, lengths, querie
             with pytest.raises(lce.LceError):
                 (lce.kv4_select(*args, 2, workspace=ws[:n - 1]) if only == "select"
                  else lce.kv4_attention(*args, workspace=ws[:n - 1]))
+
+
+def test_a_list_does_not_hide_what_is_wrong_with_q():
+    b = Batch(48, [70], [1], 4, 2, 64, "bf16")
+    cache, q, *rest = b.device(lce)
+    pages = torch.zeros(1, 2, 1, dtype=torch.int32, device="cuda")
+    for bad, error in ((None, TypeError), ([0], TypeError), (q.cpu(), ValueError), (q[0], ValueError)):
+        with pytest.raises(error, match="q must"):
+            lce.kv4_attention(cache, bad, *rest, pages=pages)
+    for table, error in ((None, TypeError), (rest[0].long(), TypeError), (rest[0][0], ValueError)):
+        with pytest.raises(error, match="table must"):
+            lce.kv4_workspace(cache, q, table)
+    with pytest.raises(ValueError, match="only must"):
+        lce.kv4_workspace(cache, q, rest[0], only="read")
