@@ -107,21 +107,21 @@ int64_t query_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
 // run at a time (1024 of 32, 512 of 128) leave CUs without work; where no sequence is
 // long, half as many tiles of 128 do.  Heads of 256 channels, and 32 rows of 128 in
 // float16 (three pieces of a query, and more registers than there are), stay at 16.
-// Measured (us, tiles of 16 / 32 / 128, 32 heads on 8, 4000 tokens before the new ones
-// if not said otherwise):
-//                                        bfloat16, 128     float16, 64    float16, 128
-//   16 sequences, 256 rows each           44 / 43 / 92     32 / 32 / 68    46 / - / 106
-//   one sequence, 1024 new tokens        114 / 95 / 106    94 / 77 / 85   117 / - / 121
-//   one sequence, 2048                   231 / 187 / 167  174 / 142 / 117 245 / - / 195
-//   one sequence, 4096                   524 / 426 / 359  382 / 319 / 254 567 / - / 423
-//   four sequences, up to 512 each        91 / 81 / 101    68 / 62 / 75    97 / - / 117
-//   four sequences, up to 1024           174 / 146 / 134  128 / 110 / 96  185 / - / 154
-//   four sequences, up to 2048           336 / 282 / 228  245 / 214 / 161 362 / - / 267
-//   16 sequences, up to 128 on 896        38 / 40 / 34     30 / 30 / 25    40 / - / 38
-//   16, up to 64 on 960, 64 heads         38 / 40 / 35     30 / 31 / 25    41 / - / 39
-//   one prompt of 1024                    30 / 29 / 30     23 / 22 / 22    31 / - / 32
-//   two, up to 359 on 5025, 8 on 2        24 / 30 / 53     21 / 23 / 33    25 / - / 54
-//   four prompts of up to 1943, 2 heads   14 / 18 / 42     12 / 15 / 27    15 / - / 44
+// Measured in graphs over three caches (us, tiles of 16 / 32 / 128; 32 heads on 8 if not
+// said otherwise):
+//                                           bfloat16, 128     float16, 64   float16, 128
+//   16 of 4064 tokens, 64 of them new        113 / 93 / 109   86 / 72 / 81  120 / - / 123
+//   one of 5024, 1024 new                    118 / 98 / 118   91 / 81 / 87  131 / - / 132
+//   one of 6048, 2048 new                   241 / 204 / 173 187 / 160 / 126 270 / - / 193
+//   one of 8096, 4096 new                   515 / 425 / 362 393 / 334 / 258 565 / - / 404
+//   four of up to 4512, up to 512 new         97 / 88 / 108   78 / 71 / 82  107 / - / 119
+//   four of up to 5024, up to 1024 new      191 / 162 / 143 146 / 132 / 108 209 / - / 163
+//   four of up to 6048, up to 2048 new      344 / 305 / 238 271 / 240 / 171 378 / - / 264
+//   16 of up to 1024, up to 128 new           42 / 44 / 36    34 / 34 / 27   46 / - / 40
+//   16 of up to 1024, up to 64, 64 heads      43 / 46 / 37    35 / 36 / 27   47 / - / 42
+//   one prompt of 1024                        33 / 33 / 32    26 / 25 / 24   36 / - / 34
+//   two of up to 5025, up to 359, 8 on 2      26 / 29 / 64    20 / 22 / 38   28 / - / 66
+//   four prompts of up to 1943, 2 on 1        15 / 20 / 51    13 / 17 / 31   16 / - / 53
 int tile_rows(const lce_kv4_cache_desc &d, const lce_kv4_query_desc &q) {
     if (d.head_dim > 128) return 16;
     const bool large = d.head_dim == 128 && q.type == LCE_FLOAT16;
@@ -318,19 +318,21 @@ lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
     // Lists are of one length: half of the workgroups that run at a time, each with more
     // pages to hide latencies behind; windows mostly: all of them.  Sequences are of
     // different lengths, of which the call knows the longest: if they were all as long,
-    // 7/4 of what runs at a time, which is about all of it when they are not.  Where a sequence has several tiles
-    // already, 512, and states of all their rows to store and join.  Measured in graphs
-    // (us, heads of 128, 32 on 8, or lists, if not said otherwise):
-    //   pages a workgroup                  8     12     16     24     32     48     64    all
-    //   1 sequence of 20001              15.2   13.3   13.6   14.4   16.2          23.9   84
-    //   32 of up to 8192                 32.0   30.5   29.3   25.8   27.5          30.0   43.4
-    //   4 of up to 65536                 38.4   36.3   32.3   29.6   29.9          33.9  297
-    //   64 of up to 8192, 64 heads       47.0   46.6   46.5   46.4   45.6   42.9   45.4   50.1
-    //   48 of up to 12000, 64 heads                           52.0   50.3   46.3   47.8   67.8
-    //   128 lists of 64                  21.6   18.9   17.5   17.7   18.2          24.2   24.3
-    //   120 lists of 24, heads of 256    21.5   18.7   20.1   20.2   20.2   20.2   20.2   20.2
-    //   2 of up to 359 on 5025, 8 heads  38.8   31.7   30.3   27.1   27.5          25.0   23.3
-    //   16 of 5 on 4096, 24 on 4 of 64   18.0   15.5   16.7   15.6   17.6          21.8   20.9
+    // 7/4 of what runs at a time, which is about all of it when they are not.  Where a
+    // sequence has several tiles already, 512, and states of all their rows to store and
+    // join.  Measured in graphs over three caches (us; up to so many tokens, new ones,
+    // heads; 128 channels, one new token and 32 heads on 8 if not said otherwise; the last
+    // of 64 channels):
+    //   pages a workgroup        choice     8    12    16    24    32    48    64   all
+    //   1 of 20001                 13.3  15.0  13.3  13.6  14.4  16.1  19.8  23.6  83.0
+    //   32 of up to 8192           33.2  41.0  40.0  38.1  37.3  33.7  35.2  35.8  48.4
+    //   4 of up to 65536           46.9  53.5  52.3  47.1  47.9  41.2  45.9  49.9   308
+    //   64 of 8192, 64 heads       54.1  60.2  59.5  60.6  60.3  59.1  55.7  57.3  55.9
+    //   48 of 12000, 64 heads      62.5  70.3  70.6  70.2  70.2  68.5  69.2  64.4  75.4
+    //   128 lists of 64            17.5  21.5  18.3  17.3  17.4  18.7  22.3  25.1  24.6
+    //   120 lists of 24, of 256    19.3  21.7  19.3  21.0  21.1  21.1  21.2  21.1  21.0
+    //   2 of 5025, 359, 8 on 2     25.1  38.4  31.6  30.9  25.8  26.1  25.1  26.5  24.9
+    //   16 of 4096, 5, 24 on 4     13.2  13.5  12.5  12.7  13.6  15.3  18.3  20.3  20.3
     const int64_t seen = most_pages(*query);
     const int64_t most = list ? std::min<int64_t>(query->list, seen) : seen;
     const int64_t each = query_rows(*desc, *query);

@@ -209,13 +209,13 @@ __device__ __forceinline__ void lds_barrier() {
 // read from LDS by all four.  Heads of 64 and 128 channels: of 256, a wave's state
 // and queries leave no registers for a second wave (0.4 of the rate).
 //
-// Bound by issue: the matrix and the vector pipe are each busy about half of the time,
-// with two waves a SIMD to fill each other's gaps.  Measured, bfloat16, 32 heads on 8
-// of 128 channels, causal: 4 sequences of up to 2048 new tokens on up to 16384, 688 us,
-// 1130 TFLOP/s of visible pairs (a large library product: 1217); of up to 1777 on up to
-// 6000, 187 to 201 us by the card, up to 1084 TFLOP/s.  float16 has three pieces of a
-// query to multiply instead of two: 806 us; heads of 64 the same softmax for half the
-// products: 449 us, 865 TFLOP/s.
+// Bound by issue: of a CU's busy cycles the matrix pipe is at work in 0.51 and the vector
+// pipe in 0.57 (counters of the 6000-token case below), with two waves a SIMD to fill each
+// other's gaps.  Measured, bfloat16, 32 heads on 8 of 128 channels, causal: 4 sequences of
+// up to 2048 new tokens on up to 16384, 681 us, 1142 TFLOP/s of visible pairs (a large
+// library product: 1217); of up to 1777 on up to 6000, 190 to 206 us by the card, up to
+// 1068 TFLOP/s.  float16 has three pieces of a query to multiply instead of two: 776 us;
+// heads of 64 the same softmax for half the products: 462 us, 842 TFLOP/s (float16 484).
 template <typename E, int D>
 __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) {
     __shared__ Page<D> pages[2];

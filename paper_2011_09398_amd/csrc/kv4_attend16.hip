@@ -344,10 +344,12 @@ struct Shared {
 // Bound by memory where a call reads much, by the latencies in a row (launch,
 // lengths, table, a page, the states out, the ticket, the states in) where it does
 // not.  Measured, us: 64 sequences of up to 8192 tokens, 64 heads of 128 on 8, bfloat16
-// (238 MB) 52.3, 4.6 TB/s with the launch; one sequence of 20001, 32 heads on 8
-// (22 MB) 12.0, of which the joining of the splits takes 3; 128 lists of 64 pages
-// (61 MB) 15.9.  Loads of a page's keys and values are 16 bytes a lane, and one page
-// is on its way while another is worked on: 12 waves of a CU hide the rest.
+// (238 MB) 51.2, 4.6 TB/s with the launch; one sequence of 20001, 32 heads on 8
+// (22 MB) 11.9, of which the joining of the splits takes 3; 128 lists of 64 pages
+// (61 MB) 16.1.  Loads of a page's keys and values are 16 bytes a lane, and one page
+// is on its way while another is worked on: 12 waves of a CU hide the rest.  What
+// float16's range costs (values past it, looked for in every page): up to 2 %, in tiles
+// of 32 rows 5 %.
 template <typename E, int D, bool LIST, int C, bool ONCE>
 __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16_kernel(
     AttendParams p) {
