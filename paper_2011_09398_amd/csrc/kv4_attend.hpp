@@ -97,6 +97,18 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
     return bits_as<uint32_t>(v);
 }
 
+// Two results.  They are means of values, which float16 holds; but their weights are
+// rounded, and half a last place past 65504 is an infinity.  (NaN stays.)
+template <typename E>
+__device__ __forceinline__ uint32_t pack_result(float a, float b) {
+    if constexpr (E::kSaturates) {
+        const float most = 65504.0f;
+        a = a > most ? most : a < -most ? -most : a;
+        b = b > most ? most : b < -most ? -most : b;
+    }
+    return pack_pair<E>(a, b);
+}
+
 // A query is multiplied in 8-bit floats (e4m3) against the 4-bit keys, in groups of
 // the same 32 channels that share a scale in a key.  With E = floor(log2 max|q|) of a
 // group, the first piece is q * 2^(7-E) rounded to 4 significant bits, the next ones

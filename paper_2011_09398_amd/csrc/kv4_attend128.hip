@@ -442,8 +442,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
             uint32_t x[D / 32];
 #pragma unroll
             for (int c = 0; c < D / 16; c += 2)
-                x[c / 2] = pack_pair<E>(o[c / 2][u / 4 * 4 + u % 4] * inv,
-                                        o[c / 2][(2 + u / 4) * 4 + u % 4] * inv);
+                x[c / 2] = pack_result<E>(o[c / 2][u / 4 * 4 + u % 4] * inv,
+                                          o[c / 2][(2 + u / 4) * 4 + u % 4] * inv);
             typename E::T *to = out + D / 16 * (8 * (u / 4) + u % 4);
 #pragma unroll
             for (int k = 0; k < D / 32; k += 2)
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
             (int64_t)(seq.start + (row0 + rr) / p.group) * (p.kv_heads * p.group) +
             head * p.group + (row0 + rr) % p.group;
         *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + 4 * quad) =
-            u32x2{pack_pair<E>(v[0] * inv, v[1] * inv), pack_pair<E>(v[2] * inv, v[3] * inv)};
+            u32x2{pack_result<E>(v[0] * inv, v[1] * inv), pack_result<E>(v[2] * inv, v[3] * inv)};
         if (p.lse && quad == 0)
             p.lse[at] = sum == 0.0f ? -__builtin_inff()
                                     : (m + __builtin_log2f(sum)) * 0.69314718055994531f;

@@ -548,7 +548,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         const int64_t at = (int64_t)(seq.start + rr / p.group) * (p.kv_heads * p.group) +
                            head * p.group + rr % p.group;
         *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + c) =
-            u32x2{pack_pair<E>(o[0] * inv, o[1] * inv), pack_pair<E>(o[2] * inv, o[3] * inv)};
+            u32x2{pack_result<E>(o[0] * inv, o[1] * inv),
+                  pack_result<E>(o[2] * inv, o[3] * inv)};
         if (p.lse && quad == 0)
             p.lse[at] = l == 0.0f ? -__builtin_inff()
                                   : (top + __builtin_log2f(l)) * 0.69314718055994531f;

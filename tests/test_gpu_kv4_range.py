@@ -347,3 +347,24 @@ def test_a_list_does_not_hide_what_is_wrong_with_q():
             lce.kv4_workspace(cache, q, table)
     with pytest.raises(ValueError, match="only must"):
         lce.kv4_workspace(cache, q, rest[0], only="read")
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("chunk", [1, 9])
+def test_a_mean_of_the_largest_values_is_finite(dim, rows, chunk):
+    """All values count as 65504 in float16, and so does every mean of them: half a last
+    place more, as weights are rounded, would be an infinity."""
+    n = 300
+    keys, values = torch.zeros(n, dim), torch.full((n, dim), 2.0 ** 17)
+    values[:, 1::2] *= -1
+    keys[256:, 0], keys[1:256, 1] = 1, 1               # page 4, in the wave of page 0
+    q = torch.zeros(1, 24, dim, dtype=torch.float16)
+    q[0, :, 0], q[0, :, 1] = torch.linspace(0.03, 8, 24), -60
+    cache = lce.KV4Cache(1, dim, pages=5)
+    with lce.tuning(kv4_rows=rows, kv4_chunk=chunk):
+        out = lce.kv4_attention(cache, q.cuda(), *fill(cache, keys, values), scale=float(np.log(2)))
+    want = torch.full((dim,), MOST, dtype=torch.float64)
+    want[1::2] *= -1
+    # weights rounded by half a last place, 2^-11, and the result by as much
+    assert ((out[0].cpu().double() - want).abs() <= 2 * 2.0 ** -11 * MOST).all()
