@@ -511,11 +511,218 @@ lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
                           int32_t keep_last, int32_t *pages, void *workspace,
                           int64_t workspace_bytes, hipStream_t stream);
 
+/* ---- 8-bit key/value cache ----------------------------------------------
+ *
+ * The same cache with a byte a channel, for models that lose too much in four bits:
+ * 8-bit floats (e4m3: a sign, four bits of exponent, three of mantissa; multiples of
+ * 2^-9 up to 448) that share one power of two per LCE_KV8_BLOCK = 16 tokens of a head,
+ * one for its keys and one for its values.
+ *
+ * A block's scale is the smallest power of two, of 2^-126 and more, with which no
+ * channel of the tokens that one call appends to it is past 448, or the scale that the
+ * block had, where it holds older tokens and that is larger:
+ *     code = x / scale rounded to the nearest e4m3 value, ties to even;
+ *     the value held is code * scale.
+ * Where a call raises the scale of a block that holds older tokens, their codes are
+ * rounded once more, to the new scale's values (which changes only those below 2^-6 of
+ * it).  A token that holds an infinity or a NaN in its key or its value gets the NaN
+ * code in all channels of its key, and 0 for what is not finite in its value: every row
+ * that attends to it is NaN, and no other row.
+ *
+ * The cache is one device buffer of pages of LCE_KV8_PAGE = 64 tokens, each page
+ * holding a record of 128*D + 128 bytes per head (D = head_dim), with token t of the
+ * page at
+ *     key codes     byte  t*D + c                       (channel c)
+ *     value codes   byte  64*D + (t/4*D + c)*4 + t%4
+ *     key scales    byte  128*D + t/16                  (2^(byte-127))
+ *     value scales  byte  128*D + 4 + t/16
+ * and 120 bytes that nothing uses, so that records begin with a line of memory.  A
+ * sequence is a row of page numbers (its table) and a length; its token j is in slot
+ * table[j/64]*64 + j%64. */
+#define LCE_KV8_PAGE 64
+#define LCE_KV8_BLOCK 16
+
+typedef struct {
+    int32_t pages;       /* pages of the buffer, >= 1                        */
+    int32_t kv_heads;    /* heads of keys and values, >= 1                   */
+    int32_t head_dim;    /* channels of a head: 64, 128 or 256               */
+} lce_kv8_cache_desc;
+
+/* Bytes of the cache buffer of `desc`: pages * kv_heads * 128 * (head_dim + 1).  Its
+ * contents need no initialization: what was never written may be anything as long as
+ * no length covers it.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim). */
+lce_status lce_kv8_cache_size(const lce_kv8_cache_desc *desc, int64_t *bytes);
+
+/* Quantize the last tokens of sequences into the cache: `tokens` rows of keys and
+ * values, those of sequence b at q_start[b] .. q_start[b+1]-1; with n of them, number i
+ * is the sequence's token lengths[b] - n + i (lengths count the new tokens).
+ *   cache  buffer of lce_kv8_cache_size bytes             (device, 16-byte aligned)
+ *   k, v   [tokens][kv_heads][head_dim] of `type`         (device, 16-byte aligned),
+ *          channels contiguous; token and head strides in elements, each a
+ *          multiple of 16 bytes
+ *   table, q_start, lengths   as for lce_kv8_attention
+ * Tokens before a sequence's beginning (n > lengths[b]) and tokens on a page outside
+ * the cache are dropped.  Older tokens of a block are those before its first new one;
+ * what the block holds behind the last new one becomes 0.  No two sequences may append
+ * to one block in a call.  Appending the same tokens again changes nothing.
+ * tokens == 0 is a no-op (pointers may then be NULL).
+ * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0), LCE_EUNSUPPORTED
+ *         (head_dim, kv_heads > 65535, table_width over 2^24, more blocks than a grid
+ *         holds), LCE_EALIGN (pointer or stride), LCE_EHIP. */
+lce_status lce_kv8_append(const lce_kv8_cache_desc *desc, void *cache, int32_t type,
+                          const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                          int32_t tokens, int32_t seqs, int32_t table_width, const int32_t *table,
+                          const int32_t *q_start, const int32_t *lengths, hipStream_t stream);
+
+/* Read tokens back: k and v [tokens][kv_heads][head_dim] of `type`, contiguous
+ * (device, 16-byte aligned), get the values that the cache holds for `slots` (int64
+ * [tokens], device), zeros for a slot outside the cache.  float32 holds every value
+ * exactly, bfloat16 those of 2^-126 and more; float16 rounds those below 2^-20 to the
+ * nearest multiple of 2^-24 and has infinities for those of 65536 and more.
+ * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0 or >= 2^31), LCE_EUNSUPPORTED
+ *         (head_dim, kv_heads > 65535), LCE_EALIGN, LCE_EHIP. */
+lce_status lce_kv8_read(const lce_kv8_cache_desc *desc, const void *cache, const int64_t *slots,
+                        int64_t tokens, int32_t type, void *k, void *v, hipStream_t stream);
+
+/* New tokens that attend over cached sequences (see lce_kv4_query_desc). */
+typedef struct {
+    int32_t tokens;        /* query tokens over all sequences, >= 0                    */
+    int32_t q_heads;       /* a multiple of kv_heads; head hq reads cache head
+                              hq / (q_heads / kv_heads)                                */
+    int32_t seqs;          /* sequences, >= 1                                          */
+    int32_t table_width;   /* page numbers per row of the table, >= 1                  */
+    int32_t type;          /* LCE_FLOAT16 or LCE_BFLOAT16: q and out                   */
+    int32_t causal;        /* 1: position p sees tokens j <= p, and a prefix; 0: all   */
+    int32_t window;        /* > 0: only tokens j > p - window; 0: no such bound        */
+    int32_t max_q;         /* hints for the split of the work, 0 = unknown: the most   */
+    int32_t max_len;       /* new tokens, the longest length.  Wrong ones cost speed.  */
+    float scale;           /* of the scores, finite and > 0                            */
+    float softcap;         /* 0: none, or what scores are capped at, 1e-30 .. 1e30     */
+    int64_t q_token_stride, q_head_stride;   /* elements, multiples of 8               */
+} lce_kv8_query_desc;
+
+/* Bytes of workspace that lce_kv8_attention calls with these tokens or fewer, q_heads,
+ * seqs and table_width can need (the other fields do not matter): 128 KiB, and at most
+ * 36 MB (heads of 64: 18, of 256: 69) of partial results.  The workspace is 16-byte
+ * aligned device memory whose first LCE_KV8_WORKSPACE_ZERO bytes are zero before its
+ * first use; each call leaves them zero.  Calls that may run at the same time need one
+ * each.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim, as
+ *         lce_kv8_attention). */
+#define LCE_KV8_WORKSPACE_ZERO 131072
+lce_status lce_kv8_workspace_size(const lce_kv8_cache_desc *desc, const lce_kv8_query_desc *query,
+                                  int64_t *bytes);
+
+/* Attention of new tokens over the cache: per token (position p) and query head
+ *     s_j = scale * (q . k_j)                        over the visible tokens j,
+ *     s_j = softcap * tanh(s_j / softcap)            with a softcap,
+ *     s_j = s_j - slopes[head] * |p - j|             with slopes,
+ *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)
+ * with k and v as the cache holds them.  Token j is visible where j <= p or j <
+ * prefix[b] (causal) or anywhere in the sequence (not causal), and j > p - window where
+ * there is a window.  Sums, scores, the running maximum and the running sum are
+ * float32; softmax weights are rounded to `type` where they multiply the values
+ * (float16: with a last place of at most 2^-31 of a row's largest weight), and out is
+ * rounded to it once.  With LCE_FLOAT16, keys are multiplied as multiples of 2^-32 times
+ * the largest scale of their page (of half a page with heads of 256), values as
+ * multiples of 2^-32 times the largest scale that a row's sequence has: this rounds only
+ * what is under a scale 2^-22 times as large.
+ * A row that sees nothing is 0 with lse -infinity.
+ *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
+ *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a
+ *           length are not read; tokens on a page outside the cache are hidden
+ *   q_start int32 [seqs+1], not decreasing, lengths int32 [seqs] (device);
+ *           values outside [0, tokens] and [0, 64*table_width] are taken as the
+ *           nearest bound
+ *   slopes  float32 [q_heads] (device) or NULL
+ *   prefix  int32 [seqs] (device) or NULL; values outside [0, length] as the nearest
+ *   out     [tokens][q_heads][head_dim] of query->type, contiguous (device,
+ *           16-byte aligned); rows of no sequence are left as they are
+ *   lse     float32 [tokens][q_heads] or NULL
+ *   workspace, workspace_bytes: see lce_kv8_workspace_size
+ * A query row that holds an infinity or a NaN gives NaN.
+ * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
+ *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
+ *         table_width over 2^24, more rows or tiles than a grid holds),
+ *         LCE_EALIGN, LCE_EHIP. */
+lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
+                             const lce_kv8_query_desc *query, const void *q, const int32_t *table,
+                             const int32_t *q_start, const int32_t *lengths, const float *slopes,
+                             const int32_t *prefix, void *out, float *lse, void *workspace,
+                             int64_t workspace_bytes, hipStream_t stream);
+
+/* ---- Rotary positions -----------------------------------------------------
+ *
+ * Queries and keys turned by their tokens' positions, before keys are appended to a
+ * cache and queries attend to it.  Of a head's first rot_dim channels, pair i is
+ * channels (i, i + rot_dim/2), or (2i, 2i + 1) interleaved; at position p
+ *     (a, b) -> scale * (a cos(p f_i) - b sin(p f_i), b cos(p f_i) + a sin(p f_i)),
+ * the channels behind them stay as they are.  Frequencies f_i are radians a position:
+ * the caller's own, or those of lce_rotary_frequencies. */
+typedef enum {
+    LCE_ROTARY_PLAIN = 0,    /* f_i = base^(-2i / rot_dim)                             */
+    LCE_ROTARY_LINEAR = 1,   /* f_i / factor                                           */
+    LCE_ROTARY_NTK = 2,      /* base times factor^(rot_dim / (rot_dim - 2))            */
+    LCE_ROTARY_YARN = 3      /* by parts: pairs that turn more than 32 times over
+                                `original` positions keep f_i, those that turn less than
+                                once have f_i / factor, a linear mixture by pair number
+                                between; scale = 0.1 ln(factor) + 1                    */
+} lce_rotary_scaling;
+
+/* Frequencies (host, double [rot_dim/2]) of a scaling for contexts `factor` >= 1 times
+ * as long as trained (`original` positions; yarn alone looks at it), and the scale
+ * that goes with them.
+ * Errors: LCE_EINVAL. */
+lce_status lce_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                                  double original, double *freqs, float *scale);
+
+/* The form in which lce_rotary takes frequencies (both host, [count]): turns a position
+ * in multiples of 2^-64, whole turns left out, so that position times frequency is exact
+ * at any position.
+ * Errors: LCE_EINVAL (null pointer, count < 1, a frequency that is not finite). */
+lce_status lce_rotary_turns(const double *freqs, int32_t count, uint64_t *turns);
+
+typedef struct {
+    int32_t tokens;        /* >= 0                                                     */
+    int32_t head_dim;      /* channels of a head, 2 .. 65536                           */
+    int32_t rot_dim;       /* of which so many are turned: even, 2 .. head_dim         */
+    int32_t type;          /* lce_float_type of x and y                                */
+    int32_t interleaved;   /* 0: pairs (i, i + rot_dim/2); 1: (2i, 2i + 1)             */
+    int32_t backward;      /* 1: the other way: x are gradients of the results, y those
+                              of what was turned                                       */
+    float scale;           /* finite                                                   */
+} lce_rotary_desc;
+
+/* Heads of one tensor, read from x and written to y: channels contiguous, strides in
+ * elements.  y may be x (with the same strides); other overlaps are not allowed. */
+typedef struct {
+    int32_t heads;         /* >= 1                                                     */
+    const void *x;
+    void *y;
+    int64_t x_token_stride, x_head_stride, y_token_stride, y_head_stride;
+} lce_rotary_rows;
+
+/* Turn `q`, and `k` unless it is NULL, in one launch.
+ *   turns      uint64 [rot_dim/2] (device): see lce_rotary_turns
+ *   positions  int64 [tokens] (device), any values
+ * Angles are known to 2^-33 turns and products are float32, rounded once to `type`.
+ * rot_dim a multiple of 32 bytes, head_dim of 16, and x, y and strides of 16 bytes take
+ * the widest loads; others work.
+ * tokens == 0 is a no-op (pointers may then be NULL).
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (more than 2^20 heads
+ *         or than a grid holds), LCE_EALIGN (pointers not aligned to their type),
+ *         LCE_EHIP. */
+lce_status lce_rotary(const lce_rotary_desc *desc, const uint64_t *turns, const int64_t *positions,
+                      const lce_rotary_rows *q, const lce_rotary_rows *k, hipStream_t stream);
+
 /* ---- Schedule overrides, for tests and tuning ----------------------------
  *
  * Every convolution picks its work split by itself.  These process-wide
  * overrides force one instead; each choice gives the identical output (of
- * lce_kv4_attention: the same but for the order of its float32 sums), only
+ * lce_kv4_attention and lce_kv8_attention: the same but for the order of their
+ * float32 sums), only
  * the speed changes.  0 (the initial value of every key) restores the
  * library's own choice.  Callers are tests, benchmarks and tuning scripts,
  * not production code.  Values are read once per launch with atomic loads,
@@ -550,7 +757,10 @@ typedef enum {
     LCE_TUNE_KV4_ROWS = 13,       /* lce_kv4_attention without a list: 16, 32 or 128 query
                                      rows per tile, where there is such a kernel (heads
                                      of up to 128; 32 not of 128 in float16)            */
-    LCE_TUNE_COUNT = 14
+    LCE_TUNE_KV8_CHUNK = 14,      /* lce_kv8_attention: pages per workgroup, as above      */
+    LCE_TUNE_KV8_ROWS = 15,       /* lce_kv8_attention: 16, 32 or 128 query rows per tile, where
+                                     there is such a kernel                                */
+    LCE_TUNE_COUNT = 16
 } lce_tuning_key;
 
 /* Set override `key` to `value` (0 = automatic).
@@ -563,12 +773,12 @@ int32_t lce_get_tuning(int32_t key);
 /* Message describing the last error on the calling thread ("" if none). */
 const char *lce_last_error(void);
 
-/* What the calling thread's last convolution or lce_kv4_attention call that got
- * as far as a launch ran, for tests and tuning: "xor", "xor-generic",
+/* What the calling thread's last convolution or lce_kv4_attention or
+ * lce_kv8_attention call that got as far as a launch ran, for tests and tuning: "xor", "xor-generic",
  * "xor-quantize", "filter-stationary", "k-split", "pixel-split", "streaming" or
  * "streaming-stored" (lce_bconv2d on the matrix cores); "kv4-16", "kv4-32" or
- * "kv4-128" by the rows of a tile, "kv4-list", each with "-split" behind it where
- * a tile's pages may be divided; "" before any. */
+ * "kv4-128" by the rows of a tile, "kv4-list", "kv8-16", "kv8-32" or "kv8-128", each
+ * with "-split" behind it where a tile's pages may be divided; "" before any. */
 const char *lce_last_schedule(void);
 
 #ifdef __cplusplus

@@ -22,6 +22,17 @@ A transformer's key/value cache in 4 bits:
     kv4_attention(cache, q, table, q_start, lengths)  attention over cached sequences
     kv4_select(cache, q, table, q_start, lengths, n)  the n pages whose key signs fit best
     kv4_workspace(cache, q, table)    memory that the last two keep between calls
+
+The same in 8 bits, and the positions of what goes into either:
+
+    KV8Cache(kv_heads, head_dim, ..)  the cache's memory: pages of 64 tokens
+    kv8_append(cache, k, v, table, q_start, lengths)  quantize sequences' last tokens
+    kv8_read(cache, slots)            read tokens back as floats
+    kv8_attention(cache, q, table, q_start, lengths)  attention over cached sequences, with
+                                      capped scores, a bias by distance, a prefix
+    kv8_workspace(cache, q, table)    memory that attention keeps between calls
+    Rotary(head_dim, ..)              frequencies of rotary positions
+    rotary(plan, positions, q, k)     queries and keys turned to their positions
 """
 from __future__ import annotations
 
@@ -49,6 +60,8 @@ EXPORTS = ("lce_packed_words", "lce_bconv2d_out_shape", "lce_bitpack", "lce_bcon
            "lce_kv4_cache_size", "lce_kv4_append", "lce_kv4_read", "lce_kv4_workspace_size",
            "lce_kv4_attention_workspace_size", "lce_kv4_select_workspace_size",
            "lce_kv4_attention", "lce_kv4_select",
+           "lce_kv8_cache_size", "lce_kv8_append", "lce_kv8_read", "lce_kv8_workspace_size",
+           "lce_kv8_attention", "lce_rotary_frequencies", "lce_rotary_turns", "lce_rotary",
            "lce_set_tuning", "lce_get_tuning",
            "lce_last_error", "lce_last_schedule")
 
@@ -56,7 +69,7 @@ EXPORTS = ("lce_packed_words", "lce_bconv2d_out_shape", "lce_bitpack", "lce_bcon
 TUNING_KEYS = {"xor_nb": 0, "xor_ks": 1, "mfma_schedule": 2, "mfma_fs_ks": 3, "mfma_fs_s": 4,
                "mfma_fs_wpc": 5, "mfma_fs_pad": 6, "mfma_packed": 7, "mfma_tile_m": 8,
                "mfma_tile_n": 9, "mfma_fs_window": 10, "xor_stream": 11, "kv4_chunk": 12,
-               "kv4_rows": 13}
+               "kv4_rows": 13, "kv8_chunk": 14, "kv8_rows": 15}
 MFMA_SCHEDULES = {"auto": 0, "fs": 1, "ksplit": 2, "pixel": 3, "stream": 4}
 
 
@@ -84,6 +97,33 @@ class KV4QueryDesc(ctypes.Structure):
         "tokens", "q_heads", "seqs", "table_width", "type", "causal", "window", "list", "max_q",
         "max_len")] + [("scale", ctypes.c_float), ("q_token_stride", ctypes.c_int64),
                        ("q_head_stride", ctypes.c_int64)]
+
+
+class KV8CacheDesc(ctypes.Structure):
+    """lce_kv8_cache_desc: three int32 fields, in header order."""
+    _fields_ = KV4CacheDesc._fields_
+
+
+class KV8QueryDesc(ctypes.Structure):
+    """lce_kv8_query_desc: nine int32 fields, two floats and two int64, in header order."""
+    _fields_ = [(name, ctypes.c_int32) for name in (
+        "tokens", "q_heads", "seqs", "table_width", "type", "causal", "window", "max_q",
+        "max_len")] + [("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                       ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    """lce_rotary_desc: six int32 fields and a float, in header order."""
+    _fields_ = [(name, ctypes.c_int32) for name in (
+        "tokens", "head_dim", "rot_dim", "type", "interleaved", "backward")] + [
+            ("scale", ctypes.c_float)]
+
+
+class RotaryRows(ctypes.Structure):
+    """lce_rotary_rows: an int32, two pointers and four int64, in header order."""
+    _fields_ = [("heads", ctypes.c_int32), ("x", ctypes.c_void_p), ("y", ctypes.c_void_p)] + [
+        (name, ctypes.c_int64) for name in ("x_token_stride", "x_head_stride", "y_token_stride",
+                                            "y_head_stride")]
 
 
 class LceError(RuntimeError):
@@ -152,6 +192,21 @@ def lib() -> ctypes.CDLL:
         L.lce_kv4_attention.restype = ctypes.c_int
         L.lce_kv4_select.argtypes = [cd, vp, qd, vp, vp, vp, vp, i32, i32, vp, vp, i64, vp]
         L.lce_kv4_select.restype = ctypes.c_int
+        cd, qd = ctypes.POINTER(KV8CacheDesc), ctypes.POINTER(KV8QueryDesc)
+        L.lce_kv8_cache_size.argtypes = [cd, ctypes.POINTER(i64)]
+        L.lce_kv8_append.argtypes = [cd, vp, i32, vp, i64, i64, vp, i64, i64, i32, i32, i32, vp, vp,
+                                     vp, vp]
+        L.lce_kv8_read.argtypes = [cd, vp, vp, i64, i32, vp, vp, vp]
+        L.lce_kv8_workspace_size.argtypes = [cd, qd, ctypes.POINTER(i64)]
+        L.lce_kv8_attention.argtypes = [cd, vp, qd, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        dp, rows = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(RotaryRows)
+        L.lce_rotary_frequencies.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double,
+                                             ctypes.c_double, dp, ctypes.POINTER(ctypes.c_float)]
+        L.lce_rotary_turns.argtypes = [dp, i32, ctypes.POINTER(ctypes.c_uint64)]
+        L.lce_rotary.argtypes = [ctypes.POINTER(RotaryDesc), vp, vp, rows, rows, vp]
+        for name in ("kv8_cache_size", "kv8_append", "kv8_read", "kv8_workspace_size",
+                     "kv8_attention", "rotary_frequencies", "rotary_turns", "rotary"):
+            getattr(L, "lce_" + name).restype = ctypes.c_int
         L.lce_set_tuning.argtypes = [i32, i32]
         L.lce_set_tuning.restype = ctypes.c_int
         L.lce_get_tuning.argtypes = [i32]
@@ -720,32 +775,28 @@ def _float_type(dtype, name):
     return code
 
 
-class KV4Cache:
-    """A 4-bit key/value cache: pages of 64 tokens in one device buffer.
-
-    KV4Cache(kv_heads, head_dim, pages=n) allocates uint8 [n, kv_heads,
-    76*head_dim] on `device`; data=t takes an existing buffer of that kind.
-    Tokens are addressed by slot = page*64 + place; which pages make up a
-    sequence is the caller's table.  head_dim is 64, 128 or 256."""
+class _PagedCache:
+    """What the caches share: a device buffer of pages, and the quick checks of calls."""
 
     def __init__(self, kv_heads: int, head_dim: int, pages: Optional[int] = None, *, data=None,
                  device="cuda"):
         import torch
         if (pages is None) == (data is None):
             raise ValueError("give either pages or data")
+        record = self._record(head_dim)
         if data is not None:
             _require(data, torch.uint8, "data")
-            if data.dim() != 3 or data.shape[1] != kv_heads or data.shape[2] != 76 * head_dim:
-                raise ValueError(f"data must be [pages, {kv_heads}, {76 * head_dim}], got "
+            if data.dim() != 3 or data.shape[1] != kv_heads or data.shape[2] != record:
+                raise ValueError(f"data must be [pages, {kv_heads}, {record}], got "
                                  f"{list(data.shape)}")
             pages = data.shape[0]
-        self.desc = KV4CacheDesc(pages, kv_heads, head_dim)
+        self.desc = self._Desc(pages, kv_heads, head_dim)
         n = ctypes.c_int64()
-        _check(lib().lce_kv4_cache_size(ctypes.byref(self.desc), ctypes.byref(n)))
+        _check(getattr(lib(), self._size)(ctypes.byref(self.desc), ctypes.byref(n)))
         if data is None:
             if torch.device(device).type != "cuda":
                 raise ValueError(f"device must be a GPU, got {device}")
-            data = torch.empty((pages, kv_heads, 76 * head_dim), dtype=torch.uint8, device=device)
+            data = torch.empty((pages, kv_heads, record), dtype=torch.uint8, device=device)
         self._data, self.pages, self.kv_heads, self.head_dim = data, pages, kv_heads, head_dim
         self._ref = ctypes.byref(self.desc)
         # what every call compares its tensors with
@@ -758,13 +809,56 @@ class KV4Cache:
 
     @property
     def data(self):
-        """The buffer, uint8 [pages, kv_heads, 76*head_dim]."""
+        """The buffer, uint8 [pages, kv_heads, bytes of a record]."""
         return self._data
 
     def _holds(self, t, dtype) -> bool:
         """Whether t is a contiguous `dtype` tensor on the cache's device: the quick
         check; _require_like says what is wrong."""
         return (t.dtype is dtype and t.get_device() == self._index and t.is_contiguous())
+
+
+def _launch(index, fn, *args) -> None:
+    """Calls the library with device `index` current: a default stream is its device's by
+    that alone."""
+    import torch
+    if torch.cuda.current_device() == index:
+        st = fn(*args)
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args)
+    if st != LCE_OK:
+        raise LceError(st, last_error())
+
+
+class KV4Cache(_PagedCache):
+    """A 4-bit key/value cache: pages of 64 tokens in one device buffer.
+
+    KV4Cache(kv_heads, head_dim, pages=n) allocates uint8 [n, kv_heads,
+    76*head_dim] on `device`; data=t takes an existing buffer of that kind.
+    Tokens are addressed by slot = page*64 + place; which pages make up a
+    sequence is the caller's table.  head_dim is 64, 128 or 256."""
+
+    _Desc, _size = KV4CacheDesc, "lce_kv4_cache_size"
+
+    @staticmethod
+    def _record(head_dim):
+        return 76 * head_dim
+
+
+class KV8Cache(_PagedCache):
+    """An 8-bit key/value cache: pages of 64 tokens in one device buffer.
+
+    KV8Cache(kv_heads, head_dim, pages=n) allocates uint8 [n, kv_heads,
+    128*head_dim + 128] on `device`; data=t takes an existing buffer of that kind.
+    Which pages make up a sequence is the caller's table; its token j is in slot
+    table[j//64]*64 + j%64.  head_dim is 64, 128 or 256."""
+
+    _Desc, _size = KV8CacheDesc, "lce_kv8_cache_size"
+
+    @staticmethod
+    def _record(head_dim):
+        return 128 * head_dim + 128
 
 
 def _require_like(t, dtype, device, name):
@@ -780,9 +874,9 @@ def _require_like(t, dtype, device, name):
         raise ValueError(f"{name} must be contiguous")
 
 
-def _require_cache(cache):
-    if not isinstance(cache, KV4Cache):
-        raise TypeError("cache must be a KV4Cache")
+def _require_cache(cache, kind=KV4Cache):
+    if not isinstance(cache, kind):
+        raise TypeError(f"cache must be a {kind.__name__}")
 
 
 def _require_heads(t, cache, name):
@@ -1026,6 +1120,312 @@ def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_
     if st != LCE_OK:
         raise LceError(st, last_error())
     return out
+
+
+KV8_PAGE = 64
+KV8_BLOCK = 16
+KV8_WORKSPACE_ZERO = 131072
+
+
+def _require_sequences(cache, table, q_start, lengths):
+    """The index tensors of a call over sequences."""
+    import torch
+    device = cache.data.device
+    _require_like(table, torch.int32, device, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences, pages]")
+    for t, name, n in ((q_start, "q_start", table.shape[0] + 1),
+                       (lengths, "lengths", table.shape[0])):
+        _require_like(t, torch.int32, device, name)
+        if t.shape != (n,):
+            raise ValueError(f"{name} must have {n} elements, got {list(t.shape)}")
+
+
+def _kv8_append_refused(cache, k, v, table, q_start, lengths):
+    """Raises for what kv8_append does not take."""
+    _require_cache(cache, KV8Cache)
+    _require_heads(k, cache, "k")
+    _require_heads(v, cache, "v")
+    if k.shape != v.shape or k.shape[1] != cache.kv_heads:
+        raise ValueError(f"k and v must be [tokens, {cache.kv_heads}, {cache.head_dim}], got "
+                         f"{list(k.shape)} and {list(v.shape)}")
+    if k.dtype != v.dtype:
+        raise TypeError(f"k and v must have one dtype, got {k.dtype} and {v.dtype}")
+    _float_type(k.dtype, "k")
+    _require_sequences(cache, table, q_start, lengths)
+
+
+def kv8_append(cache: KV8Cache, k, v, table, q_start, lengths) -> None:
+    """Quantize the last tokens of sequences into the cache (lce_kv8_append).
+
+    k and v [tokens, kv_heads, head_dim], float32, float16 or bfloat16, any token and head
+    strides that are multiples of 16 bytes: those of sequence b are rows
+    q_start[b]:q_start[b+1] and become its last tokens; table int32 [seqs, pages], lengths
+    int32 [seqs] (the new tokens included).  No two sequences may append to one block of
+    16 tokens."""
+    try:
+        n, heads, dim = k.shape
+        seqs, width = table.shape
+        ks, vs = k.stride(), v.stride()
+        dtype = k.dtype
+        code = cache._types.get(dtype, -1)
+        fine = (type(cache) is KV8Cache and code >= 0 and heads == cache.kv_heads
+                and dim == cache.head_dim and v.shape == k.shape and v.dtype is dtype
+                and ks[2] == vs[2] == 1 and k.get_device() == v.get_device() == cache._index
+                and cache._holds(table, cache._int32) and cache._holds(q_start, cache._int32)
+                and cache._holds(lengths, cache._int32) and q_start.shape == (seqs + 1,)
+                and lengths.shape == (seqs,))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _kv8_append_refused(cache, k, v, table, q_start, lengths)
+        n, code, (seqs, width), ks, vs = (k.shape[0], _float_type(k.dtype, "k"), table.shape,
+                                          k.stride(), v.stride())
+    if (n | seqs | width) >> 31:
+        _int32_refused(tokens=n, sequences=seqs, table=width)
+    _launch(cache._index, lib().lce_kv8_append, cache._ref, cache._data.data_ptr(), code,
+            k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], n, seqs, width,
+            table.data_ptr(), q_start.data_ptr(), lengths.data_ptr(), _stream_handle(k))
+
+
+def kv8_read(cache: KV8Cache, slots, *, dtype=None, out=None):
+    """The values that the cache holds for `slots` (int64 [tokens]): a pair k, v
+    [tokens, kv_heads, head_dim] of `dtype` (default bfloat16), or into the pair
+    `out`.  Slots outside the cache read as zeros."""
+    import torch
+    _require_cache(cache, KV8Cache)
+    if not isinstance(slots, torch.Tensor) or not cache._holds(slots, torch.int64):
+        _require_like(slots, torch.int64, cache.data.device, "slots")
+    if slots.dim() != 1:
+        raise ValueError("slots must have one dimension")
+    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    if out is None:
+        if dtype is None:
+            dtype = torch.bfloat16
+        code = _float_type(dtype, "dtype")
+        k = torch.empty(shape, dtype=dtype, device=cache._device)
+        v = torch.empty_like(k)
+    else:
+        k, v = out
+        for t, name in ((k, "out[0]"), (v, "out[1]")):
+            _require_like(t, k.dtype if dtype is None else dtype, slots.device, name)
+            if t.shape != shape:
+                raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        code = _float_type(k.dtype, "out")
+    _launch(cache._index, lib().lce_kv8_read, cache._ref, cache._data.data_ptr(),
+            slots.data_ptr(), shape[0], code, k.data_ptr(), v.data_ptr(), _stream_handle(slots))
+    return k, v
+
+
+def kv8_workspace(cache: KV8Cache, q, table):
+    """Workspace (uint8, zeroed) for kv8_attention calls with q's and table's shapes, or
+    with fewer tokens: at most 69 MB.  Calls that may overlap need one each."""
+    import torch
+    _require_cache(cache, KV8Cache)
+    _require_heads(q, cache, "q")
+    _require_like(table, torch.int32, cache.data.device, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [sequences, pages]")
+    _int32_refused(tokens=q.shape[0], heads=q.shape[1], sequences=table.shape[0],
+                   table=table.shape[1])
+    d = KV8QueryDesc(q.shape[0], q.shape[1], table.shape[0], table.shape[1])
+    n = ctypes.c_int64()
+    _check(lib().lce_kv8_workspace_size(cache._ref, ctypes.byref(d), ctypes.byref(n)))
+    ws = torch.empty(n.value, dtype=torch.uint8, device=cache.data.device)
+    ws[:KV8_WORKSPACE_ZERO].zero_()
+    return ws
+
+
+def _kv8_attention_refused(cache, q, table, q_start, lengths, slopes, prefix):
+    """Raises for what kv8_attention does not take."""
+    import torch
+    _require_cache(cache, KV8Cache)
+    _require_heads(q, cache, "q")
+    _require_sequences(cache, table, q_start, lengths)
+    if q.dtype == torch.float32:
+        raise TypeError("q must be float16 or bfloat16, got torch.float32")
+    _float_type(q.dtype, "q")
+    for t, name, dtype, n in ((slopes, "slopes", torch.float32, q.shape[1]),
+                              (prefix, "prefix", torch.int32, table.shape[0])):
+        if t is not None:
+            _require_like(t, dtype, cache.data.device, name)
+            if t.shape != (n,):
+                raise ValueError(f"{name} must have {n} elements, got {list(t.shape)}")
+
+
+def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optional[float] = None,
+                  causal: bool = True, window: int = 0, softcap: float = 0.0, slopes=None,
+                  prefix=None, max_q: Optional[int] = None, max_len: Optional[int] = None,
+                  out=None, return_lse: bool = False, workspace=None):
+    """Attention of new tokens over cached sequences (lce_kv8_attention).
+
+    q [tokens, q_heads, head_dim], float16 or bfloat16: the tokens of sequence b are rows
+    q_start[b]:q_start[b+1] and stand at its end; table int32 [seqs, pages], lengths int32
+    [seqs] (cached tokens, the new ones included).  window > 0 hides tokens further back;
+    softcap > 0 caps scores at softcap*tanh(score/softcap); slopes float32 [q_heads] takes
+    slope times the distance off them; prefix int32 [seqs] is the number of a sequence's
+    first tokens that all its rows see (causal).  max_q and max_len, the most new tokens
+    and the longest length, help to split the work.  Returns out, or (out, lse float32
+    [tokens, q_heads])."""
+    try:
+        tokens, heads, dim = q.shape
+        seqs, width = table.shape
+        strides = q.stride()
+        code = cache._types.get(q.dtype, 0)
+        i32 = cache._int32
+        fine = (type(cache) is KV8Cache and code > 0 and dim == cache.head_dim and strides[2] == 1
+                and table.dtype is q_start.dtype is lengths.dtype is i32
+                and q.get_device() == table.get_device() == q_start.get_device()
+                == lengths.get_device() == cache._index
+                and table.is_contiguous() and q_start.is_contiguous() and lengths.is_contiguous()
+                and q_start.shape == (seqs + 1,) and lengths.shape == (seqs,)
+                and (slopes is None or cache._holds(slopes, cache._float32)
+                     and slopes.shape == (heads,))
+                and (prefix is None or cache._holds(prefix, i32) and prefix.shape == (seqs,)))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _kv8_attention_refused(cache, q, table, q_start, lengths, slopes, prefix)
+        (tokens, heads, _), (seqs, width), strides = q.shape, table.shape, q.stride()
+        code = _float_type(q.dtype, "q")
+    max_q, max_len = max_q or 0, max_len or 0
+    if (tokens | heads | seqs | width | window | max_q | max_len) >> 31:
+        _int32_refused(tokens=tokens, heads=heads, sequences=seqs, table=width, window=window,
+                       max_q=max_q, max_len=max_len)
+    d = KV8QueryDesc(tokens, heads, seqs, width, code, 1 if causal else 0, window, max_q, max_len,
+                     cache._scale if scale is None else scale, softcap, strides[0], strides[1])
+    if out is None:
+        out = cache._empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
+    else:
+        _require_like(out, q.dtype, q.device, "out")
+        if out.shape != q.shape:
+            raise ValueError(f"out must be {list(q.shape)}, got {list(out.shape)}")
+    lse = (cache._empty((tokens, heads), dtype=cache._float32, device=cache._device) if return_lse
+           else None)
+    if workspace is None:
+        workspace = kv8_workspace(cache, q, table)
+    elif not cache._holds(workspace, cache._uint8):
+        _require_like(workspace, cache._uint8, cache.data.device, "workspace")
+    _launch(cache._index, lib().lce_kv8_attention, cache._ref, cache._data.data_ptr(),
+            ctypes.byref(d), q.data_ptr(), table.data_ptr(), q_start.data_ptr(),
+            lengths.data_ptr(), None if slopes is None else slopes.data_ptr(),
+            None if prefix is None else prefix.data_ptr(), out.data_ptr(),
+            None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
+            _stream_handle(q))
+    return (out, lse) if return_lse else out
+
+
+ROTARY_SCALING = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+class Rotary:
+    """Frequencies of rotary positions, for rotary().
+
+    The first rot_dim channels (default: all) of heads of head_dim are turned, in pairs
+    (i, i + rot_dim/2) or, interleaved, (2i, 2i + 1), pair i by base**(-2i/rot_dim) radians a
+    position.  scaling, for contexts `factor` times as long as trained: "linear", "ntk" or
+    "yarn" (trained on `original` positions); see lce_rotary_frequencies.  freqs (float64
+    [rot_dim/2], host) gives frequencies instead, and scale what results are multiplied
+    by."""
+
+    def __init__(self, head_dim: int, *, rot_dim: Optional[int] = None, base: float = 10000.0,
+                 interleaved: bool = False, scaling: Optional[str] = None, factor: float = 1.0,
+                 original: int = 4096, freqs=None, scale: Optional[float] = None, device="cuda"):
+        import torch
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        _int32_refused(head_dim=head_dim, rot_dim=rot_dim)
+        if not 2 <= head_dim <= 65536:
+            raise ValueError(f"head_dim must be in [2, 65536], got {head_dim}")
+        if rot_dim < 2 or rot_dim % 2 or rot_dim > head_dim:
+            raise ValueError(f"rot_dim must be an even number in [2, {head_dim}], got {rot_dim}")
+        if scaling not in ROTARY_SCALING:
+            raise ValueError(f"scaling must be one of {list(ROTARY_SCALING)}, got {scaling!r}")
+        n = rot_dim // 2
+        values, factor_out = (ctypes.c_double * n)(), ctypes.c_float(1.0)
+        if freqs is None:
+            _check(lib().lce_rotary_frequencies(rot_dim, base, ROTARY_SCALING[scaling], factor,
+                                                original, values, ctypes.byref(factor_out)))
+        else:
+            if scaling is not None:
+                raise ValueError("give either freqs or scaling")
+            freqs = torch.as_tensor(freqs, dtype=torch.float64, device="cpu")
+            if freqs.shape != (n,):
+                raise ValueError(f"freqs must have {n} elements, got {list(freqs.shape)}")
+            values[:] = freqs.tolist()
+        turns = (ctypes.c_uint64 * n)()
+        _check(lib().lce_rotary_turns(values, n, turns))
+        self.head_dim, self.rot_dim, self.interleaved = head_dim, rot_dim, bool(interleaved)
+        self.scale = factor_out.value if scale is None else float(scale)
+        self.freqs = torch.tensor(list(values), dtype=torch.float64)
+        if torch.device(device).type != "cuda":
+            raise ValueError(f"device must be a GPU, got {device}")
+        # (as int64: the same bits)
+        self._turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns],
+                                   dtype=torch.int64).to(device)
+        self._index = self._turns.get_device()
+
+
+def _rotary_rows(plan, t, out, name, n, dtype):
+    """Checks one tensor of a rotary call; its rows."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != plan._index:
+        raise ValueError(f"{name} must be on {plan._turns.device}, got {t.device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != plan.head_dim:
+        raise ValueError(f"{name} must be [{n}, heads, {plan.head_dim}], got {list(t.shape)}")
+    if t.stride(2) != 1 and t.numel():
+        raise ValueError(f"{name}'s channels must be contiguous")
+    _int32_refused(heads=t.shape[1])
+    x, y = t.stride(), out.stride()
+    return RotaryRows(t.shape[1], t.data_ptr(), out.data_ptr(), x[0], x[1], y[0], y[1])
+
+
+def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=None):
+    """q [tokens, q_heads, head_dim], and k [tokens, kv_heads, head_dim] unless it is None,
+    turned to `positions` (int64 [tokens]) in one launch (lce_rotary): float32, float16 or
+    bfloat16, any token and head strides.  backward: q and k are gradients of what was
+    turned, and get turned back (and scaled) to those of what went in.  Returns new
+    tensors, or writes `out` (q's, or a pair), which may be q and k themselves."""
+    import torch
+    if not isinstance(plan, Rotary):
+        raise TypeError("plan must be a Rotary")
+    if not isinstance(q, torch.Tensor):
+        raise TypeError("q must be a torch.Tensor")
+    code = _float_type(q.dtype, "q")
+    if q.dim() != 3:
+        raise ValueError(f"q must be [tokens, heads, {plan.head_dim}], got {list(q.shape)}")
+    n = q.shape[0]
+    _int32_refused(tokens=n)
+    _require_like(positions, torch.int64, plan._turns.device, "positions")
+    if positions.shape != (n,):
+        raise ValueError(f"positions must have {n} elements, got {list(positions.shape)}")
+    ins = (q,) if k is None else (q, k)
+    if out is None:
+        outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device)
+                     if isinstance(t, torch.Tensor) else t for t in ins)
+    else:
+        outs = (out,) if k is None else tuple(out)
+        if len(outs) != len(ins):
+            raise ValueError(f"out must be {len(ins)} tensors")
+        for t, o, name in zip(ins, outs, ("q", "k")):
+            if not isinstance(o, torch.Tensor):
+                raise TypeError(f"out of {name} must be a torch.Tensor")
+            if (o.shape, o.dtype, o.device) != (t.shape, t.dtype, t.device):
+                raise ValueError(f"out of {name} must be like it: {list(t.shape)} {t.dtype} on "
+                                 f"{t.device}, got {list(o.shape)} {o.dtype} on {o.device}")
+            if o.stride(2) != 1 and o.numel():
+                raise ValueError(f"out of {name}: channels must be contiguous")
+    rows = [_rotary_rows(plan, t, o, name, n, q.dtype)
+            for t, o, name in zip(ins, outs, ("q", "k"))]
+    d = RotaryDesc(n, plan.head_dim, plan.rot_dim, code, 1 if plan.interleaved else 0,
+                   1 if backward else 0, plan.scale)
+    _launch(plan._index, lib().lce_rotary, ctypes.byref(d), plan._turns.data_ptr(),
+            positions.data_ptr(), ctypes.byref(rows[0]),
+            ctypes.byref(rows[1]) if k is not None else None, _stream_handle(q))
+    return outs[0] if k is None else outs
 
 
 class PreparedBitpack:

@@ -17,7 +17,8 @@ SOURCES = [os.path.join(CSRC, f) for f in ("lce.hip", "mfma_tiles.hip", "mfma_fs
                                                   "mfma_stream_ohwi.hip",
                                                   "quant_conv.hip", "kv4.hip", "kv4_codec.hip",
                                                   "kv4_attend16.hip", "kv4_attend128.hip",
-                                                  "kv4_select.hip")]
+                                                  "kv4_select.hip", "kv8.hip", "kv8_codec.hip",
+                                                  "kv8_attend16.hip", "rotary.hip")]
 BUILD_DIR = os.path.join(PKG, "_build")
 # Measurement-only probe of the xor/popcount VALU rate (not part of the C ABI).
 PROBE_LIB = os.path.join(PKG, "libprobe.so")
@@ -25,7 +26,8 @@ PROBE_SOURCES = [os.path.join(CSRC, "valu_probe.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("bitpack.hpp", "bconv.hpp", "pool.hpp",
                                                  "bconv_mfma.hpp", "launch.hpp", "mfma_fs_launch.hpp", "dpp.hpp",
                                                  "bconv_quant.hpp", "bconv_mfma_stream.hpp", "fastdiv.hpp", "mfma_stream_launch.hpp",
-                                                 "status.hpp", "kv4.hpp", "kv4_launch.hpp", "kv4_attend.hpp")] + \
+                                                 "status.hpp", "kv4.hpp", "kv4_launch.hpp", "kv4_attend.hpp", "kv8.hpp",
+                                                 "kv8_attend.hpp")] + \
           [os.path.join(INCLUDE, "lce.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,183 @@
+// What the attention kernels over the 8-bit cache share.
+#pragma once
+
+#include "kv8.hpp"
+
+namespace lce {
+namespace kv8 {
+
+// Codes are multiplied in the queries' type, times a power of two that brings the largest
+// scale of what is multiplied together to 2^kUp: bfloat16 then holds every code of every
+// scale that counts, float16 every code whose scale is down to 2^-22 of the largest, and
+// smaller ones to 2^-25 (of 448 * 2^7).
+template <typename E>
+constexpr int kUp = __is_same(E, F16) ? 7 : 0;
+
+// Two codes (the low or the high half of w) as a packed pair of E::T, times s, a power of two.
+template <typename E, bool HIGH>
+__device__ __forceinline__ uint32_t decode_codes(uint32_t w, float s) {
+    if constexpr (__is_same(E, F16))
+        return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HIGH));
+    else
+        return bits_as<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HIGH));
+}
+
+template <typename E>
+__device__ __forceinline__ u32x4 decode_eight(uint32_t a, uint32_t b, float sa, float sb) {
+    return u32x4{decode_codes<E, false>(a, sa), decode_codes<E, true>(a, sa),
+                 decode_codes<E, false>(b, sb), decode_codes<E, true>(b, sb)};
+}
+
+// 2^(e - of + up) for scale bytes e <= of (2^-126 where it would be less).
+__device__ __forceinline__ float relative(int e, int of, int up) {
+    return bits_as<float>((uint32_t)max(127 + e - of + up, 1) << 23);
+}
+
+// The scale bytes (byte i: block i) of a page of which some row sees tokens [lo, hi):
+// blocks that no row sees weigh next to nothing, whatever their bytes are.
+__device__ __forceinline__ uint32_t settled_scales(uint32_t scales, int lo, int hi) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) {
+        const bool seen = kBlock * i < hi && kBlock * (i + 1) > lo;
+        const uint32_t e = (uint32_t)clampi((int)(scales >> (8 * i) & 255u), kLeastScale, kMostScale);
+        w |= (seen ? e : (uint32_t)kLeastScale) << (8 * i);
+    }
+    return w;
+}
+
+__device__ __forceinline__ int byte_of(uint32_t w, int i) { return (int)(w >> (8 * i) & 255u); }
+
+__device__ __forceinline__ int largest_of(uint32_t w) {
+    return max(max(byte_of(w, 0), byte_of(w, 1)), max(byte_of(w, 2), byte_of(w, 3)));
+}
+
+// The bytes of a word of value codes, tokens first .. first + 3, that some row sees, [lo,
+// hi) being what some row sees: the others may be anything, and a weight of 0 times a NaN
+// is not 0.
+__device__ __forceinline__ uint32_t seen_bytes(int first, int lo, int hi) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (first + i >= lo && first + i < hi) w |= 255u << (8 * i);
+    return w;
+}
+
+// What a call does to a score between its product and the softmax.
+struct Change {
+    float cap, inverse;    // log2 units; 1 / cap
+    float slope;           // of this lane's row, log2 units a token
+    int position;          // of this lane's row
+
+    // x: a scaled score (log2 units) of token j
+    __device__ __forceinline__ float operator()(float x, int j) const {
+        if (cap > 0.0f) {
+            // cap * tanh(u): 1 - 2 / (exp(2u) + 1), whose ends, exponentials of 0 and
+            // infinity, give -1 and 1; of small u, where that cancels, the power series
+            // (|u| < 1/4: up to u^9, off by less than 2^-26 of it)
+            const float u = x * inverse, z = u * u;
+            const float e = __builtin_amdgcn_exp2f(u * 2.88539008177792681f);
+            float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
+            t = __builtin_fmaf(z, t, 2.0f / 15);
+            t = __builtin_fmaf(z, t, -1.0f / 3);
+            t = __builtin_fmaf(z * t, x, x);
+            const float far = __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
+            x = z < 0.0625f ? t : far;
+        }
+        return __builtin_fmaf(-slope, __builtin_fabsf((float)(position - j)), x);
+    }
+};
+
+// A split's state in the workspace: (m, l) of each row and the scale byte of its sums,
+// then the sums of four channels at a time, `rows` rows next to each other.
+template <int D, int ROWS>
+struct Part {
+    static constexpr int kFloats = ROWS * (D + 4);
+    static __device__ __forceinline__ int state(int row) { return 4 * row; }
+    static __device__ __forceinline__ int sums(int rows, int row, int quad) {
+        return 4 * ROWS + 4 * (quad * rows + row);
+    }
+};
+
+// Four channels of a row over all its splits, sixteen splits at a time, each with its own
+// maximum and scale, against running ones.
+struct Joined {
+    f32x4 o;
+    float top, l;
+    int scale;
+};
+
+template <int D, int ROWS>
+__device__ __forceinline__ Joined join_parts(const float *part, int splits, int rows, int row,
+                                             int quad) {
+    typedef Part<D, ROWS> P;
+    Joined r;
+    r.o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    r.top = kNone;
+    r.l = 0.0f;
+    r.scale = kLeastScale;
+    for (int s0 = 0; s0 < splits; s0 += 16) {
+        f32x2 ml[16];
+        int scale[16];
+        f32x4 y[16];
+        // four at a time are there or not: what is past the last split is read again,
+        // and weighs nothing
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            ml[k] = f32x2{kNone, 0.0f};
+            scale[k] = kLeastScale;
+            y[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+#pragma unroll
+        for (int k0 = 0; k0 < 16; k0 += 4)
+            if (s0 + k0 < splits) {
+#pragma unroll
+                for (int k = k0; k < k0 + 4; ++k) {
+                    const float *from = part + (int64_t)min(s0 + k, splits - 1) * P::kFloats;
+                    const float *sums = from + P::sums(rows, row, quad);
+                    const f32x2 a = got(sums), b = got(sums + 2);
+                    ml[k] = got(from + P::state(row));
+                    scale[k] = (int)got(from + P::state(row) + 2)[0];
+                    y[k] = f32x4{a[0], a[1], b[0], b[1]};
+                }
+            }
+        float high = r.top;
+        int most = r.scale;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            high = fmaxf(high, ml[k][0]);
+            most = max(most, scale[k]);
+        }
+        const float f = __builtin_amdgcn_exp2f(r.top - high);
+        r.l *= f;
+        r.o *= f * relative(r.scale, most, 0);
+        r.top = high;
+        r.scale = most;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const float w = s0 + k < splits ? __builtin_amdgcn_exp2f(ml[k][0] - r.top) : 0.0f;
+            r.l += ml[k][1] * w;
+            r.o += y[k] * (w * relative(scale[k], most, 0));
+        }
+    }
+    return r;
+}
+
+// Four channels of a row's result, and the log of its sum.
+template <typename E>
+__device__ __forceinline__ u32x2 result(const f32x4 &o, float l, int scale) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    // codes' means are at most 448 * 2^kUp: only the last factor leaves float32's middle
+    const int e = scale - 127 - kUp<E>;
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_ldexpf(o[i] * inv, e);
+    return u32x2{pack_pair<E>(x[0], x[1]), pack_pair<E>(x[2], x[3])};
+}
+
+__device__ __forceinline__ float log_sum(float top, float l) {
+    return l == 0.0f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+}
+
+}  // namespace kv8
+}  // namespace lce

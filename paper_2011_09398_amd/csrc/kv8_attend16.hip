@@ -1,0 +1,489 @@
+// Attention over the 8-bit cache, 16 or 32 query rows a tile: single tokens, a few tokens,
+// short prompts.
+#include "kv8_attend.hpp"
+
+namespace lce {
+namespace kv8 {
+namespace {
+
+constexpr int kWaves = kThreads / 64;
+
+// A load from the cache; ONCE: past the caches, of what nobody else will read soon.
+template <bool ONCE, typename V>
+__device__ __forceinline__ V fetch(const uint8_t *p) {
+    if constexpr (ONCE)
+        return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+    else
+        return *reinterpret_cast<const V *>(p);
+}
+
+// What a wave takes at a time: a page, or half of one where heads are so wide that the
+// codes of a whole one would leave no registers for what else there is.
+template <int D>
+struct Step {
+    static constexpr int kTiles = D <= 128 ? 4 : 2;        // of 16 tokens
+    static constexpr int kPerPage = 4 / kTiles;
+    static constexpr int kTokens = 16 * kTiles;
+    static constexpr int kChunks = D / 64;
+};
+
+// Key codes as a wave's lanes hold them.  Lane (n, g), n = lane % 16, g = lane / 16: of
+// tokens 16t + n the channels 64c + 16g .. +15, which are the first operands of two
+// products of 32 channels (the order of channels does not matter, as long as the queries
+// are in the same).
+template <int D>
+struct Keys {
+    u32x4 k[Step<D>::kTiles][Step<D>::kChunks];
+
+    template <bool ONCE>
+    __device__ __forceinline__ void load(const uint8_t *rec, int half, int n, int g) {
+#pragma unroll
+        for (int t = 0; t < Step<D>::kTiles; ++t)
+#pragma unroll
+            for (int c = 0; c < Step<D>::kChunks; ++c)
+                k[t][c] = fetch<ONCE, u32x4>(rec + Record<D>::kKey +
+                                             (half * Step<D>::kTokens + 16 * t + n) * D + 64 * c +
+                                             16 * g);
+    }
+};
+
+// Value codes: lane (n, g) holds of channels 64c + 4n .. +3 tokens 16t + 4g .. +3, a word
+// for each channel.
+template <int D>
+struct Values {
+    u32x4 v[Step<D>::kTiles][Step<D>::kChunks];
+
+    template <bool ONCE>
+    __device__ __forceinline__ void load(const uint8_t *rec, int half, int n, int g) {
+#pragma unroll
+        for (int t = 0; t < Step<D>::kTiles; ++t)
+#pragma unroll
+            for (int c = 0; c < Step<D>::kChunks; ++c)
+                v[t][c] = fetch<ONCE, u32x4>(
+                    rec + Record<D>::kValue +
+                    ((half * Step<D>::kTiles + t) * 4 + g) * 4 * D + (64 * c + 4 * n) * 4);
+    }
+    // what no row sees
+    __device__ __forceinline__ void clear(int first, int lo, int hi) {
+#pragma unroll
+        for (int t = 0; t < Step<D>::kTiles; ++t) {
+            const uint32_t mask = seen_bytes(first + 16 * t, lo, hi);
+#pragma unroll
+            for (int c = 0; c < Step<D>::kChunks; ++c) v[t][c] &= mask;
+        }
+    }
+};
+
+// Queries of 16 rows as second operands: lane (n, g) holds of row n the channels that it
+// holds of the keys.
+template <int D>
+struct Queries {
+    u32x4 q[Step<D>::kChunks][2];
+
+    __device__ __forceinline__ void load(const void *row, bool valid, int g) {
+#pragma unroll
+        for (int c = 0; c < Step<D>::kChunks; ++c) {
+            q[c][0] = q[c][1] = u32x4{0, 0, 0, 0};
+            if (valid) {
+                const u32x4 *at = reinterpret_cast<const u32x4 *>(
+                    static_cast<const uint16_t *>(row) + 64 * c + 16 * g);
+                q[c][0] = at[0], q[c][1] = at[1];
+            }
+        }
+    }
+};
+
+// A row's state: running maximum of scores (log2), this lane's share of the sum, and the
+// sums of weighted values: o[4c + x][i] of lane (n, g) is row n, channel 64c + 16g + 4i + x.
+template <int D>
+struct RowState {
+    float m, l;
+    f32x4 o[D / 16];
+};
+
+template <int D, int C>
+struct Shared {
+    f32x4 o[kWaves][D / 4][16 * C];
+    f32x2 ml[kWaves][16 * C];
+    int scale[kWaves];
+    int last;
+};
+
+// A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
+// Scores times c are in log2 units.
+template <typename E, int D>
+__device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[Step<D>::kTiles],
+                                      u32x4 (&p)[Step<D>::kTiles / 2], float c) {
+    constexpr int kTiles = Step<D>::kTiles;
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
+    top *= c;
+    // (Of large maxima, the difference is exact where a sum is not.  Each row goes by
+    // its own maximum, so that no bit of it depends on the rows beside it.)
+    if (__builtin_amdgcn_ballot_w64(top - st.m > kLag + E::kLift)) {
+        const float high = across_rows(top, [](float a, float b) { return fmaxf(a, b); });
+        const float all = high - st.m > kLag + E::kLift ? high - E::kLift : st.m;
+        const float f = __builtin_amdgcn_exp2f(st.m - all);
+        st.m = all;
+        st.l *= f;
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) st.o[m] *= f;
+    }
+    // The fused product below differs from the rounded one that the maximum is: where
+    // that could show (scores past kLarge), round the scores' products too.
+    const bool large = __builtin_fabsf(st.m) > kLarge;
+    if (__builtin_amdgcn_ballot_w64(large)) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) s[t] = large ? s[t] * c : s[t];
+        c = large ? 1.0f : c;
+    }
+    // summed by themselves: a long sequence's many small ones would be rounded one by one
+    // to the last place of a large sum
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, -st.m));
+            sum += w[i];
+        }
+        p[t / 2][t % 2 * 2] = pack_pair<E>(w[0], w[1]);
+        p[t / 2][t % 2 * 2 + 1] = pack_pair<E>(w[2], w[3]);
+    }
+    st.l += sum;
+}
+
+}  // namespace
+
+// Grid (tiles * kv_heads, splits), four waves.  A tile is C times 16 rows of one head
+// of the cache: rows are the queries of one sequence times the heads that share the cache
+// head, in that order.  The waves take the pages of their workgroup's split in turn, each
+// with all rows, and join their states at the end; the last split of a tile to finish
+// joins all of them, in the order of the splits, so that results do not depend on timing.
+//
+// Keys are the first operand and queries the second, so that a lane's scores belong to one
+// row and the weights leave the softmax as the second operand of the product with the
+// values; no weight and no score crosses lanes.  Codes become two-byte floats in the
+// conversion instruction, which multiplies them by their block's power of two as well: of
+// the keys against the page's largest, which the scores are multiplied by in float32, of
+// the values against the largest that the wave has seen.
+template <typename E, int D, int C, bool CHANGE, bool ONCE>
+__global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16_kernel(
+    AttendParams p) {
+    constexpr int kRows = 16 * C;
+    typedef Step<D> S;
+    __shared__ Shared<D, C> sh;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Workgroups go to the eight XCDs in turn, and where the grid is a multiple of eight
+    // wide all splits of a tile would go to one: tiles are moved on by one a split.
+    const int split = blockIdx.y;
+    int unit = blockIdx.x;
+    if (p.turn) {
+        unit += split % 8;
+        if (unit >= p.turn) unit -= p.turn;
+    }
+    const int head = unit % p.kv_heads, slot = unit / p.kv_heads;
+
+    // a sequence's tiles begin at floor(rows before it / kRows) + its index: at most one
+    // more than it needs, and none shared
+    const auto first = [&](int s, int b) { return (int64_t)s * p.group / kRows + b; };
+    const Sequence seq =
+        find_sequence(p.q_start, p.lengths, p.seqs, p.tokens, p.width, slot, first);
+    if (seq.index < 0) return;
+    const int rows = seq.queries * p.group;
+    const int row0 = (int)(slot - first(seq.start, seq.index)) * kRows;
+    if (row0 >= rows) return;
+    const int valid = min(rows - row0, kRows);
+    const int prefix = p.prefix ? p.prefix[seq.index] : 0;
+    // this lane's row of each sixteen
+    int i[C], hq[C];
+    bool mine[C];
+    Span span[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int row = row0 + 16 * c + n;
+        i[c] = row / p.group, hq[c] = head * p.group + row % p.group;
+        mine[c] = 16 * c + n < valid;
+        span[c] = visible(seq, i[c], p.causal, p.window, prefix);
+    }
+    // spans move up with the rows: the tile's first and last row bound them
+    const Span a = visible(seq, row0 / p.group, p.causal, p.window, prefix);
+    const Span z = visible(seq, (row0 + valid - 1) / p.group, p.causal, p.window, prefix);
+
+    // this workgroup's share of the pages
+    const int page0 = a.lo / kPage;
+    const int count = z.hi > a.lo ? (z.hi + kPage - 1) / kPage - page0 : 0;
+    const int splits = clampi((count + p.chunk - 1) / p.chunk, 1, (int)gridDim.y);
+    if (split >= splits) return;
+    const int begin = split * p.chunk * S::kPerPage;               // in steps
+    const int end = (split == splits - 1 ? count : (split + 1) * p.chunk) * S::kPerPage;
+
+    RowState<D> st[C];
+    Queries<D> q[C];
+    Change change[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        st[c].m = kNone;
+        st[c].l = 0.0f;
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m) st[c].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        q[c].load((const uint16_t *)p.q + (int64_t)(seq.start + i[c]) * p.q_token +
+                      (int64_t)hq[c] * p.q_head,
+                  mine[c], g);
+        if constexpr (CHANGE) {
+            change[c].cap = p.cap_log2;
+            change[c].inverse = 1.0f / p.cap_log2;
+            change[c].slope =
+                p.slopes && mine[c] ? p.slopes[hq[c]] * 1.44269504088896341f : 0.0f;
+            change[c].position = seq.length - seq.queries + i[c];
+        }
+    }
+    const int32_t *table = p.table + (int64_t)seq.index * p.width;
+    const int64_t stride = (int64_t)p.kv_heads * Record<D>::kBytes;
+    const uint8_t *cache = p.cache + (int64_t)head * Record<D>::kBytes;
+
+    // 64 of this wave's steps at a time, one a lane: their numbers in the sequence, their
+    // pages in the cache, and which are there
+    int from = begin + wave, number = 0, phys = -1;
+    uint64_t todo = 0;
+    const auto look = [&]() {
+        while (!todo && from < end) {
+            const int e = from + kWaves * lane;
+            from += kWaves * 64;
+            number = page0 * S::kPerPage + e;
+            phys = e < end ? table[number / S::kPerPage] : -1;
+            todo = __builtin_amdgcn_ballot_w64(phys >= 0 && phys < p.pages);
+        }
+    };
+    const auto next = [&](int &step) {
+        const int at = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        step = __builtin_amdgcn_readlane(number, at);
+        return cache + (int64_t)__builtin_amdgcn_readlane(phys, at) * stride;
+    };
+
+    // Keys and values of one step are in registers at a time: the next one's keys are on
+    // their way once this one's weights are there, its values once this one's are added.
+    look();
+    Keys<D> keys;
+    Values<D> values;
+    u32x2 scales = {0, 0};
+    int step = 0, biggest = kLeastScale;
+    bool more = todo != 0;
+    if (more) {
+        const uint8_t *rec = next(step);
+        scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
+        keys.template load<ONCE>(rec, step % S::kPerPage, n, g);
+        values.template load<ONCE>(rec, step % S::kPerPage, n, g);
+    }
+    while (more) {
+        const int t0 = step * S::kTokens;
+        const bool masked = t0 < z.lo || t0 + S::kTokens > a.hi;
+        // scales of the page's blocks, then of the step's
+        const int from_block = step % S::kPerPage * S::kTiles;
+        uint32_t ks = __builtin_amdgcn_readfirstlane(scales[0]) >> (8 * from_block);
+        uint32_t vs = __builtin_amdgcn_readfirstlane(scales[1]) >> (8 * from_block);
+        // (of half a page, the other half's bytes are moved out: tokens from kTokens on)
+        ks = settled_scales(ks, a.lo - t0, min(z.hi - t0, S::kTokens));
+        vs = settled_scales(vs, a.lo - t0, min(z.hi - t0, S::kTokens));
+        const int km = largest_of(ks), vm = largest_of(vs);
+        f32x4 s[C][S::kTiles];
+#pragma unroll
+        for (int t = 0; t < S::kTiles; ++t) {
+            const float f = relative(byte_of(ks, t), km, kUp<E>);
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[c][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < S::kChunks; ++h)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const u32x4 k =
+                        decode_eight<E>(keys.k[t][h][2 * x], keys.k[t][h][2 * x + 1], f, f);
+#pragma unroll
+                    for (int c = 0; c < C; ++c) s[c][t] = E::mfma16(k, q[c].q[h][x], s[c][t]);
+                }
+        }
+        look();
+        more = todo != 0;
+        const uint8_t *rec = nullptr;
+        int following = 0;
+        if (more) rec = next(following);
+        float scale = __builtin_amdgcn_ldexpf(p.scale_log2, km - 127 - kUp<E>);
+        if constexpr (CHANGE) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int t = 0; t < S::kTiles; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        s[c][t][k] = change[c](s[c][t][k] * scale, t0 + 16 * t + 4 * g + k);
+            scale = 1.0f;
+        }
+        if (masked) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int lo = span[c].lo - t0 - 4 * g, hi = span[c].hi - t0 - 4 * g;
+#pragma unroll
+                for (int t = 0; t < S::kTiles; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int j = 16 * t + k;
+                        s[c][t][k] = j >= lo && j < hi ? s[c][t][k] : -__builtin_inff();
+                    }
+            }
+            values.clear(4 * g, a.lo - t0, z.hi - t0);
+        }
+        u32x4 w[C][S::kTiles / 2];
+#pragma unroll
+        for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], scale);
+        if (more) {
+            scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
+            keys.template load<ONCE>(rec, following % S::kPerPage, n, g);
+        }
+        if (vm > biggest) {
+            const float f = relative(biggest, vm, 0);
+            biggest = vm;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int m = 0; m < D / 16; ++m) st[c].o[m] *= f;
+        }
+        // ahead of the other waves' scores
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int u = 0; u < S::kTiles / 2; ++u) {
+            const float f0 = relative(byte_of(vs, 2 * u), biggest, kUp<E>);
+            const float f1 = relative(byte_of(vs, 2 * u + 1), biggest, kUp<E>);
+#pragma unroll
+            for (int h = 0; h < S::kChunks; ++h)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const u32x4 v = decode_eight<E>(values.v[2 * u][h][x],
+                                                    values.v[2 * u + 1][h][x], f0, f1);
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+                        st[c].o[4 * h + x] = E::mfma16(v, w[c][u], st[c].o[4 * h + x]);
+                }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (more) values.template load<ONCE>(rec, following % S::kPerPage, n, g);
+        step = following;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const float l = across_rows(st[c].l, [](float x, float y) { return x + y; });
+        if (g == 0) sh.ml[wave][16 * c + n] = f32x2{st[c].m, l};
+#pragma unroll
+        for (int h = 0; h < S::kChunks; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                sh.o[wave][16 * h + 4 * g + k][16 * c + n] =
+                    f32x4{st[c].o[4 * h][k], st[c].o[4 * h + 1][k], st[c].o[4 * h + 2][k],
+                          st[c].o[4 * h + 3][k]};
+    }
+    if (lane == 0) sh.scale[wave] = biggest;
+    __syncthreads();
+
+    // a thread for every four channels of a row, rows next to each other
+    const int shift = valid > 1 ? 32 - __builtin_clz(valid - 1) : 0;   // rows, a power of two
+    const auto write = [&](int r, int quad, const f32x4 &o, float top, float l, int scale) {
+        const int rr = row0 + r;
+        const int64_t at = (int64_t)(seq.start + rr / p.group) * (p.kv_heads * p.group) +
+                           head * p.group + rr % p.group;
+        *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + 4 * quad) =
+            result<E>(o, l, scale);
+        if (p.lse && quad == 0) p.lse[at] = log_sum(top, l);
+    };
+    typedef Part<D, kRows> P;
+    float *part = p.part + (int64_t)unit * gridDim.y * P::kFloats;
+    float *my = part + (int64_t)split * P::kFloats;
+    int most = sh.scale[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) most = max(most, sh.scale[w]);
+    for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
+        const int r = x & ((1 << shift) - 1), quad = x >> shift;
+        if (r >= valid) continue;
+        // the waves' states in their order
+        float top = sh.ml[0][r][0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][r][0]);
+        float l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const f32x2 ml = sh.ml[w][r];
+            const float f = __builtin_amdgcn_exp2f(ml[0] - top);
+            l += ml[1] * f;
+            o += sh.o[w][quad][r] * (f * relative(sh.scale[w], most, 0));
+        }
+        if (splits == 1) {
+            write(r, quad, o, top, l, most);
+        } else {
+            // several splits: this one's state into the workspace
+            if (quad == 0) {
+                put(my + P::state(r), f32x2{top, l});
+                put(my + P::state(r) + 2, f32x2{(float)most, 0.0f});
+            }
+            float *to = my + P::sums(valid, r, quad);
+            put(to, f32x2{o[0], o[1]});
+            put(to + 2, f32x2{o[2], o[3]});
+        }
+    }
+    if (splits == 1) return;
+
+    // the last split to get here joins them
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+        sh.last = last_of(p.tickets + (int64_t)unit * kTicketStride, splits);
+    __syncthreads();
+    if (!sh.last) return;
+    for (int x = threadIdx.x; x < D / 4 << shift; x += kThreads) {
+        const int r = x & ((1 << shift) - 1), quad = x >> shift;
+        if (r >= valid) continue;
+        const Joined j = join_parts<D, kRows>(part, splits, valid, r, quad);
+        write(r, quad, j.o, j.top, j.l, j.scale);
+    }
+}
+
+namespace {
+
+template <typename E, int D, int C, bool ONCE>
+void launch_c(const AttendParams &p, dim3 grid, hipStream_t s) {
+    if (p.slopes || p.cap_log2 > 0.0f)
+        hipLaunchKernelGGL((attend16_kernel<E, D, C, true, ONCE>), grid, dim3(kThreads), 0, s, p);
+    else
+        hipLaunchKernelGGL((attend16_kernel<E, D, C, false, ONCE>), grid, dim3(kThreads), 0, s, p);
+}
+
+template <typename E, int D>
+void launch_d(const AttendParams &p, int rows, bool once, dim3 grid, hipStream_t s) {
+    if constexpr (D <= 128) {
+        if (rows == 32) return launch_c<E, D, 2, false>(p, grid, s);
+    }
+    if (once) return launch_c<E, D, 1, true>(p, grid, s);
+    launch_c<E, D, 1, false>(p, grid, s);
+}
+
+template <typename E>
+void launch_t(const AttendParams &p, int dim, int rows, bool once, dim3 grid, hipStream_t s) {
+    if (dim == 64) launch_d<E, 64>(p, rows, once, grid, s);
+    else if (dim == 128) launch_d<E, 128>(p, rows, once, grid, s);
+    else launch_d<E, 256>(p, rows, once, grid, s);
+}
+
+}  // namespace
+
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool once, dim3 grid,
+                     hipStream_t s) {
+    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, rows, once, grid, s);
+    else launch_t<Bf16>(p, dim, rows, once, grid, s);
+}
+
+}  // namespace kv8
+}  // namespace lce
