@@ -100,11 +100,13 @@ int64_t query_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
     return (int64_t)(q.max_q > 0 ? q.max_q : q.tokens / q.seqs) * (q.q_heads / d.kv_heads);
 }
 
-int tile_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
+int tile_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q, bool prefix) {
     if (d.head_dim > 128) return 16;
     const int forced = tuning(LCE_TUNE_KV8_ROWS);
-    if (forced == 16 || forced == 32) return forced;
+    if (forced == 16 || forced == 32 || forced == 128) return forced;
     const int64_t most = query_rows(d, q), all = (int64_t)q.tokens * q.q_heads;
+    const bool brief = most_pages(q, prefix) <= 16;
+    if (most >= 128 && all >= 128 * (brief ? 256 : 512)) return 128;
     return most >= 256 && all >= 32 * 1024 ? 32 : 16;
 }
 
@@ -264,7 +266,7 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
         return fail(LCE_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
                     (long long)need);
 
-    const int rows = tile_rows(*desc, *query);
+    const int rows = tile_rows(*desc, *query, prefix != nullptr);
     const int64_t units = tiles(*desc, *query, rows) * desc->kv_heads;
     const double size = desc->head_dim / 128.0;
     const int64_t slots = desc->head_dim > 128 ? 512 : 768;   // workgroups that run at a time
@@ -275,10 +277,13 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     // floating point: max_q is the caller's word)
     const double spread = query->seqs * (double)desc->kv_heads;
     const int64_t likely = (int64_t)std::min((double)units, spread * ((each + rows - 1) / rows));
-    const Split s = split_pages(units, likely, most, 0.6 + 0.6 * size,
-                                (0.5 + 1.3 * size) * (several ? 2.5 : 1.0),
-                                query->window ? slots : several ? 512 : 7 * slots / 4,
-                                kMostParts * 16 / rows, 4);
+    const Split s =
+        rows == 128
+            ? split_pages(units, likely, most, 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8, 1)
+            : split_pages(units, likely, most, 0.6 + 0.6 * size,
+                          (0.5 + 1.3 * size) * (several ? 2.5 : 1.0),
+                          query->window ? slots : several ? 512 : 7 * slots / 4,
+                          kMostParts * 16 / rows, 4);
     const bool once = each <= 16 && 128.0 * desc->head_dim * most * likely >= (240 << 20);
     lce::kv8::AttendParams p;
     p.cache = static_cast<const uint8_t *>(cache);
@@ -300,9 +305,13 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     if (units > kMostGroups)
         return fail(LCE_EUNSUPPORTED, "%lld tiles: too many for one call", (long long)units);
     const dim3 grid((unsigned)units, (unsigned)s.splits);
-    static const char *const kNames[2][2] = {{"kv8-16", "kv8-32"}, {"kv8-16-split", "kv8-32-split"}};
-    lce::g_last_schedule = kNames[s.splits > 1][rows == 32];
-    lce::kv8::launch_attend16(p, query->type, desc->head_dim, rows, once, grid, stream);
+    static const char *const kNames[2][3] = {
+        {"kv8-16", "kv8-32", "kv8-128"}, {"kv8-16-split", "kv8-32-split", "kv8-128-split"}};
+    lce::g_last_schedule = kNames[s.splits > 1][rows == 16 ? 0 : rows == 32 ? 1 : 2];
+    if (rows == 128)
+        lce::kv8::launch_attend128(p, query->type, desc->head_dim, grid, stream);
+    else
+        lce::kv8::launch_attend16(p, query->type, desc->head_dim, rows, once, grid, stream);
     return check_launch("lce_kv8_attention launch");
 }
 

@@ -80,6 +80,8 @@ void launch_read(const ReadParams &p, int type, int dim, hipStream_t s);
 // the caches
 void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool once, dim3 grid,
                      hipStream_t s);
+// 128 query rows a workgroup, heads of up to 128; grid = (tiles * kv_heads, splits)
+void launch_attend128(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);
 
 }  // namespace kv8
 }  // namespace lce

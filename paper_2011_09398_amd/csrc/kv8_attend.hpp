@@ -46,6 +46,14 @@ __device__ __forceinline__ uint32_t settled_scales(uint32_t scales, int lo, int 
     return w;
 }
 
+// A value that all lanes have, in a scalar register (or what is made of it would be made in
+// all lanes).
+__device__ __forceinline__ uint32_t in_scalar(uint32_t x) {
+    uint32_t s = (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+    asm volatile("" : "+s"(s));
+    return s;
+}
+
 __device__ __forceinline__ int byte_of(uint32_t w, int i) { return (int)(w >> (8 * i) & 255u); }
 
 __device__ __forceinline__ int largest_of(uint32_t w) {
@@ -65,24 +73,38 @@ __device__ __forceinline__ uint32_t seen_bytes(int first, int lo, int hi) {
 
 // What a call does to a score between its product and the softmax.
 struct Change {
-    float cap, inverse;    // log2 units; 1 / cap
+    float cap;             // log2 units, 0: none
+    float inverse, twice;  // 1 / cap, 2 log2(e) / cap
     float slope;           // of this lane's row, log2 units a token
     int position;          // of this lane's row
+
+    __device__ __forceinline__ void set(float cap_log2, float slope_nats, int at) {
+        cap = cap_log2;
+        inverse = 1.0f / cap;
+        twice = 2.88539008177792681f / cap;
+        slope = slope_nats * 1.44269504088896341f;
+        position = at;
+    }
 
     // x: a scaled score (log2 units) of token j
     __device__ __forceinline__ float operator()(float x, int j) const {
         if (cap > 0.0f) {
             // cap * tanh(u): 1 - 2 / (exp(2u) + 1), whose ends, exponentials of 0 and
-            // infinity, give -1 and 1; of small u, where that cancels, the power series
-            // (|u| < 1/4: up to u^9, off by less than 2^-26 of it)
-            const float u = x * inverse, z = u * u;
-            const float e = __builtin_amdgcn_exp2f(u * 2.88539008177792681f);
-            float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
-            t = __builtin_fmaf(z, t, 2.0f / 15);
-            t = __builtin_fmaf(z, t, -1.0f / 3);
-            t = __builtin_fmaf(z * t, x, x);
+            // infinity, give -1 and 1, known to 2^-22 of the cap.  That is enough of caps
+            // in use; under large ones small u take the power series (|u| < 1/4: up to
+            // u^9, off by less than 2^-26 of it)
+            const float e = __builtin_amdgcn_exp2f(x * twice);
             const float far = __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
-            x = z < 0.0625f ? t : far;
+            if (cap > 256.0f) {
+                const float u = x * inverse, z = u * u;
+                float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
+                t = __builtin_fmaf(z, t, 2.0f / 15);
+                t = __builtin_fmaf(z, t, -1.0f / 3);
+                t = __builtin_fmaf(z * t, x, x);
+                x = z < 0.0625f ? t : far;
+            } else {
+                x = far;
+            }
         }
         return __builtin_fmaf(-slope, __builtin_fabsf((float)(position - j)), x);
     }
@@ -172,7 +194,7 @@ __device__ __forceinline__ u32x2 result(const f32x4 &o, float l, int scale) {
     float x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = __builtin_amdgcn_ldexpf(o[i] * inv, e);
-    return u32x2{pack_pair<E>(x[0], x[1]), pack_pair<E>(x[2], x[3])};
+    return u32x2{pack_result<E>(x[0], x[1]), pack_result<E>(x[2], x[3])};
 }
 
 __device__ __forceinline__ float log_sum(float top, float l) {

@@ -236,11 +236,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
                       (int64_t)hq[c] * p.q_head,
                   mine[c], g);
         if constexpr (CHANGE) {
-            change[c].cap = p.cap_log2;
-            change[c].inverse = 1.0f / p.cap_log2;
-            change[c].slope =
-                p.slopes && mine[c] ? p.slopes[hq[c]] * 1.44269504088896341f : 0.0f;
-            change[c].position = seq.length - seq.queries + i[c];
+            change[c].set(p.cap_log2, p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
+                          seq.length - seq.queries + i[c]);
         }
     }
     const int32_t *table = p.table + (int64_t)seq.index * p.width;
