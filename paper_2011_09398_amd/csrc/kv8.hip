@@ -138,24 +138,25 @@ struct Split {
 // `pages` pages of each of `likely` tiles (the grid has room for `units`), `step`
 // microseconds for a wave to take one: how many workgroups (of four waves) share a tile.
 // Sharing costs about `fixed` microseconds for the partial states, the ticket and the
-// joining, and 0.06 for each state joined, so a tile is divided only where its pages take
+// joining, and 0.11 for each state joined, so a tile is divided only where its pages take
 // longer, and no further than `most` workgroups in all and `parts` states in the
 // workspace.  `each`: the number of pages that a workgroup takes is a multiple of it, so
 // that all waves are busy to the end.
-Split split_pages(int64_t units, int64_t likely, int64_t pages, double step, double fixed,
-                  int64_t most, int64_t parts, int64_t each) {
+// Windows span `usual` pages, one or two less than they can.
+Split split_pages(int64_t units, int64_t likely, int64_t pages, int64_t usual, double step,
+                  double fixed, int64_t most, int64_t parts, int64_t each) {
     const int64_t some = std::max<int64_t>(likely, 1);
     const int64_t room = most_splits(units, parts);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV8_CHUNK)) {
         chunk = std::max(std::clamp<int64_t>(t, 1, chunk), (pages + room - 1) / room);
     } else {
-        const double whole = pages * step / 4;
-        // the least of whole / z + fixed + 0.06 z
+        const double whole = usual * step / 4;
+        // the least of whole / z + fixed + 0.11 z
         const double z = std::min(std::min((double)room, (double)most / some),
-                                  std::sqrt(whole / 0.06));
-        if (z > 1 && whole / z + fixed + 0.06 * z < whole)
-            chunk = ((int64_t)std::ceil(pages / z) + each - 1) / each * each;
+                                  std::sqrt(whole / 0.11));
+        if (z > 1 && whole / z + fixed + 0.11 * z < whole)
+            chunk = ((int64_t)std::ceil(usual / z) + each - 1) / each * each;
     }
     Split s;
     s.chunk = (int)chunk;
@@ -277,12 +278,18 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     // floating point: max_q is the caller's word)
     const double spread = query->seqs * (double)desc->kv_heads;
     const int64_t likely = (int64_t)std::min((double)units, spread * ((each + rows - 1) / rows));
+    const int64_t usual =
+        most < most_pages(*query, true) ? std::max<int64_t>(most - 2, 1) : most;
     const Split s =
         rows == 128
-            ? split_pages(units, likely, most, 2 + 2 * size, 4 + 8 * size, 512, kMostParts / 8, 1)
-            : split_pages(units, likely, most, 0.6 + 0.6 * size,
+            ? split_pages(units, likely, most, usual, 2 + 2 * size, 4 + 8 * size, 512,
+                          kMostParts / 8, 1)
+            : split_pages(units, likely, most, usual, 0.5 + 0.6 * size,
                           (0.5 + 1.3 * size) * (several ? 2.5 : 1.0),
-                          query->window ? slots : several ? 512 : 7 * slots / 4,
+                          query->window    ? slots
+                          : several        ? 512
+                          : likely < slots ? 4 * slots
+                                           : 7 * slots / 4,
                           kMostParts * 16 / rows, 4);
     const bool once = each <= 16 && 128.0 * desc->head_dim * most * likely >= (240 << 20);
     lce::kv8::AttendParams p;

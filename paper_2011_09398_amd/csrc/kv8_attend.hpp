@@ -71,42 +71,56 @@ __device__ __forceinline__ uint32_t seen_bytes(int first, int lo, int hi) {
     return w;
 }
 
-// What a call does to a score between its product and the softmax.
+// What a call does to scores between their product and the softmax.
 struct Change {
     float cap;             // log2 units, 0: none
-    float inverse, twice;  // 1 / cap, 2 log2(e) / cap
     float slope;           // of this lane's row, log2 units a token
     int position;          // of this lane's row
+    bool sloped;
 
-    __device__ __forceinline__ void set(float cap_log2, float slope_nats, int at) {
+    __device__ __forceinline__ void set(float cap_log2, bool slopes, float slope_nats, int at) {
         cap = cap_log2;
-        inverse = 1.0f / cap;
-        twice = 2.88539008177792681f / cap;
+        sloped = slopes;
         slope = slope_nats * 1.44269504088896341f;
         position = at;
     }
-
-    // x: a scaled score (log2 units) of token j
-    __device__ __forceinline__ float operator()(float x, int j) const {
+    // N scores of one row, which times `by` are in log2 units: number i is token `token` +
+    // place(i).  Capped ones are cap * tanh(u): cap (1 - 2 / (exp(2u) + 1)), whose ends,
+    // exponentials of 0 and infinity, give -1 and 1, known to 2^-22 of the cap.  That is
+    // enough of caps in use; under large ones small u take the power series (|u| < 1/4: up to
+    // u^9, off by less than 2^-26 of it).
+    template <int N, typename V, typename Place>
+    __device__ __forceinline__ void apply(V &s, float by, int token, Place place) const {
         if (cap > 0.0f) {
-            // cap * tanh(u): 1 - 2 / (exp(2u) + 1), whose ends, exponentials of 0 and
-            // infinity, give -1 and 1, known to 2^-22 of the cap.  That is enough of caps
-            // in use; under large ones small u take the power series (|u| < 1/4: up to
-            // u^9, off by less than 2^-26 of it)
-            const float e = __builtin_amdgcn_exp2f(x * twice);
-            const float far = __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
-            if (cap > 256.0f) {
-                const float u = x * inverse, z = u * u;
-                float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
-                t = __builtin_fmaf(z, t, 2.0f / 15);
-                t = __builtin_fmaf(z, t, -1.0f / 3);
-                t = __builtin_fmaf(z * t, x, x);
-                x = z < 0.0625f ? t : far;
+            const float inverse = by / cap, twice = inverse * 2.88539008177792681f;
+            const auto far = [&](float x) {
+                const float e = __builtin_amdgcn_exp2f(x * twice);
+                return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
+            };
+            if (cap <= 256.0f) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[i] = far(s[i]);
             } else {
-                x = far;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float x = s[i] * by, u = s[i] * inverse, z = u * u;
+                    float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
+                    t = __builtin_fmaf(z, t, 2.0f / 15);
+                    t = __builtin_fmaf(z, t, -1.0f / 3);
+                    t = __builtin_fmaf(z * t, x, x);
+                    s[i] = z < 0.0625f ? t : far(s[i]);
+                }
             }
+            by = 1.0f;
         }
-        return __builtin_fmaf(-slope, __builtin_fabsf((float)(position - j)), x);
+        if (sloped) {
+            // (of positions past 2^24 the distance is off by a last place, as it would be
+            // rounded to float32 itself)
+            const float from = (float)(position - token);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                s[i] = __builtin_fmaf(-slope, __builtin_fabsf(from - (float)place(i)), s[i] * by);
+        }
     }
 };
 

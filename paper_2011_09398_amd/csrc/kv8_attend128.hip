@@ -10,8 +10,8 @@ constexpr int kWaveRows = 32;
 constexpr int kRows = kWaves * kWaveRows;
 static_assert(kWaves == kBlocks, "a wave makes one block of the values into two-byte floats");
 
-// One wave's block of a page's keys as they come from memory: lane (r, f), r = lane % 16,
-// f = lane / 16, holds of token r channels 64c + 16f .. +15.
+// One wave's block of a page's keys as they come from memory: lane (r, f) holds of token
+// r channels 64c + 16f .. +15.
 template <int D>
 struct Keys {
     u32x4 k[D / 64];
@@ -24,8 +24,7 @@ struct Keys {
     }
 };
 
-// One wave's block of a page's values: lane (r, g), r = lane % 16, g = lane / 16, holds
-// tokens 4g .. 4g + 3 of channels 64c + 4r .. +3, a word for each channel.
+// One wave's block of a page's values: lane (r, g) holds tokens 4g .. 4g + 3 of channels 64c + 4r .. +3, a word for each channel.
 template <int D>
 struct Values {
     u32x4 v[D / 64];
@@ -116,16 +115,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % p.kv_heads, split = blockIdx.y;
-    // the last tiles of a sequence see the most: they start first
-    const int slot = (int)gridDim.x / p.kv_heads - 1 - (int)blockIdx.x / p.kv_heads;
+    const int slot = (int)blockIdx.x / p.kv_heads;
 
     const auto first = [&](int s, int b) { return (int64_t)s * p.group / kRows + b; };
     const Sequence seq =
         find_sequence(p.q_start, p.lengths, p.seqs, p.tokens, p.width, slot, first);
     if (seq.index < 0) return;
     const int rows = seq.queries * p.group;
-    const int row0 = (int)(slot - first(seq.start, seq.index)) * kRows;
-    if (row0 >= rows) return;
+    // the last tiles of a sequence see the most: they start first
+    const int tile = (rows + kRows - 1) / kRows - 1 - (int)(slot - first(seq.start, seq.index));
+    if (tile < 0) return;
+    const int row0 = tile * kRows;
     const int valid = min(rows - row0, kRows);
     const int row = row0 + kWaveRows * wave + n;
     const bool mine = row < rows;
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
            mine, h);
     Change change;
     if constexpr (CHANGE)
-        change.set(p.cap_log2, p.slopes && mine ? p.slopes[hq] : 0.0f,
+        change.set(p.cap_log2, p.slopes != nullptr, p.slopes && mine ? p.slopes[hq] : 0.0f,
                    seq.length - seq.queries + i);
 
     // the state of a row: running maximum (log2), this lane's share of the sum, sums of
@@ -181,8 +181,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         number = __builtin_amdgcn_readlane(page, at);
         return cache + (int64_t)__builtin_amdgcn_readlane(phys, at) * stride;
     };
-    // (of a wave's first half both runs of 8 bytes, which are all banks between them)
-    const int r = lane & 15, g = (lane >> 4 & 1) * 2 + (lane >> 5);
+    // the lane's token of a block of keys and its channels; its channels of a block of values
+    // and their tokens (neighbouring lanes write the two halves of 16 bytes)
+    const int kr = lane & 15, kq = lane >> 4, r = lane >> 1 & 15, g = (lane & 1) * 2 + (lane >> 5);
     Keys<D> keys;
     Values<D> values;
     // of the page whose keys the registers hold, and of the one before it, whose values they do
@@ -235,9 +236,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     const auto judge = [&](int t, int of, float by, bool there) {
         const int t0 = of * kPage + 32 * t;
         if constexpr (CHANGE) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-                s[t][k] = change(s[t][k] * by, t0 + 8 * (k / 4) + 4 * h + k % 4);
+            change.template apply<16>(s[t], by, t0 + 4 * h,
+                                      [](int k) { return 8 * (k / 4) + k % 4; });
             by = 1.0f;
         }
         if (!there || t0 < wz.lo || t0 + 32 > wa.hi) {
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
             }
             next = E::mfma32(k[j % 3], q.q[j], next);
             if (t == 0 && j % 4 == 1)
-                ours.template store_keys<E>(keys, kf, wave, r, lane >> 4, j / 4);
+                ours.template store_keys<E>(keys, kf, wave, kr, kq, j / 4);
             if (t == 1) other.template store_values<E>(values, vf, wave, r, g, j / 4, j % 4);
             o[j % kWidth] = E::mfma32(v[j % 3], w[2 * t + j / kWidth], o[j % kWidth]);
 #pragma unroll
@@ -341,11 +341,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     const auto load_keys = [&](const uint8_t *from) {
         value_scales = scales[1];
         scales = *reinterpret_cast<const u32x2 *>(from + Record<D>::kScale);
-        keys.load(from, wave, r, lane >> 4);
+        keys.load(from, wave, kr, kq);
     };
     const auto store_keys = [&](Page<D> &page) {
 #pragma unroll
-        for (int x = 0; x < D / 64; ++x) page.template store_keys<E>(keys, kf, wave, r, lane >> 4, x);
+        for (int x = 0; x < D / 64; ++x) page.template store_keys<E>(keys, kf, wave, kr, kq, x);
     };
     pull(0);
     const bool any = number[0] >= 0;

@@ -18,32 +18,44 @@ __device__ __forceinline__ V fetch(const uint8_t *p) {
 }
 
 // What a wave takes at a time: a page, or half of one where heads are so wide that the
-// codes of a whole one would leave no registers for what else there is.
+// codes of a whole one would leave too few registers for what else there is (heads of 128:
+// 67 us against 87 of the case below, when keys did not come through LDS yet).
 template <int D>
 struct Step {
-    static constexpr int kTiles = D <= 128 ? 4 : 2;        // of 16 tokens
+    static constexpr int kTiles = D <= 64 ? 4 : 2;         // of 16 tokens
     static constexpr int kPerPage = 4 / kTiles;
     static constexpr int kTokens = 16 * kTiles;
     static constexpr int kChunks = D / 64;
 };
 
-// Key codes as a wave's lanes hold them.  Lane (n, g), n = lane % 16, g = lane / 16: of
-// tokens 16t + n the channels 64c + 16g .. +15, which are the first operands of two
-// products of 32 channels (the order of channels does not matter, as long as the queries
-// are in the same).
+// Key codes of a step as they come from memory, whole lines of it: 16 bytes a lane at a
+// time, pieces lane, lane + 64 .. of the step's.  The wave's own part of LDS turns them into
+// first operands: lane (n, g), n = lane % 16, g = lane / 16, wants piece 4c + g, 16 channels
+// for two products, of tokens 16t + n (loads in that order are sixteen pieces of lines each,
+// 67 against 59 us).  A token's pieces change places with its number, or they would meet in
+// a bank.
 template <int D>
 struct Keys {
-    u32x4 k[Step<D>::kTiles][Step<D>::kChunks];
+    static constexpr int kPieces = D / 16, kLoads = Step<D>::kTiles * D / 64;
+    u32x4 k[kLoads];
 
     template <bool ONCE>
-    __device__ __forceinline__ void load(const uint8_t *rec, int half, int n, int g) {
+    __device__ __forceinline__ void load(const uint8_t *rec, int half, int lane) {
 #pragma unroll
-        for (int t = 0; t < Step<D>::kTiles; ++t)
+        for (int i = 0; i < kLoads; ++i)
+            k[i] = fetch<ONCE, u32x4>(rec + Record<D>::kKey + half * Step<D>::kTokens * D +
+                                      1024 * i + 16 * lane);
+    }
+    static __device__ __forceinline__ int place(int token, int piece) {
+        constexpr int kApart = kPieces < 8 ? 4 : 1;
+        return token * kPieces + (piece ^ (token / kApart % kPieces));
+    }
+    __device__ __forceinline__ void store(u32x4 *to, int lane) const {
 #pragma unroll
-            for (int c = 0; c < Step<D>::kChunks; ++c)
-                k[t][c] = fetch<ONCE, u32x4>(rec + Record<D>::kKey +
-                                             (half * Step<D>::kTokens + 16 * t + n) * D + 64 * c +
-                                             16 * g);
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = 64 * i + lane;
+            to[place(at / kPieces, at % kPieces)] = k[i];
+        }
     }
 };
 
@@ -101,12 +113,14 @@ struct RowState {
     f32x4 o[D / 16];
 };
 
+// The waves' states, where they are joined; before that, each wave's part holds its keys.
 template <int D, int C>
 struct Shared {
     f32x4 o[kWaves][D / 4][16 * C];
     f32x2 ml[kWaves][16 * C];
     int scale[kWaves];
     int last;
+    static_assert(sizeof(o[0]) >= Step<D>::kTokens * D, "a step's keys");
 };
 
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
@@ -236,7 +250,8 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
                       (int64_t)hq[c] * p.q_head,
                   mine[c], g);
         if constexpr (CHANGE) {
-            change[c].set(p.cap_log2, p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
+            change[c].set(p.cap_log2, p.slopes != nullptr,
+                          p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
                           seq.length - seq.queries + i[c]);
         }
     }
@@ -265,7 +280,9 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     };
 
     // Keys and values of one step are in registers at a time: the next one's keys are on
-    // their way once this one's weights are there, its values once this one's are added.
+    // their way once this one's scores are there, its values once this one's are added.
+    // (Two steps at a time, with less to hide them behind: 59 us as well.)
+    u32x4 *const pieces = reinterpret_cast<u32x4 *>(&sh.o[wave][0][0]);
     look();
     Keys<D> keys;
     Values<D> values;
@@ -275,20 +292,24 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
     if (more) {
         const uint8_t *rec = next(step);
         scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
-        keys.template load<ONCE>(rec, step % S::kPerPage, n, g);
+        keys.template load<ONCE>(rec, step % S::kPerPage, lane);
         values.template load<ONCE>(rec, step % S::kPerPage, n, g);
     }
     while (more) {
         const int t0 = step * S::kTokens;
+        // whether some row does not see all of the step
         const bool masked = t0 < z.lo || t0 + S::kTokens > a.hi;
-        // scales of the page's blocks, then of the step's
-        const int from_block = step % S::kPerPage * S::kTiles;
-        uint32_t ks = __builtin_amdgcn_readfirstlane(scales[0]) >> (8 * from_block);
-        uint32_t vs = __builtin_amdgcn_readfirstlane(scales[1]) >> (8 * from_block);
-        // (of half a page, the other half's bytes are moved out: tokens from kTokens on)
-        ks = settled_scales(ks, a.lo - t0, min(z.hi - t0, S::kTokens));
-        vs = settled_scales(vs, a.lo - t0, min(z.hi - t0, S::kTokens));
+        // scales of the step's blocks (the bytes behind them are the page's others, or 0)
+        const int before = step % S::kPerPage * 8 * S::kTiles;
+        uint32_t ks = in_scalar(scales[0]) >> before, vs = in_scalar(scales[1]) >> before;
+        if constexpr (S::kTiles < 4) ks &= 0xFFFFu, vs &= 0xFFFFu;
+        if (masked) {
+            const int lo = a.lo - t0, hi = min(z.hi - t0, S::kTokens);
+            ks = settled_scales(ks, lo, hi);
+            vs = settled_scales(vs, lo, hi);
+        }
         const int km = largest_of(ks), vm = largest_of(vs);
+        keys.store(pieces, lane);
         f32x4 s[C][S::kTiles];
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t) {
@@ -296,29 +317,33 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
 #pragma unroll
             for (int c = 0; c < C; ++c) s[c][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int h = 0; h < S::kChunks; ++h)
+            for (int h = 0; h < S::kChunks; ++h) {
+                const u32x4 codes = pieces[Keys<D>::place(16 * t + n, 4 * h + g)];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const u32x4 k =
-                        decode_eight<E>(keys.k[t][h][2 * x], keys.k[t][h][2 * x + 1], f, f);
+                    const u32x4 k = decode_eight<E>(codes[2 * x], codes[2 * x + 1], f, f);
 #pragma unroll
                     for (int c = 0; c < C; ++c) s[c][t] = E::mfma16(k, q[c].q[h][x], s[c][t]);
                 }
+            }
         }
         look();
         more = todo != 0;
         const uint8_t *rec = nullptr;
         int following = 0;
-        if (more) rec = next(following);
+        if (more) {
+            rec = next(following);
+            scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
+            keys.template load<ONCE>(rec, following % S::kPerPage, lane);
+        }
         float scale = __builtin_amdgcn_ldexpf(p.scale_log2, km - 127 - kUp<E>);
         if constexpr (CHANGE) {
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int t = 0; t < S::kTiles; ++t)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        s[c][t][k] = change[c](s[c][t][k] * scale, t0 + 16 * t + 4 * g + k);
+                    change[c].template apply<4>(s[c][t], scale, t0 + 16 * t + 4 * g,
+                                                [](int k) { return k; });
             scale = 1.0f;
         }
         if (masked) {
@@ -338,10 +363,6 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
         for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], scale);
-        if (more) {
-            scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
-            keys.template load<ONCE>(rec, following % S::kPerPage, n, g);
-        }
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
