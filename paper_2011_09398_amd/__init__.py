@@ -38,6 +38,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence, Tuple, Union
 
 from . import build as _build
@@ -198,12 +199,12 @@ def lib() -> ctypes.CDLL:
                                      vp, vp]
         L.lce_kv8_read.argtypes = [cd, vp, vp, i64, i32, vp, vp, vp]
         L.lce_kv8_workspace_size.argtypes = [cd, qd, ctypes.POINTER(i64)]
-        L.lce_kv8_attention.argtypes = [cd, vp, qd, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
-        dp, rows = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(RotaryRows)
+        L.lce_kv8_attention.argtypes = [cd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        dp = ctypes.POINTER(ctypes.c_double)
         L.lce_rotary_frequencies.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double,
                                              ctypes.c_double, dp, ctypes.POINTER(ctypes.c_float)]
         L.lce_rotary_turns.argtypes = [dp, i32, ctypes.POINTER(ctypes.c_uint64)]
-        L.lce_rotary.argtypes = [ctypes.POINTER(RotaryDesc), vp, vp, rows, rows, vp]
+        L.lce_rotary.argtypes = [vp, vp, vp, vp, vp, vp]
         for name in ("kv8_cache_size", "kv8_append", "kv8_read", "kv8_workspace_size",
                      "kv8_attention", "rotary_frequencies", "rotary_turns", "rotary"):
             getattr(L, "lce_" + name).restype = ctypes.c_int
@@ -818,13 +819,20 @@ class _PagedCache:
         return (t.dtype is dtype and t.get_device() == self._index and t.is_contiguous())
 
 
+_current_device = None
+
+
 def _launch(index, fn, *args) -> None:
     """Calls the library with device `index` current: a default stream is its device's by
     that alone."""
-    import torch
-    if torch.cuda.current_device() == index:
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = lambda: torch.cuda.current_device()
+    if _current_device() == index:
         st = fn(*args)
     else:
+        import torch
         with torch.cuda.device(index):
             st = fn(*args)
     if st != LCE_OK:
@@ -1125,6 +1133,11 @@ def kv4_select(cache: KV4Cache, q, table, q_start, lengths, count: int, *, keep_
 KV8_PAGE = 64
 KV8_BLOCK = 16
 KV8_WORKSPACE_ZERO = 131072
+# lce_kv8_query_desc, lce_rotary_desc and lce_rotary_rows as bytes: packing them takes a
+# third of the time that filling the ctypes structures does.
+_pack_kv8_query = struct.Struct("@9i2f2q").pack
+_pack_rotary = struct.Struct("@6if").pack
+_pack_rotary_rows = struct.Struct("@i2P4q").pack
 
 
 def _require_sequences(cache, table, q_start, lengths):
@@ -1292,8 +1305,12 @@ def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optiona
     if (tokens | heads | seqs | width | window | max_q | max_len) >> 31:
         _int32_refused(tokens=tokens, heads=heads, sequences=seqs, table=width, window=window,
                        max_q=max_q, max_len=max_len)
-    d = KV8QueryDesc(tokens, heads, seqs, width, code, 1 if causal else 0, window, max_q, max_len,
-                     cache._scale if scale is None else scale, softcap, strides[0], strides[1])
+    try:
+        d = _pack_kv8_query(tokens, heads, seqs, width, code, 1 if causal else 0, window, max_q,
+                            max_len, cache._scale if scale is None else scale, softcap, strides[0],
+                            strides[1])
+    except OverflowError:
+        raise ValueError(f"scale {scale} or softcap {softcap} is past float32's range") from None
     if out is None:
         out = cache._empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
     else:
@@ -1306,8 +1323,8 @@ def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optiona
         workspace = kv8_workspace(cache, q, table)
     elif not cache._holds(workspace, cache._uint8):
         _require_like(workspace, cache._uint8, cache.data.device, "workspace")
-    _launch(cache._index, lib().lce_kv8_attention, cache._ref, cache._data.data_ptr(),
-            ctypes.byref(d), q.data_ptr(), table.data_ptr(), q_start.data_ptr(),
+    _launch(cache._index, lib().lce_kv8_attention, cache._ref, cache._data.data_ptr(), d,
+            q.data_ptr(), table.data_ptr(), q_start.data_ptr(),
             lengths.data_ptr(), None if slopes is None else slopes.data_ptr(),
             None if prefix is None else prefix.data_ptr(), out.data_ptr(),
             None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
@@ -1363,24 +1380,48 @@ class Rotary:
         self._turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns],
                                    dtype=torch.int64).to(device)
         self._index = self._turns.get_device()
+        # what every call compares its tensors with
+        self._int64, self._empty_like = torch.int64, torch.empty_like
+        self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
-def _rotary_rows(plan, t, out, name, n, dtype):
-    """Checks one tensor of a rotary call; its rows."""
+def _rotary_refused(plan, positions, q, k):
+    """Raises for what rotary does not take."""
     import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.get_device() != plan._index:
-        raise ValueError(f"{name} must be on {plan._turns.device}, got {t.device}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or t.shape[0] != n or t.shape[2] != plan.head_dim:
-        raise ValueError(f"{name} must be [{n}, heads, {plan.head_dim}], got {list(t.shape)}")
-    if t.stride(2) != 1 and t.numel():
-        raise ValueError(f"{name}'s channels must be contiguous")
-    _int32_refused(heads=t.shape[1])
-    x, y = t.stride(), out.stride()
-    return RotaryRows(t.shape[1], t.data_ptr(), out.data_ptr(), x[0], x[1], y[0], y[1])
+    if not isinstance(plan, Rotary):
+        raise TypeError("plan must be a Rotary")
+    device = plan._turns.device
+    for t, name in ((q, "q"), (k, "k")):
+        if t is None and name == "k":
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if t.device != device:
+            raise ValueError(f"{name} must be on {device}, got {t.device}")
+        _float_type(t.dtype, name)
+        if t.dtype != q.dtype:
+            raise TypeError(f"q and k must have one dtype, got {q.dtype} and {t.dtype}")
+        if t.dim() != 3 or t.shape[0] != q.shape[0] or t.shape[2] != plan.head_dim:
+            raise ValueError(f"{name} must be [{q.shape[0]}, heads, {plan.head_dim}], got "
+                             f"{list(t.shape)}")
+        if t.stride(2) != 1 and t.numel():
+            raise ValueError(f"{name}'s channels must be contiguous")
+    _require_like(positions, torch.int64, device, "positions")
+    if positions.shape != q.shape[:1]:
+        raise ValueError(f"positions must have {q.shape[0]} elements, got {list(positions.shape)}")
+
+
+def _rotary_out(t, out, name):
+    """Checks a tensor that rotary writes t's result to."""
+    import torch
+    if not isinstance(out, torch.Tensor):
+        raise TypeError(f"out of {name} must be a torch.Tensor")
+    if (out.shape, out.dtype, out.device) != (t.shape, t.dtype, t.device):
+        raise ValueError(f"out of {name} must be like it: {list(t.shape)} {t.dtype} on {t.device}, "
+                         f"got {list(out.shape)} {out.dtype} on {out.device}")
+    if out.stride(2) != 1 and out.numel():
+        raise ValueError(f"out of {name}: channels must be contiguous")
+    return out
 
 
 def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=None):
@@ -1389,43 +1430,52 @@ def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=No
     bfloat16, any token and head strides.  backward: q and k are gradients of what was
     turned, and get turned back (and scaled) to those of what went in.  Returns new
     tensors, or writes `out` (q's, or a pair), which may be q and k themselves."""
-    import torch
-    if not isinstance(plan, Rotary):
-        raise TypeError("plan must be a Rotary")
-    if not isinstance(q, torch.Tensor):
-        raise TypeError("q must be a torch.Tensor")
-    code = _float_type(q.dtype, "q")
-    if q.dim() != 3:
-        raise ValueError(f"q must be [tokens, heads, {plan.head_dim}], got {list(q.shape)}")
-    n = q.shape[0]
-    _int32_refused(tokens=n)
-    _require_like(positions, torch.int64, plan._turns.device, "positions")
-    if positions.shape != (n,):
-        raise ValueError(f"positions must have {n} elements, got {list(positions.shape)}")
-    ins = (q,) if k is None else (q, k)
+    try:
+        n, heads, dim = q.shape
+        x = q.stride()
+        code = plan._types.get(q.dtype, -1)
+        fine = (type(plan) is Rotary and code >= 0 and dim == plan.head_dim and x[2] == 1
+                and q.get_device() == positions.get_device() == plan._index
+                and positions.dtype is plan._int64 and positions.shape == (n,)
+                and positions.is_contiguous())
+        if k is not None:
+            shape, y = k.shape, k.stride()
+            fine = (fine and len(shape) == 3 and shape[0] == n and shape[2] == dim and y[2] == 1
+                    and k.dtype is q.dtype and k.get_device() == plan._index)
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _rotary_refused(plan, positions, q, k)
+        n, heads, dim, x, code = *q.shape, q.stride(), _float_type(q.dtype, "q")
+        if k is not None:
+            shape, y = k.shape, k.stride()
+    if (n | heads) >> 31 or k is not None and shape[1] >> 31:
+        _int32_refused(tokens=n, heads=heads if k is None else max(heads, shape[1]))
     if out is None:
-        outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device)
-                     if isinstance(t, torch.Tensor) else t for t in ins)
+        outs = tuple(_empty_rows(plan, t) for t in ((q,) if k is None else (q, k)))
+    elif k is None:
+        outs = (_rotary_out(q, out, "q"),)
     else:
-        outs = (out,) if k is None else tuple(out)
-        if len(outs) != len(ins):
-            raise ValueError(f"out must be {len(ins)} tensors")
-        for t, o, name in zip(ins, outs, ("q", "k")):
-            if not isinstance(o, torch.Tensor):
-                raise TypeError(f"out of {name} must be a torch.Tensor")
-            if (o.shape, o.dtype, o.device) != (t.shape, t.dtype, t.device):
-                raise ValueError(f"out of {name} must be like it: {list(t.shape)} {t.dtype} on "
-                                 f"{t.device}, got {list(o.shape)} {o.dtype} on {o.device}")
-            if o.stride(2) != 1 and o.numel():
-                raise ValueError(f"out of {name}: channels must be contiguous")
-    rows = [_rotary_rows(plan, t, o, name, n, q.dtype)
-            for t, o, name in zip(ins, outs, ("q", "k"))]
-    d = RotaryDesc(n, plan.head_dim, plan.rot_dim, code, 1 if plan.interleaved else 0,
-                   1 if backward else 0, plan.scale)
-    _launch(plan._index, lib().lce_rotary, ctypes.byref(d), plan._turns.data_ptr(),
-            positions.data_ptr(), ctypes.byref(rows[0]),
-            ctypes.byref(rows[1]) if k is not None else None, _stream_handle(q))
+        if len(out) != 2:
+            raise ValueError("out must be a pair of tensors")
+        outs = (_rotary_out(q, out[0], "q"), _rotary_out(k, out[1], "k"))
+    to = outs[0].stride()
+    qr = _pack_rotary_rows(heads, q.data_ptr(), outs[0].data_ptr(), x[0], x[1], to[0], to[1])
+    kr = None
+    if k is not None:
+        to = outs[1].stride()
+        kr = _pack_rotary_rows(shape[1], k.data_ptr(), outs[1].data_ptr(), y[0], y[1], to[0], to[1])
+    _launch(plan._index, lib().lce_rotary,
+            _pack_rotary(n, dim, plan.rot_dim, code, 1 if plan.interleaved else 0,
+                         1 if backward else 0, plan.scale),
+            plan._turns.data_ptr(), positions.data_ptr(), qr, kr, _stream_handle(q))
     return outs[0] if k is None else outs
+
+
+def _empty_rows(plan, t):
+    """A tensor like t with contiguous channels."""
+    out = plan._empty_like(t)
+    return out if out.stride(2) == 1 else t.new_empty(t.shape)
 
 
 class PreparedBitpack:
