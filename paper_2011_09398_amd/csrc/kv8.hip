@@ -16,6 +16,7 @@ using lce::tuning;
 using lce::kv8::kBlock;
 using lce::kv8::kPage;
 
+constexpr double kCus = 256;
 // Workgroups of 256 threads in a grid: threads are counted in 32 bits.
 constexpr int64_t kMostGroups = (1LL << 24) - 1;
 
@@ -135,28 +136,33 @@ struct Split {
     int splits;   // workgroups that share a tile, at most
 };
 
-// `pages` pages of each of `likely` tiles (the grid has room for `units`), `step`
-// microseconds for a wave to take one: how many workgroups (of four waves) share a tile.
-// Sharing costs about `fixed` microseconds for the partial states, the ticket and the
-// joining, and 0.11 for each state joined, so a tile is divided only where its pages take
-// longer, and no further than `most` workgroups in all and `parts` states in the
-// workspace.  `each`: the number of pages that a workgroup takes is a multiple of it, so
-// that all waves are busy to the end.
-// Windows span `usual` pages, one or two less than they can.
-Split split_pages(int64_t units, int64_t likely, int64_t pages, int64_t usual, double step,
-                  double fixed, int64_t most, int64_t parts, int64_t each) {
-    const int64_t some = std::max<int64_t>(likely, 1);
+// What a tile's pages cost and what sharing it does, in microseconds: `step` for a wave to
+// take a page, `fixed` for the partial states, the ticket and the joining, and `each` for
+// every state joined, which one workgroup reads.
+struct Cost {
+    double step, fixed, each;
+};
+
+// `pages` pages of each of `likely` tiles (the grid has room for `units`): how many
+// workgroups (of four waves) share a tile.  It is divided only where its pages take longer,
+// and no further than `most` workgroups in all and `parts` states in the workspace; the
+// number of pages that a workgroup takes is a multiple of `whole`, so that all waves are
+// busy to the end.  Windows span `usual` pages, one or two less than they can.
+Split split_pages(int64_t units, int64_t likely, int64_t pages, int64_t usual, const Cost &c,
+                  int64_t most, int64_t parts, int64_t whole) {
+    const double some = (double)std::max<int64_t>(likely, 1);
     const int64_t room = most_splits(units, parts);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV8_CHUNK)) {
         chunk = std::max(std::clamp<int64_t>(t, 1, chunk), (pages + room - 1) / room);
     } else {
-        const double whole = usual * step / 4;
-        // the least of whole / z + fixed + 0.11 z
-        const double z = std::min(std::min((double)room, (double)most / some),
-                                  std::sqrt(whole / 0.11));
-        if (z > 1 && whole / z + fixed + 0.11 * z < whole)
-            chunk = ((int64_t)std::ceil(usual / z) + each - 1) / each * each;
+        const double alone = usual * c.step / 4;
+        // the least of alone / z + fixed + each * z
+        double z = std::min(std::min((double)room, (double)most / some), std::sqrt(alone / c.each));
+        // (one workgroup a CU, rather than two on some)
+        if (z * some > kCus && z * some < 2 * kCus) z = std::max(kCus / some, 1.0);
+        if (z > 1 && alone / z + c.fixed + c.each * z < alone)
+            chunk = ((int64_t)std::ceil(usual / z) + whole - 1) / whole * whole;
     }
     Split s;
     s.chunk = (int)chunk;
@@ -280,17 +286,16 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     const int64_t likely = (int64_t)std::min((double)units, spread * ((each + rows - 1) / rows));
     const int64_t usual =
         most < most_pages(*query, true) ? std::max<int64_t>(most - 2, 1) : most;
-    const Split s =
-        rows == 128
-            ? split_pages(units, likely, most, usual, 2 + 2 * size, 4 + 8 * size, 512,
-                          kMostParts / 8, 1)
-            : split_pages(units, likely, most, usual, 0.5 + 0.6 * size,
-                          (0.5 + 1.3 * size) * (several ? 2.5 : 1.0),
-                          query->window    ? slots
-                          : several        ? 512
-                          : likely < slots ? 4 * slots
-                                           : 7 * slots / 4,
-                          kMostParts * 16 / rows, 4);
+    const double state = std::min<int64_t>(each, rows) * desc->head_dim * 4e-3;   // kB
+    const Cost cost = rows == 128 ? Cost{2 + 2 * size, 4 + 8 * size, 0.06}
+                                  : Cost{0.3 + size, (1.2 + state * 0.19) * (several ? 2.0 : 1.0),
+                                         0.05 + state / 45};
+    const int64_t limit = rows == 128 || several ? 512
+                          : query->window        ? slots
+                          : likely < slots       ? 4 * slots
+                                                 : 7 * slots / 4;
+    const Split s = split_pages(units, likely, most, usual, cost, limit, kMostParts * 16 / rows,
+                                rows == 128 ? 1 : 4);
     const bool once = each <= 16 && 128.0 * desc->head_dim * most * likely >= (240 << 20);
     lce::kv8::AttendParams p;
     p.cache = static_cast<const uint8_t *>(cache);
