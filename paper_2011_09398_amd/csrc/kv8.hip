@@ -101,13 +101,34 @@ int64_t query_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
     return (int64_t)(q.max_q > 0 ? q.max_q : q.tokens / q.seqs) * (q.q_heads / d.kv_heads);
 }
 
-int tile_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q, bool prefix) {
+// Query rows of a tile.  In tiles of 128 rows a page's codes become two-byte floats once
+// for all of them, but the more rows a tile has the fewer tiles there are, and fewer than run
+// at a time (512) leave CUs without work; tiles of 16 and 32 rows share a page between their
+// rows alone, and their waves share the pages.  Heads of 64 channels have half the products
+// for the same softmax, which the smaller tiles' third wave a SIMD does better, until there
+// are many tiles.  Heads of 256 channels stay at 16: 32 rows of them, or 128, have more state
+// than registers.  Measured in graphs (us, tiles of 16 / 32 / 128; 32 heads on 8 if not said
+// otherwise; the last two columns float16):
+//                                          128 channels      64 channels      128, capped
+//   16 of 4064 tokens, 64 of them new      48 / 55 / 99      29 / 38 / 80     57 / 71 / 144
+//   one of 5024, 1024 new                 142 / 111 / 121    81 / 65 / 97    173 / 147 / 173
+//   one of 6048, 2048 new                 279 / 222 / 183   162 / 123 / 129  353 / 311 / 252
+//   one of 8096, 4096 new                 640 / 512 / 413   366 / 277 / 286  814 / 720 / 563
+//   four of up to 4512, up to 512 new      86 / 75 / 111     52 / 41 / 89    106 / 97 / 161
+//   four of up to 5024, up to 1024 new    166 / 137 / 126   101 / 76 / 100   207 / 185 / 178
+//   four of up to 6048, up to 2048 new    330 / 272 / 206   197 / 149 / 145  410 / 369 / 284
+//   16 of up to 1024, up to 128 new        34 / 34 / 33      25 / 22 / 26     40 / 41 / 47
+//   one prompt of 1024                     29 / 28 / 31      21 / 20 / 25     35 / 34 / 45
+//   one prompt of 2048                     81 / 71 / 61      50 / 40 / 47     98 / 89 / 86
+//   two of up to 5025, 359 new, 8 on 2     30 / 31 / 60      18 / 20 / 40     36 / 39 / 71
+//   four prompts of up to 1943, 2 on 1     19 / 23 / 49      12 / 16 / 31     23 / 30 / 54
+//   three prompts of up to 2500, 16 on 2   66 / 62 / 67      45 / 37 / 54     83 / 78 / 96
+int tile_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
     if (d.head_dim > 128) return 16;
     const int forced = tuning(LCE_TUNE_KV8_ROWS);
     if (forced == 16 || forced == 32 || forced == 128) return forced;
     const int64_t most = query_rows(d, q), all = (int64_t)q.tokens * q.q_heads;
-    const bool brief = most_pages(q, prefix) <= 16;
-    if (most >= 128 && all >= 128 * (brief ? 256 : 512)) return 128;
+    if (most >= 128 && all >= 128 * (d.head_dim == 64 ? 2048 : 512)) return 128;
     return most >= 256 && all >= 32 * 1024 ? 32 : 16;
 }
 
@@ -273,7 +294,7 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
         return fail(LCE_EINVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
                     (long long)need);
 
-    const int rows = tile_rows(*desc, *query, prefix != nullptr);
+    const int rows = tile_rows(*desc, *query);
     const int64_t units = tiles(*desc, *query, rows) * desc->kv_heads;
     const double size = desc->head_dim / 128.0;
     const int64_t slots = desc->head_dim > 128 ? 512 : 768;   // workgroups that run at a time

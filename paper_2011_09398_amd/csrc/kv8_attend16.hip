@@ -186,7 +186,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[Step<D>::kTile
 // the keys against the page's largest, which the scores are multiplied by in float32, of
 // the values against the largest that the wave has seen.
 template <typename E, int D, int C, bool CHANGE, bool ONCE>
-__global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16_kernel(
+__global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) void attend16_kernel(
     AttendParams p) {
     constexpr int kRows = 16 * C;
     typedef Step<D> S;
@@ -210,8 +210,10 @@ __global__ __launch_bounds__(kThreads, D <= 128 && C == 1 ? 3 : 2) void attend16
         find_sequence(p.q_start, p.lengths, p.seqs, p.tokens, p.width, slot, first);
     if (seq.index < 0) return;
     const int rows = seq.queries * p.group;
-    const int row0 = (int)(slot - first(seq.start, seq.index)) * kRows;
-    if (row0 >= rows) return;
+    // the last tiles of a sequence see the most: they start first
+    const int tile = (rows + kRows - 1) / kRows - 1 - (int)(slot - first(seq.start, seq.index));
+    if (tile < 0) return;
+    const int row0 = tile * kRows;
     const int valid = min(rows - row0, kRows);
     const int prefix = p.prefix ? p.prefix[seq.index] : 0;
     // this lane's row of each sixteen
