@@ -564,8 +564,9 @@ lce_status lce_kv8_cache_size(const lce_kv8_cache_desc *desc, int64_t *bytes);
  *   table, q_start, lengths   as for lce_kv8_attention
  * Tokens before a sequence's beginning (n > lengths[b]) and tokens on a page outside
  * the cache are dropped.  Older tokens of a block are those before its first new one;
- * what the block holds behind the last new one becomes 0.  No two sequences may append
- * to one block in a call.  Appending the same tokens again changes nothing.
+ * what a block holds behind the last new one is lost.  No two sequences may append to
+ * one block in a call.  Appending the same tokens again, nothing having been appended
+ * behind them, changes nothing.
  * tokens == 0 is a no-op (pointers may then be NULL).
  * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0), LCE_EUNSUPPORTED
  *         (head_dim, kv_heads > 65535, table_width over 2^24, more blocks than a grid

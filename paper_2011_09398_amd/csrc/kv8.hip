@@ -305,9 +305,25 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     // floating point: max_q is the caller's word)
     const double spread = query->seqs * (double)desc->kv_heads;
     const int64_t likely = (int64_t)std::min((double)units, spread * ((each + rows - 1) / rows));
+    // Where no window makes sequences alike and there are fewer tiles than run at a time, up
+    // to four times as many workgroups as do: sequences are of different lengths, of which
+    // the call knows the longest.  Measured in graphs over three caches (us by pages a
+    // workgroup; one new token and 32 heads on 8 of 128 channels if not said otherwise):
+    //                                         choice    8    12    16    24    32    64   all
+    //   1 of 30011                              18.9  23.0  20.9  18.9  20.4  22.6  34.9   205
+    //   48 of up to 8192                        58.8  58.7  58.8  58.9  59.5  59.3     -  81.7
+    //   16, window 4096, 4 new, 16 on 8 of 256  44.9  51.1  53.4  45.0  49.4  55.9     -  66.7
+    //   24 of up to 4001, 32 on 32 of 64        36.5  43.1  42.5  41.2  39.0  39.8     -  38.8
+    //   27 of up to 3877, 4 new, 4 on 1 of 256  22.6  22.6  25.4  27.2  32.9  38.9  54.9  54.7
+    //   14 of up to 11385, 5, 10 on 2 of 256    37.0  46.0  37.2  36.9  37.6  41.3  56.1   122
+    //   2 of up to 26367, 16 on 4 of 256        25.2  27.4  26.6  25.3  30.2  34.9  58.3   320
+    //   26 of up to 7976, 8 on 2                17.6  17.6  20.2  19.5  23.5  26.1  44.1  76.4
+    //   4 of up to 33362, 64 on 4 of 64         23.8  30.5  23.0  22.6  23.7  23.4  28.5   167
+    //   29 of up to 2315, 128 on 8 of 64        21.8  21.7  20.6  19.0  21.1  24.1  23.6  23.6
     const int64_t usual =
         most < most_pages(*query, true) ? std::max<int64_t>(most - 2, 1) : most;
-    const double state = std::min<int64_t>(each, rows) * desc->head_dim * 4e-3;   // kB
+    // kB of a tile's state: a workgroup writes them at 5, and the last one reads 45 a us
+    const double state = std::min<int64_t>(each, rows) * desc->head_dim * 4e-3;
     const Cost cost = rows == 128 ? Cost{2 + 2 * size, 4 + 8 * size, 0.06}
                                   : Cost{0.3 + size, (1.2 + state * 0.19) * (several ? 2.0 : 1.0),
                                          0.05 + state / 45};
@@ -317,6 +333,9 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
                                                  : 7 * slots / 4;
     const Split s = split_pages(units, likely, most, usual, cost, limit, kMostParts * 16 / rows,
                                 rows == 128 ? 1 : 4);
+    // Loads past the caches where no other tile reads the same pages and the whole is long
+    // (all sequences as long as the longest: calls read half of that or less): 48 of up to
+    // 8192 tokens 59 us against 64 through them.
     const bool once = each <= 16 && 128.0 * desc->head_dim * most * likely >= (240 << 20);
     lce::kv8::AttendParams p;
     p.cache = static_cast<const uint8_t *>(cache);

@@ -24,7 +24,8 @@ struct Keys {
     }
 };
 
-// One wave's block of a page's values: lane (r, g) holds tokens 4g .. 4g + 3 of channels 64c + 4r .. +3, a word for each channel.
+// One wave's block of a page's values: lane (r, g) holds tokens 4g .. 4g + 3 of channels
+// 64c + 4r .. +3, a word for each channel.
 template <int D>
 struct Values {
     u32x4 v[D / 64];
@@ -102,12 +103,22 @@ __device__ __forceinline__ void lds_barrier() {
 }  // namespace
 
 // Grid (tiles * kv_heads, splits), four waves of 32 rows.  Rows are the queries of one
-// sequence times the heads that share the cache head.  Every wave multiplies all keys of a
-// page, made into two-byte floats by itself, by its own queries; the values are made into
-// two-byte floats once a workgroup, a block by each wave.  Both come through LDS (keys from
-// memory in the order of the products are 32 pieces of lines a load).
-// (8-bit products of keys and queries in 8-bit pieces would need no conversion, but sum
-// with fewer bits than float32: scores of 350 are off by 6e-3, against 3e-5.)
+// sequence times the heads that share the cache head.  A page's keys and values are made
+// into two-byte floats once a workgroup, a block by each wave, and read from LDS by all four.
+// (From memory in the order of the products, keys are 32 pieces of lines a load, and with
+// conversions in every wave, 8-bit keys through LDS gained nothing: 590 us of the first
+// case below each, 550 now.  8-bit products of keys and queries in 8-bit pieces would need
+// no conversion, but sum with fewer bits than float32: scores of 350 are off by 6e-3,
+// against 3e-5.)
+//
+// Bound by issue: of a CU's busy cycles the matrix pipe is at work in 0.49 and the vector
+// pipe in 0.59 (counters of the first case).  With two waves a SIMD the sum hardly passes 1:
+// a matrix instruction holds up about six vector ones, measured alone (32x32x16 products
+// with 8, 12 and 16 independent fused multiply-adds each: 21, 28 and 33 ns, 15 without).
+// Measured, bfloat16, 32 heads on 8 of 128 channels: 4096 tokens seeing 8192, 550 us, 999
+// TFLOP/s; 4 sequences of up to 2048 new tokens on up to 16384, causal, 616 us, 998 TFLOP/s
+// of visible pairs (a large library product: 1170 to 1390); of up to 1700 on up to 6500, of
+// which one has 85 % of the work, 192 us, 930 TFLOP/s.
 template <typename E, int D, bool CHANGE>
 __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) {
     __shared__ Page<D> pages[2];

@@ -108,7 +108,9 @@ __device__ __forceinline__ void store_words(uint8_t *p, const uint32_t (&w)[N]) 
 // whole words of four tokens.  The new tokens' largest absolute value gives the scale, or
 // the scale that the block's older tokens have, where that is larger; where it is smaller,
 // their codes are rounded again.
-// Bound by memory: reads 2*D elements a token and head, writes 2*D bytes.
+// Bound by memory: reads 2*D elements a token and head, writes 2*D bytes.  Measured, 8
+// heads of 128: 10900 new tokens of 7 sequences, float16 (67 MB) 16 us, of which the loads
+// in a row (lengths, table, tokens) take 4; one token of each of 32 sequences 5 us.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendParams p) {
     constexpr int N = D / 16, W = N / 4;
@@ -262,8 +264,10 @@ __device__ __forceinline__ void unpack8(float (&x)[8], uint32_t lo, uint32_t hi,
 
 }  // namespace
 
-// One thread per eight channels of a token; U tokens a thread.  Bound by memory, mostly
-// its writes.
+// One thread per eight channels of a token; U tokens a thread.  Of the values, which
+// interleave four tokens, it reads the words of all four and takes a byte of each: the
+// tokens beside it find them in the cache.  Bound by memory, mostly its writes.  Measured, 8
+// heads of 128: 40000 tokens to bfloat16 (246 MB) 37 us, 6.7 TB/s; 10900 to float16 12 us.
 template <typename T, int D, int U, bool LONG>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadParams p) {
     constexpr int L = D / 8, N = kThreads / L;
@@ -313,6 +317,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadParams p) {
 
 namespace {
 
+// Four tokens a thread where that still gives every CU a few workgroups (the loads of the
+// four are in flight together).
 bool four_per_thread(int64_t tokens, int heads, int dim) {
     return tokens * heads * (dim / 8) >= (int64_t)1024 * kThreads * 4;
 }
@@ -329,6 +335,8 @@ void launch_read_d(const ReadParams &p, hipStream_t s) {
         const int64_t per = (int64_t)kThreads / (D / 8) * u;
         return dim3((unsigned)((p.tokens + per - 1) / per * p.kv_heads));
     };
+    // results of more than 100 MB are stored past the caches, which would not hold them for
+    // whoever reads them next (as measured for the 4-bit cache, whose results are the same)
     const int64_t bytes = p.tokens * p.kv_heads * 2 * D * (int64_t)sizeof(T);
     if (bytes > 100 << 20)
         hipLaunchKernelGGL((read_kernel<T, D, 4, true>), grid(4), dim3(kThreads), 0, s, p);

@@ -140,7 +140,10 @@ __device__ __forceinline__ void turn(Span<T, N> &a, Span<T, N> &b, const Angles<
 // A thread takes one unit of a token's heads, every `lanes`-th of them: N pairs of
 // channels whose angles it computes once, or 2N channels behind the turned ones, which
 // are copied.  N = 16 bytes of channels, or 1 where sizes and strides do not allow it.
-// Bound by memory: every channel is read once and written once.
+// Bound by memory: every channel is read once and written once.  Measured: 16001 tokens, 32
+// and 8 heads of 128, bfloat16 (328 MB) 64 us, 5.1 TB/s (a large copy 4.8 to 5.4, by the
+// card); 8190 tokens, 16 and 16 heads of 64, float32, 16 channels turned (134 MB) 25 us; 32
+// tokens 4 us, a launch.
 template <typename T, int N, bool NEXT>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p) {
     const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
