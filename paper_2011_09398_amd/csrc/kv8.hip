@@ -349,6 +349,7 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     p.q_token = query->q_token_stride, p.q_head = query->q_head_stride;
     p.scale_log2 = query->scale * 1.44269504088896341f;
     p.cap_log2 = query->softcap * 1.44269504088896341f;
+    p.cap_inverse = p.cap_log2 > 0.0f ? 1.0f / p.cap_log2 : 0.0f;
     p.pages = desc->pages, p.kv_heads = desc->kv_heads, p.group = query->q_heads / desc->kv_heads;
     p.tokens = query->tokens, p.seqs = query->seqs, p.width = query->table_width;
     p.causal = query->causal, p.window = query->window;

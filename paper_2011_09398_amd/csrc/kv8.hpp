@@ -56,7 +56,7 @@ struct AttendParams {
     float *part;                                         // workspace: partial results
     int64_t q_token, q_head;                             // strides in elements
     float scale_log2;
-    float cap_log2;                                      // of scores, or 0
+    float cap_log2, cap_inverse;                         // of scores, or 0; 1 / cap_log2
     int pages, kv_heads, group;                          // group = q_heads / kv_heads
     int tokens, seqs, width, causal, window;
     int chunk;                                           // pages per workgroup

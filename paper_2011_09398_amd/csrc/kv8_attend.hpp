@@ -71,56 +71,52 @@ __device__ __forceinline__ uint32_t seen_bytes(int first, int lo, int hi) {
     return w;
 }
 
-// What a call does to scores between their product and the softmax.
+// What a call does to scores between their product and the softmax; the same for all lanes.
 struct Change {
-    float cap;             // log2 units, 0: none
-    float slope;           // of this lane's row, log2 units a token
-    int position;          // of this lane's row
+    float cap, inverse;    // log2 units, 0: none; 1 / cap
     bool sloped;
 
-    __device__ __forceinline__ void set(float cap_log2, bool slopes, float slope_nats, int at) {
-        cap = cap_log2;
-        sloped = slopes;
-        slope = slope_nats * 1.44269504088896341f;
+    // Caps scores, which times `by` are in log2 units: each(f) puts f(x) in the place of
+    // every score x.  cap * tanh(u) is computed as
+    // cap (1 - 2 / (exp(2u) + 1)), whose ends, exponentials of 0 and infinity, give -1 and 1,
+    // known to 2^-22 of the cap.  That is enough of caps in use; under large ones small u
+    // take the power series (|u| < 1/4: up to u^9, off by less than 2^-26 of it).
+    template <typename Each>
+    __device__ __forceinline__ void limit(float by, Each each) const {
+        const float u1 = by * inverse, twice = u1 * 2.88539008177792681f;
+        const auto far = [&](float x) {
+            const float e = __builtin_amdgcn_exp2f(x * twice);
+            return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
+        };
+        if (cap <= 256.0f) {
+            each(far);
+        } else {
+            each([&](float x) {
+                const float y = x * by, u = x * u1, z = u * u;
+                float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
+                t = __builtin_fmaf(z, t, 2.0f / 15);
+                t = __builtin_fmaf(z, t, -1.0f / 3);
+                t = __builtin_fmaf(z * t, y, y);
+                return z < 0.0625f ? t : far(x);
+            });
+        }
+    }
+};
+
+// A lane's row, for a bias by distance.
+struct Slope {
+    float slope;           // log2 units a token
+    int position;
+
+    __device__ __forceinline__ void set(float nats, int at) {
+        slope = nats * 1.44269504088896341f;
         position = at;
     }
-    // N scores of one row, which times `by` are in log2 units: number i is token `token` +
-    // place(i).  Capped ones are cap * tanh(u): cap (1 - 2 / (exp(2u) + 1)), whose ends,
-    // exponentials of 0 and infinity, give -1 and 1, known to 2^-22 of the cap.  That is
-    // enough of caps in use; under large ones small u take the power series (|u| < 1/4: up to
-    // u^9, off by less than 2^-26 of it).
-    template <int N, typename V, typename Place>
-    __device__ __forceinline__ void apply(V &s, float by, int token, Place place) const {
-        if (cap > 0.0f) {
-            const float inverse = by / cap, twice = inverse * 2.88539008177792681f;
-            const auto far = [&](float x) {
-                const float e = __builtin_amdgcn_exp2f(x * twice);
-                return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
-            };
-            if (cap <= 256.0f) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) s[i] = far(s[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float x = s[i] * by, u = s[i] * inverse, z = u * u;
-                    float t = __builtin_fmaf(z, 62.0f / 2835, -17.0f / 315);
-                    t = __builtin_fmaf(z, t, 2.0f / 15);
-                    t = __builtin_fmaf(z, t, -1.0f / 3);
-                    t = __builtin_fmaf(z * t, x, x);
-                    s[i] = z < 0.0625f ? t : far(s[i]);
-                }
-            }
-            by = 1.0f;
-        }
-        if (sloped) {
-            // (of positions past 2^24 the distance is off by a last place, as it would be
-            // rounded to float32 itself)
-            const float from = (float)(position - token);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                s[i] = __builtin_fmaf(-slope, __builtin_fabsf(from - (float)place(i)), s[i] * by);
-        }
+    // (Of positions past 2^24 the distance is off by a last place, as it would be rounded to
+    // float32 itself.)
+    __device__ __forceinline__ float from(int token) const { return (float)(position - token); }
+    __device__ __forceinline__ float operator()(float x, float distance) const {
+        return __builtin_fmaf(-slope, __builtin_fabsf(distance), x);
     }
 };
 

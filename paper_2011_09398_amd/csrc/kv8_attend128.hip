@@ -159,10 +159,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     Queries<D> q;
     q.load((const uint16_t *)p.q + (int64_t)(seq.start + i) * p.q_token + (int64_t)hq * p.q_head,
            mine, h);
-    Change change;
+    const Change change = {p.cap_log2, p.cap_inverse, p.slopes != nullptr};
+    Slope slope;
     if constexpr (CHANGE)
-        change.set(p.cap_log2, p.slopes != nullptr, p.slopes && mine ? p.slopes[hq] : 0.0f,
-                   seq.length - seq.queries + i);
+        slope.set(p.slopes && mine ? p.slopes[hq] : 0.0f, seq.length - seq.queries + i);
 
     // the state of a row: running maximum (log2), this lane's share of the sum, sums of
     // weighted values and their scale: o[m][i] is place 32m + 8 (i / 4) + 4h + i % 4
@@ -247,9 +247,19 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     const auto judge = [&](int t, int of, float by, bool there) {
         const int t0 = of * kPage + 32 * t;
         if constexpr (CHANGE) {
-            change.template apply<16>(s[t], by, t0 + 4 * h,
-                                      [](int k) { return 8 * (k / 4) + k % 4; });
-            by = 1.0f;
+            const auto all = [&](auto f) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) s[t][k] = f(s[t][k], 8 * (k / 4) + k % 4);
+            };
+            if (change.cap > 0.0f) {
+                change.limit(by, [&](auto f) { all([&](float x, int) { return f(x); }); });
+                by = 1.0f;
+            }
+            if (change.sloped) {
+                const float far = slope.from(t0 + 4 * h);
+                all([&](float x, int j) { return slope(x * by, far - (float)j); });
+                by = 1.0f;
+            }
         }
         if (!there || t0 < wz.lo || t0 + 32 > wa.hi) {
             const int lo = span.lo - t0 - 4 * h, hi = there ? span.hi - t0 - 4 * h : lo;

@@ -17,16 +17,21 @@ __device__ __forceinline__ V fetch(const uint8_t *p) {
         return *reinterpret_cast<const V *>(p);
 }
 
-// What a wave takes at a time: a page, or half of one where heads are so wide that the
-// codes of a whole one would leave too few registers for what else there is (heads of 128:
-// 67 us against 87 of the case below, when keys did not come through LDS yet).
-template <int D>
+// What a wave takes at a time: T tiles of 16 tokens, a page or half of one.
+template <int D, int T>
 struct Step {
-    static constexpr int kTiles = D <= 64 ? 4 : 2;         // of 16 tokens
+    static constexpr int kTiles = T;
     static constexpr int kPerPage = 4 / kTiles;
     static constexpr int kTokens = 16 * kTiles;
     static constexpr int kChunks = D / 64;
 };
+
+// Half a page where the codes of a whole one would leave too few registers for what else
+// there is: wide heads (of 128: 67 us against 87 of 48 sequences of up to 8192 tokens, when
+// keys did not come through LDS yet), and 32 rows of 64 with scores to change (47 against 50
+// us of the prompts below; without, 41 against 37).
+template <int D, int C, bool CHANGE>
+constexpr int kTilesOf = D <= 64 && !(C == 2 && CHANGE) ? 4 : 2;
 
 // Key codes of a step as they come from memory, whole lines of it: 16 bytes a lane at a
 // time, pieces lane, lane + 64 .. of the step's.  The wave's own part of LDS turns them into
@@ -34,16 +39,16 @@ struct Step {
 // for two products, of tokens 16t + n (loads in that order are sixteen pieces of lines each,
 // 67 against 59 us).  A token's pieces change places with its number, or they would meet in
 // a bank.
-template <int D>
+template <int D, int T>
 struct Keys {
-    static constexpr int kPieces = D / 16, kLoads = Step<D>::kTiles * D / 64;
+    static constexpr int kPieces = D / 16, kLoads = T * D / 64;
     u32x4 k[kLoads];
 
     template <bool ONCE>
     __device__ __forceinline__ void load(const uint8_t *rec, int half, int lane) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            k[i] = fetch<ONCE, u32x4>(rec + Record<D>::kKey + half * Step<D>::kTokens * D +
+            k[i] = fetch<ONCE, u32x4>(rec + Record<D>::kKey + half * Step<D, T>::kTokens * D +
                                       1024 * i + 16 * lane);
     }
     static __device__ __forceinline__ int place(int token, int piece) {
@@ -61,27 +66,27 @@ struct Keys {
 
 // Value codes: lane (n, g) holds of channels 64c + 4n .. +3 tokens 16t + 4g .. +3, a word
 // for each channel.
-template <int D>
+template <int D, int T>
 struct Values {
-    u32x4 v[Step<D>::kTiles][Step<D>::kChunks];
+    u32x4 v[Step<D, T>::kTiles][Step<D, T>::kChunks];
 
     template <bool ONCE>
     __device__ __forceinline__ void load(const uint8_t *rec, int half, int n, int g) {
 #pragma unroll
-        for (int t = 0; t < Step<D>::kTiles; ++t)
+        for (int t = 0; t < Step<D, T>::kTiles; ++t)
 #pragma unroll
-            for (int c = 0; c < Step<D>::kChunks; ++c)
+            for (int c = 0; c < Step<D, T>::kChunks; ++c)
                 v[t][c] = fetch<ONCE, u32x4>(
                     rec + Record<D>::kValue +
-                    ((half * Step<D>::kTiles + t) * 4 + g) * 4 * D + (64 * c + 4 * n) * 4);
+                    ((half * Step<D, T>::kTiles + t) * 4 + g) * 4 * D + (64 * c + 4 * n) * 4);
     }
     // what no row sees
     __device__ __forceinline__ void clear(int first, int lo, int hi) {
 #pragma unroll
-        for (int t = 0; t < Step<D>::kTiles; ++t) {
+        for (int t = 0; t < Step<D, T>::kTiles; ++t) {
             const uint32_t mask = seen_bytes(first + 16 * t, lo, hi);
 #pragma unroll
-            for (int c = 0; c < Step<D>::kChunks; ++c) v[t][c] &= mask;
+            for (int c = 0; c < Step<D, T>::kChunks; ++c) v[t][c] &= mask;
         }
     }
 };
@@ -90,11 +95,11 @@ struct Values {
 // holds of the keys.
 template <int D>
 struct Queries {
-    u32x4 q[Step<D>::kChunks][2];
+    u32x4 q[D / 64][2];
 
     __device__ __forceinline__ void load(const void *row, bool valid, int g) {
 #pragma unroll
-        for (int c = 0; c < Step<D>::kChunks; ++c) {
+        for (int c = 0; c < D / 64; ++c) {
             q[c][0] = q[c][1] = u32x4{0, 0, 0, 0};
             if (valid) {
                 const u32x4 *at = reinterpret_cast<const u32x4 *>(
@@ -120,15 +125,14 @@ struct Shared {
     f32x2 ml[kWaves][16 * C];
     int scale[kWaves];
     int last;
-    static_assert(sizeof(o[0]) >= Step<D>::kTokens * D, "a step's keys");
+    static_assert(sizeof(o[0]) >= (D <= 64 ? 64 : 32) * D, "a step's keys");
 };
 
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
 // Scores times c are in log2 units.
-template <typename E, int D>
-__device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[Step<D>::kTiles],
-                                      u32x4 (&p)[Step<D>::kTiles / 2], float c) {
-    constexpr int kTiles = Step<D>::kTiles;
+template <typename E, int D, int kTiles>
+__device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4 (&p)[kTiles / 2],
+                                      float c) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -199,7 +203,7 @@ template <typename E, int D, int C, bool CHANGE, bool ONCE>
 __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) void attend16_kernel(
     AttendParams p) {
     constexpr int kRows = 16 * C;
-    typedef Step<D> S;
+    typedef Step<D, kTilesOf<D, C, CHANGE>> S;
     __shared__ Shared<D, C> sh;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -251,7 +255,8 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
 
     RowState<D> st[C];
     Queries<D> q[C];
-    Change change[C];
+    const Change change = {p.cap_log2, p.cap_inverse, p.slopes != nullptr};
+    Slope slope[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         st[c].m = kNone;
@@ -262,9 +267,8 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
                       (int64_t)hq[c] * p.q_head,
                   mine[c], g);
         if constexpr (CHANGE) {
-            change[c].set(p.cap_log2, p.slopes != nullptr,
-                          p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
-                          seq.length - seq.queries + i[c]);
+            slope[c].set(p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
+                         seq.length - seq.queries + i[c]);
         }
     }
     const int32_t *table = p.table + (int64_t)seq.index * p.width;
@@ -296,8 +300,9 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
     // (Two steps at a time, with less to hide them behind: 59 us as well.)
     u32x4 *const pieces = reinterpret_cast<u32x4 *>(&sh.o[wave][0][0]);
     look();
-    Keys<D> keys;
-    Values<D> values;
+    typedef Keys<D, S::kTiles> K;
+    K keys;
+    Values<D, S::kTiles> values;
     u32x2 scales = {0, 0};
     int step = 0, biggest = kLeastScale;
     bool more = todo != 0;
@@ -330,7 +335,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
             for (int c = 0; c < C; ++c) s[c][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int h = 0; h < S::kChunks; ++h) {
-                const u32x4 codes = pieces[Keys<D>::place(16 * t + n, 4 * h + g)];
+                const u32x4 codes = pieces[K::place(16 * t + n, 4 * h + g)];
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const u32x4 k = decode_eight<E>(codes[2 * x], codes[2 * x + 1], f, f);
@@ -350,13 +355,24 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         float scale = __builtin_amdgcn_ldexpf(p.scale_log2, km - 127 - kUp<E>);
         if constexpr (CHANGE) {
+            const auto all = [&](auto f) {
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int t = 0; t < S::kTiles; ++t)
-                    change[c].template apply<4>(s[c][t], scale, t0 + 16 * t + 4 * g,
-                                                [](int k) { return k; });
-            scale = 1.0f;
+                    for (int t = 0; t < S::kTiles; ++t)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) s[c][t][k] = f(s[c][t][k], c, 16 * t + k);
+            };
+            if (change.cap > 0.0f)
+                change.limit(scale, [&](auto f) { all([&](float x, int, int) { return f(x); }); });
+            if (change.cap > 0.0f) scale = 1.0f;
+            if (change.sloped) {
+                float far[C];
+#pragma unroll
+                for (int c = 0; c < C; ++c) far[c] = slope[c].from(t0 + 4 * g);
+                all([&](float x, int c, int j) { return slope[c](x * scale, far[c] - (float)j); });
+                scale = 1.0f;
+            }
         }
         if (masked) {
 #pragma unroll
@@ -374,7 +390,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) weigh<E, D>(st[c], s[c], w[c], scale);
+        for (int c = 0; c < C; ++c) weigh<E, D, S::kTiles>(st[c], s[c], w[c], scale);
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
