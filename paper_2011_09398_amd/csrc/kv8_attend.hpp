@@ -77,17 +77,24 @@ struct Change {
     bool sloped;
 
     // Caps scores, which times `by` are in log2 units: each(f) puts f(x) in the place of
-    // every score x.  cap * tanh(u) is computed as
-    // cap (1 - 2 / (exp(2u) + 1)), whose ends, exponentials of 0 and infinity, give -1 and 1,
-    // known to 2^-22 of the cap.  That is enough of caps in use; under large ones small u
-    // take the power series (|u| < 1/4: up to u^9, off by less than 2^-26 of it).
+    // every score x, and what times `by` plus `offset` is in log2 units is then
+    // cap * tanh(u), as cap (1 - 2 / (exp(2u) + 1)), whose ends, exponentials of 0 and
+    // infinity, give -1 and 1, known to 2^-22 of the cap.  That is enough of caps in use; under
+    // large ones small u take the power series (|u| < 1/4: up to u^9, off by less than 2^-26
+    // of it).
     template <typename Each>
-    __device__ __forceinline__ void limit(float by, Each each) const {
+    __device__ __forceinline__ void limit(float &by, float &offset, Each each) const {
         const float u1 = by * inverse, twice = u1 * 2.88539008177792681f;
-        const auto far = [&](float x) {
-            const float e = __builtin_amdgcn_exp2f(x * twice);
-            return __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(e + 1.0f), cap);
+        const auto part = [&](float x) {
+            return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(x * twice));
         };
+        if (cap <= 256.0f && !sloped) {
+            each(part);
+            by = 2.0f * cap;
+            offset = cap;
+            return;
+        }
+        const auto far = [&](float x) { return __builtin_fmaf(2.0f * cap, part(x), cap); };
         if (cap <= 256.0f) {
             each(far);
         } else {
@@ -100,6 +107,7 @@ struct Change {
                 return z < 0.0625f ? t : far(x);
             });
         }
+        by = 1.0f;
     }
 };
 

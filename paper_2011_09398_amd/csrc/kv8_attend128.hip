@@ -233,7 +233,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     };
     int now = 0;                               // which LDS buffer holds the page at hand
     f32x16 s[2];
-    float factor[2];                           // what s is multiplied by
+    float factor[2];                           // what s is multiplied by, and then, by the cap,
+    float offset = 0.0f;                       // what is added
     u32x4 w[4];                                // weights: second operands of 16 tokens each
     const auto add = [&](int t) {
 #pragma unroll
@@ -251,10 +252,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
 #pragma unroll
                 for (int k = 0; k < 16; ++k) s[t][k] = f(s[t][k], 8 * (k / 4) + k % 4);
             };
-            if (change.cap > 0.0f) {
-                change.limit(by, [&](auto f) { all([&](float x, int) { return f(x); }); });
-                by = 1.0f;
-            }
+            if (change.cap > 0.0f)
+                change.limit(by, offset, [&](auto f) { all([&](float x, int) { return f(x); }); });
             if (change.sloped) {
                 const float far = slope.from(t0 + 4 * h);
                 all([&](float x, int j) { return slope(x * by, far - (float)j); });
@@ -272,7 +271,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         float high = s[t][0];
 #pragma unroll
         for (int k = 1; k < 16; ++k) high = fmaxf(high, s[t][k]);
-        high *= by;
+        high = __builtin_fmaf(high, by, offset);
         // (of large maxima, the difference is exact where a sum is not; each row goes by
         // its own maximum, so that no bit of it depends on the rows beside it)
         if (__builtin_amdgcn_ballot_w64(high - top > kLag + E::kLift)) {
@@ -297,8 +296,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     };
     // The weights of scores k and k + 1 of half t.
     const auto weigh = [&](int t, int k, float &sum) {
-        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k], factor[t], -top));
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k + 1], factor[t], -top));
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k], factor[t], offset - top));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][k + 1], factor[t], offset - top));
         sum += x;
         sum += y;
         w[2 * t + k / 8][k % 8 / 2] = pack_pair<E>(x, y);

@@ -129,16 +129,16 @@ struct Shared {
 };
 
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
-// Scores times c are in log2 units.
+// Scores times c, plus `offset`, are in log2 units.
 template <typename E, int D, int kTiles>
 __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4 (&p)[kTiles / 2],
-                                      float c) {
+                                      float c, float offset) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
-    top *= c;
+    top = __builtin_fmaf(top, c, offset);
     // (Of large maxima, the difference is exact where a sum is not.  Each row goes by
     // its own maximum, so that no bit of it depends on the rows beside it.)
     if (__builtin_amdgcn_ballot_w64(top - st.m > kLag + E::kLift)) {
@@ -161,12 +161,13 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
     // summed by themselves: a long sequence's many small ones would be rounded one by one
     // to the last place of a large sum
     float sum = 0.0f;
+    const float minus = offset - st.m;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
         float w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, -st.m));
+            w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, minus));
             sum += w[i];
         }
         p[t / 2][t % 2 * 2] = pack_pair<E>(w[0], w[1]);
@@ -354,6 +355,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
             keys.template load<ONCE>(rec, following % S::kPerPage, lane);
         }
         float scale = __builtin_amdgcn_ldexpf(p.scale_log2, km - 127 - kUp<E>);
+        float offset = 0.0f;
         if constexpr (CHANGE) {
             const auto all = [&](auto f) {
 #pragma unroll
@@ -364,8 +366,8 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
                         for (int k = 0; k < 4; ++k) s[c][t][k] = f(s[c][t][k], c, 16 * t + k);
             };
             if (change.cap > 0.0f)
-                change.limit(scale, [&](auto f) { all([&](float x, int, int) { return f(x); }); });
-            if (change.cap > 0.0f) scale = 1.0f;
+                change.limit(scale, offset,
+                             [&](auto f) { all([&](float x, int, int) { return f(x); }); });
             if (change.sloped) {
                 float far[C];
 #pragma unroll
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) weigh<E, D, S::kTiles>(st[c], s[c], w[c], scale);
+        for (int c = 0; c < C; ++c) weigh<E, D, S::kTiles>(st[c], s[c], w[c], scale, offset);
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
