@@ -110,19 +110,19 @@ int64_t query_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
 // than registers.  Measured in graphs (us, tiles of 16 / 32 / 128; 32 heads on 8 if not said
 // otherwise; the last two columns float16):
 //                                          128 channels      64 channels      128, capped
-//   16 of 4064 tokens, 64 of them new      48 / 55 / 99      29 / 38 / 80     57 / 71 / 144
-//   one of 5024, 1024 new                 142 / 111 / 121    81 / 65 / 97    173 / 147 / 173
-//   one of 6048, 2048 new                 279 / 222 / 183   162 / 123 / 129  353 / 311 / 252
-//   one of 8096, 4096 new                 640 / 512 / 413   366 / 277 / 286  814 / 720 / 563
-//   four of up to 4512, up to 512 new      86 / 75 / 111     52 / 41 / 89    106 / 97 / 161
-//   four of up to 5024, up to 1024 new    166 / 137 / 126   101 / 76 / 100   207 / 185 / 178
-//   four of up to 6048, up to 2048 new    330 / 272 / 206   197 / 149 / 145  410 / 369 / 284
-//   16 of up to 1024, up to 128 new        34 / 34 / 33      25 / 22 / 26     40 / 41 / 47
-//   one prompt of 1024                     29 / 28 / 31      21 / 20 / 25     35 / 34 / 45
-//   one prompt of 2048                     81 / 71 / 61      50 / 40 / 47     98 / 89 / 86
-//   two of up to 5025, 359 new, 8 on 2     30 / 31 / 60      18 / 20 / 40     36 / 39 / 71
-//   four prompts of up to 1943, 2 on 1     19 / 23 / 49      12 / 16 / 31     23 / 30 / 54
-//   three prompts of up to 2500, 16 on 2   66 / 62 / 67      45 / 37 / 54     83 / 78 / 96
+//   16 of 4064 tokens, 64 of them new      48 / 55 / 99      29 / 38 / 80     54 / 65 / 140
+//   one of 5024, 1024 new                 142 / 111 / 121    81 / 65 / 97    165 / 136 / 169
+//   one of 6048, 2048 new                 279 / 222 / 183   162 / 123 / 129  336 / 287 / 246
+//   one of 8096, 4096 new                 640 / 512 / 413   366 / 277 / 286  769 / 660 / 558
+//   four of up to 4512, up to 512 new      86 / 75 / 111     52 / 41 / 89    100 / 91 / 157
+//   four of up to 5024, up to 1024 new    166 / 137 / 126   101 / 76 / 100   205 / 173 / 173
+//   four of up to 6048, up to 2048 new    330 / 272 / 206   197 / 149 / 145  391 / 342 / 280
+//   16 of up to 1024, up to 128 new        34 / 34 / 33      25 / 22 / 26     38 / 38 / 46
+//   one prompt of 1024                     29 / 28 / 31      21 / 20 / 25     34 / 32 / 44
+//   one prompt of 2048                     81 / 71 / 61      50 / 40 / 47     93 / 83 / 84
+//   two of up to 5025, 359 new, 8 on 2     30 / 31 / 60      18 / 20 / 40     35 / 37 / 70
+//   four prompts of up to 1943, 2 on 1     19 / 23 / 49      12 / 16 / 31     22 / 28 / 54
+//   three prompts of up to 2500, 16 on 2   66 / 62 / 67      45 / 37 / 54     81 / 74 / 94
 int tile_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
     if (d.head_dim > 128) return 16;
     const int forced = tuning(LCE_TUNE_KV8_ROWS);
@@ -175,7 +175,7 @@ Split split_pages(int64_t units, int64_t likely, int64_t pages, int64_t usual, c
     const int64_t room = most_splits(units, parts);
     int64_t chunk = std::max<int64_t>(pages, 1);
     if (const int t = tuning(LCE_TUNE_KV8_CHUNK)) {
-        chunk = std::max(std::clamp<int64_t>(t, 1, chunk), (pages + room - 1) / room);
+        chunk = std::clamp<int64_t>(t, 1, chunk);
     } else {
         const double alone = usual * c.step / 4;
         // the least of alone / z + fixed + each * z
@@ -185,6 +185,8 @@ Split split_pages(int64_t units, int64_t likely, int64_t pages, int64_t usual, c
         if (z > 1 && alone / z + c.fixed + c.each * z < alone)
             chunk = ((int64_t)std::ceil(usual / z) + whole - 1) / whole * whole;
     }
+    // (more pages than usual could be more states than there is room for)
+    chunk = std::max(chunk, (pages + room - 1) / room);
     Split s;
     s.chunk = (int)chunk;
     s.splits = (int)std::max<int64_t>((pages + chunk - 1) / chunk, 1);

@@ -261,6 +261,38 @@ def test_longest_hints_and_workspaces():
     assert not ws[:lce.KV8_WORKSPACE_ZERO].any()
 
 
+@pytest.mark.parametrize("rows,counts,window", [(0, [256, 256], 4600), (16, [300, 212], 4600),
+                                                (32, [512, 512], 4550), (128, [2048, 2048], 4600)])
+def test_states_stay_in_the_workspace(rows, counts, window):
+    """A hint of one new token where there are many, and windows that end inside pages: there
+    is room for as many splits of a tile as pages that windows usually span would make, and
+    not for another."""
+    gen = torch.Generator("cuda").manual_seed(5)
+    cache = lce.KV8Cache(8, 64, pages=160)
+    table = torch.arange(160, dtype=torch.int32, device="cuda").reshape(2, 80)
+    lengths = torch.tensor([5000, 5100], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(10100, 8, 64, generator=gen, device="cuda", dtype=torch.bfloat16)
+            for _ in range(2))
+    begin = torch.tensor([0, 5000, 10100], dtype=torch.int32, device="cuda")
+    lce.kv8_append(cache, k, v, table, begin, lengths)
+    start = torch.tensor([0, counts[0], sum(counts)], dtype=torch.int32, device="cuda")
+    q = torch.randn(sum(counts), 32, 64, generator=gen, device="cuda", dtype=torch.bfloat16)
+    need = lce.kv8_workspace(cache, q, table).numel()
+    behind = 4 << 20
+    space = torch.full((need + behind,), 0x5A, dtype=torch.uint8, device="cuda")
+    space[:lce.KV8_WORKSPACE_ZERO] = 0
+    with lce.tuning(kv8_rows=rows):
+        out = lce.kv8_attention(cache, q, table, start, lengths, window=window, max_q=1,
+                                workspace=space[:need])
+        with lce.tuning(kv8_chunk=80):
+            whole = lce.kv8_attention(cache, q, table, start, lengths, window=window, max_q=1,
+                                      workspace=space[:need])
+    assert (space[need:] == 0x5A).all() and not space[:lce.KV8_WORKSPACE_ZERO].any()
+    # each rounds the result and weights of values of at most `most` by half a step of bfloat16
+    most = v.float().abs().max().item() * (1 + 2.0 ** -4)
+    assert (out.float() - whole.float()).abs().max().item() <= 4 * 2.0 ** -8 * most
+
+
 def test_rows_of_no_sequence_stay():
     batch = ref.Batch(4, [70, 20], [3, 2], 4, 2, 64, "bf16")
     cache, q, table, start, lengths = batch.device(lce)
