@@ -565,7 +565,7 @@ lce_status lce_kv8_cache_size(const lce_kv8_cache_desc *desc, int64_t *bytes);
  * Tokens before a sequence's beginning (n > lengths[b]) and tokens on a page outside
  * the cache are dropped.  Older tokens of a block are those before its first new one;
  * what a block holds behind the last new one is lost.  No two sequences may append to
- * one block in a call.  Appending the same tokens again, nothing having been appended
+ * one block in a call, nor one that has a page twice.  Appending the same tokens again, nothing having been appended
  * behind them, changes nothing.
  * tokens == 0 is a no-op (pointers may then be NULL).
  * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0), LCE_EUNSUPPORTED
@@ -626,10 +626,10 @@ lce_status lce_kv8_workspace_size(const lce_kv8_cache_desc *desc, const lce_kv8_
  * there is a window.  Sums, scores, the running maximum and the running sum are
  * float32; softmax weights are rounded to `type` where they multiply the values
  * (float16: with a last place of at most 2^-31 of a row's largest weight), and out is
- * rounded to it once.  With LCE_FLOAT16, keys are multiplied as multiples of 2^-32 times
- * the largest scale of their page (of half a page with heads of 256), values as
- * multiples of 2^-32 times the largest scale that a row's sequence has: this rounds only
- * what is under a scale 2^-22 times as large.
+ * rounded to it once (float16: what is past 65504 to that).  With LCE_FLOAT16, keys are
+ * multiplied as multiples of 2^-32 times the largest scale of their page, or of less,
+ * values as multiples of 2^-32 times the largest scale that a row's sequence has: this
+ * rounds only what is under a scale 2^-22 times as large.
  * A row that sees nothing is 0 with lse -infinity.
  *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
  *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a
@@ -674,7 +674,7 @@ typedef enum {
 
 /* Frequencies (host, double [rot_dim/2]) of a scaling for contexts `factor` >= 1 times
  * as long as trained (`original` positions; yarn alone looks at it), and the scale
- * that goes with them.
+ * that goes with them.  Yarn's `original` is 7 or more: the first pair's whole turn.
  * Errors: LCE_EINVAL. */
 lce_status lce_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
                                   double original, double *freqs, float *scale);
@@ -697,7 +697,9 @@ typedef struct {
 } lce_rotary_desc;
 
 /* Heads of one tensor, read from x and written to y: channels contiguous, strides in
- * elements.  y may be x (with the same strides); other overlaps are not allowed. */
+ * elements.  y may be x (with the same strides); other overlaps are not allowed.  Rows of
+ * y do not lie between each other: its smaller stride is head_dim or more, its larger one
+ * all that the rows of the other axis take, or more. */
 typedef struct {
     int32_t heads;         /* >= 1                                                     */
     const void *x;

@@ -37,6 +37,7 @@ The same in 8 bits, and the positions of what goes into either:
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import struct
 from typing import Optional, Sequence, Tuple, Union
@@ -1220,11 +1221,15 @@ def kv8_read(cache: KV8Cache, slots, *, dtype=None, out=None):
         v = torch.empty_like(k)
     else:
         k, v = out
+        if dtype is None:
+            dtype = getattr(k, "dtype", torch.bfloat16)
         for t, name in ((k, "out[0]"), (v, "out[1]")):
-            _require_like(t, k.dtype if dtype is None else dtype, slots.device, name)
+            _require_like(t, dtype, slots.device, name)
             if t.shape != shape:
                 raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-        code = _float_type(k.dtype, "out")
+        if k.numel() and k.data_ptr() == v.data_ptr():
+            raise ValueError("out must be two tensors")
+        code = _float_type(dtype, "out")
     _launch(cache._index, lib().lce_kv8_read, cache._ref, cache._data.data_ptr(),
             slots.data_ptr(), shape[0], code, k.data_ptr(), v.data_ptr(), _stream_handle(slots))
     return k, v
@@ -1311,6 +1316,9 @@ def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optiona
                             strides[1])
     except OverflowError:
         raise ValueError(f"scale {scale} or softcap {softcap} is past float32's range") from None
+    except struct.error as e:
+        raise TypeError(f"scale {scale!r}, softcap {softcap!r}, window {window!r}, max_q "
+                        f"{max_q!r} and max_len {max_len!r} must be numbers ({e})") from None
     if out is None:
         out = cache._empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
     else:
@@ -1372,7 +1380,9 @@ class Rotary:
         turns = (ctypes.c_uint64 * n)()
         _check(lib().lce_rotary_turns(values, n, turns))
         self.head_dim, self.rot_dim, self.interleaved = head_dim, rot_dim, bool(interleaved)
-        self.scale = factor_out.value if scale is None else float(scale)
+        self.scale = factor_out.value if scale is None else ctypes.c_float(scale).value
+        if not math.isfinite(self.scale):
+            raise ValueError(f"scale {scale} is not a finite float32")
         self.freqs = torch.tensor(list(values), dtype=torch.float64)
         if torch.device(device).type != "cuda":
             raise ValueError(f"device must be a GPU, got {device}")

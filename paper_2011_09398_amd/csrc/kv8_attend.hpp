@@ -33,6 +33,13 @@ __device__ __forceinline__ float relative(int e, int of, int up) {
     return bits_as<float>((uint32_t)max(127 + e - of + up, 1) << 23);
 }
 
+// What the scores of keys whose largest scale byte is `most` are multiplied by: finite, so
+// that a score of 0 stays one.
+template <typename E>
+__device__ __forceinline__ float score_factor(float scale_log2, int most) {
+    return __builtin_fminf(__builtin_amdgcn_ldexpf(scale_log2, most - 127 - kUp<E>), __FLT_MAX__);
+}
+
 // The scale bytes (byte i: block i) of a page of which some row sees tokens [lo, hi):
 // blocks that no row sees weigh next to nothing, whatever their bytes are.
 __device__ __forceinline__ uint32_t settled_scales(uint32_t scales, int lo, int hi) {
@@ -84,7 +91,9 @@ struct Change {
     // of it).
     template <typename Each>
     __device__ __forceinline__ void limit(float &by, float &offset, Each each) const {
-        const float u1 = by * inverse, twice = u1 * 2.88539008177792681f;
+        // (finite: a score of 0 stays one)
+        const float u1 = by * inverse;
+        const float twice = __builtin_fminf(u1 * 2.88539008177792681f, __FLT_MAX__);
         const auto part = [&](float x) {
             return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(x * twice));
         };

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     const auto settle_keys = [&](int of) {
         const uint32_t ks = settled(scales[0], of);
         const int km = largest_of(ks);
-        c = __builtin_amdgcn_ldexpf(p.scale_log2, km - 127 - kUp<E>);
+        c = score_factor<E>(p.scale_log2, km);
         kf = relative(byte_of(ks, wave), km, kUp<E>);
     };
     const auto settle_values = [&](int of) {

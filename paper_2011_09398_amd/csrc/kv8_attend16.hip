@@ -354,7 +354,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
             scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
             keys.template load<ONCE>(rec, following % S::kPerPage, lane);
         }
-        float scale = __builtin_amdgcn_ldexpf(p.scale_log2, km - 127 - kUp<E>);
+        float scale = score_factor<E>(p.scale_log2, km);
         float offset = 0.0f;
         if constexpr (CHANGE) {
             const auto all = [&](auto f) {

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstdlib>
 
 #include "status.hpp"
 
@@ -217,6 +218,24 @@ lce_status validate_rows(const lce_rotary_rows *r, const char *name, int size) {
     return LCE_OK;
 }
 
+// Rows of a tensor along one of its axes: how many, and how many elements apart.
+struct Axis {
+    int64_t count, apart;
+};
+
+lce_status validate_apart(const lce_rotary_rows *r, const char *name, int64_t tokens, int dim) {
+    // rows that share memory would be written in any order, and in place read after that
+    const Axis axes[2] = {{r->heads, std::abs(r->y_head_stride)}, {tokens, std::abs(r->y_token_stride)}};
+    const Axis &in = axes[axes[1].apart < axes[0].apart], &out = axes[axes[1].apart >= axes[0].apart];
+    if ((in.count > 1 && in.apart < dim) || (out.count > 1 && out.apart < dim) ||
+        (in.count > 1 && out.count > 1 && (out.apart - dim) / (in.count - 1) < in.apart))
+        return fail(LCE_EINVAL, "%s: rows of y overlap or lie between each other", name);
+    if (r->x == r->y && ((r->heads > 1 && r->x_head_stride != r->y_head_stride) ||
+                         (tokens > 1 && r->x_token_stride != r->y_token_stride)))
+        return fail(LCE_EINVAL, "%s: y is x with other strides", name);
+    return LCE_OK;
+}
+
 bool whole(const lce_rotary_rows &r, int per) {
     return aligned(r.x, 16) && aligned(r.y, 16) && r.x_token_stride % per == 0 &&
            r.x_head_stride % per == 0 && r.y_token_stride % per == 0 && r.y_head_stride % per == 0;
@@ -240,8 +259,9 @@ lce_status lce_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling,
         return fail(LCE_EINVAL, "unknown scaling %d", scaling);
     if (scaling != LCE_ROTARY_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor)))
         return fail(LCE_EINVAL, "factor %g is not a finite number >= 1", factor);
-    if (scaling == LCE_ROTARY_YARN && (!(original >= 1.0) || !std::isfinite(original)))
-        return fail(LCE_EINVAL, "original %g is not a finite number >= 1", original);
+    // (the first pair turns once in 2 pi positions, and is the one that yarn leaves as it is)
+    if (scaling == LCE_ROTARY_YARN && (!(original >= 7.0) || !std::isfinite(original)))
+        return fail(LCE_EINVAL, "original %g is not a finite number >= 7", original);
     if (!freqs || !scale) return fail(LCE_EINVAL, "freqs/scale is NULL");
     const double r = rot_dim;
     if (scaling == LCE_ROTARY_NTK && rot_dim > 2) base *= std::pow(factor, r / (r - 2));
@@ -335,6 +355,9 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const uint64_t *turns, const 
     if (groups > (1 << 24) - 1)
         return fail(LCE_EUNSUPPORTED, "%d tokens of %lld heads: too many for one call", d.tokens,
                     (long long)heads);
+    if (const lce_status st = validate_apart(q, "q", d.tokens, d.head_dim)) return st;
+    if (k)
+        if (const lce_status st = validate_apart(k, "k", d.tokens, d.head_dim)) return st;
     const dim3 grid((unsigned)groups);
     if (d.type == LCE_FLOAT32)
         n > 1 ? launch<float, 4>(p, grid, stream) : launch<float, 1>(p, grid, stream);

@@ -360,6 +360,34 @@ def test_largest_values_stay_finite():
             assert ((out / held - 1).abs() <= 4 * ref.HALF_ULP[dtype]).all()
 
 
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("opts", [dict(softcap=1e-6), dict(softcap=1e-6, slopes=True),
+                                  dict(scale=1e30)], ids=str)
+def test_scores_of_zero_beside_the_largest_keys(rows, opts):
+    """A block whose scale times the call's, or over its cap, is past float32's range: its
+    zero keys score 0."""
+    n, dim = 40, 64
+    v = torch.randn(n, 1, dim, generator=torch.Generator().manual_seed(1)).bfloat16()
+    k = torch.zeros(n, 1, dim).bfloat16()
+    k[3, 0, 5] = -1e36
+    cache = lce.KV8Cache(1, dim, pages=1)
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    start, length = (torch.tensor(x, dtype=torch.int32).cuda() for x in ([0, n], [n]))
+    lce.kv8_append(cache, k.cuda(), v.cuda(), table, start, length)
+    seen = lce.kv8_read(cache, torch.arange(n).cuda(), dtype=torch.float32)[1][:, 0].double().cpu()
+    q = torch.ones(n, 1, dim).bfloat16().cuda()
+    if opts.get("slopes"):
+        opts = dict(opts, slopes=torch.zeros(1, device="cuda"))
+    with lce.tuning(kv8_rows=rows):
+        out = lce.kv8_attention(cache, q, table, start, length, causal=False, **opts)[:, 0].cpu()
+    # capped, all weights are alike to 2e-6; else the token of the score below all has none
+    some = seen if "softcap" in opts else torch.cat((seen[:3], seen[4:]))
+    mean, size = some.mean(0), some.abs().mean(0)
+    # weights' and the result's rounding, each half a step of bfloat16, and float32 sums
+    bound = 2.0 ** -8 * 1.01 * (size + mean.abs()) + 1e-5 * size
+    assert ((out.double() - mean).abs() <= bound).all()
+
+
 def test_pages_outside_the_cache_are_hidden():
     batch = ref.Batch(8, [300, 100], [2, 1], 4, 2, 64, "bf16")
     whole = batch.attention(64 ** -0.5)[0]
@@ -405,6 +433,28 @@ def test_strided_queries():
     assert torch.equal(want, lce.kv8_attention(cache, rows[:, 2:6], table, start, lengths))
     first = q.transpose(0, 1).contiguous().transpose(0, 1)
     assert torch.equal(want, lce.kv8_attention(cache, first, table, start, lengths))
+
+
+def test_refusals_of_what_is_no_number_and_of_one_output_twice():
+    batch = ref.Batch(3, [5], [1], 4, 2, 64, "bf16")
+    args = batch.device(lce)
+    for kw in (dict(softcap=None), dict(softcap="2"), dict(scale="1"), dict(window=None),
+               dict(window=1.5), dict(max_q=1.5)):
+        with pytest.raises(TypeError):
+            lce.kv8_attention(*args, **kw)
+    for kw in (dict(scale=1e300), dict(softcap=1e300), dict(window=-1), dict(max_len=2 ** 31)):
+        with pytest.raises((ValueError, lce.LceError)):
+            lce.kv8_attention(*args, **kw)
+    slots = torch.zeros(3, dtype=torch.int64, device="cuda")
+    one = torch.empty(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        lce.kv8_read(args[0], slots, out=(one, one))
+    with pytest.raises(TypeError):
+        lce.kv8_read(args[0], slots, out=(None, one))
+    plan, positions = lce.Rotary(64), torch.zeros(3, dtype=torch.int64, device="cuda")
+    for out in (one[:1].expand(3, 2, 64), one[:, :1].expand(3, 2, 64)):
+        with pytest.raises(lce.LceError):
+            lce.rotary(plan, positions, one, out=out)
 
 
 def test_far_into_a_large_buffer():

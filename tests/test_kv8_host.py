@@ -267,6 +267,32 @@ def test_rotary_refusals():
     assert lce.lib().lce_rotary(None, P, P, None, None, None) == lce.LCE_EINVAL
 
 
+def test_rotary_refuses_rows_that_share_memory():
+    for kw in (dict(y_head_stride=0), dict(y_head_stride=63), dict(y_token_stride=0),
+               dict(y_token_stride=255), dict(y_token_stride=-255), dict(y_head_stride=-63),
+               dict(y_head_stride=128, y_token_stride=64), dict(x_head_stride=128, x_token_stride=512),
+               dict(y_head_stride=2 ** 63 - 1, y_token_stride=2 ** 63 - 1)):
+        bad = rows(**kw)
+        assert call_rotary(bad) == lce.LCE_EINVAL, kw
+        assert call_rotary(rows(), bad) == lce.LCE_EINVAL, kw
+    assert call_rotary(rows(heads=1, y=BIG, y_token_stride=63)) == lce.LCE_EINVAL
+
+
+def test_yarn_needs_the_first_pairs_whole_turn():
+    out, s = (ctypes.c_double * 8)(), ctypes.c_float()
+    for original, want in ((6.0, lce.LCE_EINVAL), (7.0, lce.LCE_OK)):
+        assert lce.lib().lce_rotary_frequencies(16, 1e4, 3, 4.0, original, out,
+                                                ctypes.byref(s)) == want
+    # every pair but the first, which turns 1.1 times, is slowed
+    assert out[0] == 1 and np.allclose(out[1:], 1e4 ** (-np.arange(1, 8) / 8) / 4, rtol=1e-14)
+
+
+@pytest.mark.parametrize("scale", [1e300, float("inf"), float("nan"), -1e39])
+def test_rotary_scale_is_a_float32(scale):
+    with pytest.raises(ValueError, match="scale"):
+        lce.Rotary(8, scale=scale)
+
+
 # ---- the oracle, pinned
 
 def test_reference_codes_by_hand_worked_values():
