@@ -78,6 +78,17 @@ __device__ __forceinline__ uint32_t seen_bytes(int first, int lo, int hi) {
     return w;
 }
 
+// A sum, and two weights in the type in which they multiply values.
+__device__ __forceinline__ float add_rounded(Bf16, uint32_t w, float sum) {
+    constexpr bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(bits_as<bf16x2>(w), one, sum, false);
+}
+
+__device__ __forceinline__ float add_rounded(F16, uint32_t w, float sum) {
+    constexpr f16x2 one = {(_Float16)1.0f, (_Float16)1.0f};
+    return __builtin_amdgcn_fdot2(bits_as<f16x2>(w), one, sum, false);
+}
+
 // What a call does to scores between their product and the softmax; the same for all lanes.
 struct Change {
     float cap, inverse;    // log2 units, 0: none; 1 / cap
@@ -137,8 +148,8 @@ struct Slope {
     }
 };
 
-// A split's state in the workspace: (m, l) of each row and the scale byte of its sums,
-// then the sums of four channels at a time, `rows` rows next to each other.
+// A split's state in the workspace: of each row its maximum and its sum of weights, the scale
+// byte of its sums of values and what they are divided by, then the sums of four channels at a time, `rows` rows next to each other.
 template <int D, int ROWS>
 struct Part {
     static constexpr int kFloats = ROWS * (D + 4);
@@ -152,7 +163,7 @@ struct Part {
 // maximum and scale, against running ones.
 struct Joined {
     f32x4 o;
-    float top, l;
+    float top, l, divisor;
     int scale;
 };
 
@@ -163,18 +174,18 @@ __device__ __forceinline__ Joined join_parts(const float *part, int splits, int 
     Joined r;
     r.o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     r.top = kNone;
-    r.l = 0.0f;
+    r.l = r.divisor = 0.0f;
     r.scale = kLeastScale;
     for (int s0 = 0; s0 < splits; s0 += 16) {
         f32x2 ml[16];
-        int scale[16];
+        f32x2 divisor[16];                     // and the scale byte before it
         f32x4 y[16];
         // four at a time are there or not: what is past the last split is read again,
         // and weighs nothing
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             ml[k] = f32x2{kNone, 0.0f};
-            scale[k] = kLeastScale;
+            divisor[k] = f32x2{(float)kLeastScale, 0.0f};
             y[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 #pragma unroll
@@ -186,7 +197,7 @@ __device__ __forceinline__ Joined join_parts(const float *part, int splits, int 
                     const float *sums = from + P::sums(rows, row, quad);
                     const f32x2 a = got(sums), b = got(sums + 2);
                     ml[k] = got(from + P::state(row));
-                    scale[k] = (int)got(from + P::state(row) + 2)[0];
+                    divisor[k] = got(from + P::state(row) + 2);
                     y[k] = f32x4{a[0], a[1], b[0], b[1]};
                 }
             }
@@ -195,10 +206,11 @@ __device__ __forceinline__ Joined join_parts(const float *part, int splits, int 
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             high = fmaxf(high, ml[k][0]);
-            most = max(most, scale[k]);
+            most = max(most, (int)divisor[k][0]);
         }
         const float f = __builtin_amdgcn_exp2f(r.top - high);
         r.l *= f;
+        r.divisor *= f;
         r.o *= f * relative(r.scale, most, 0);
         r.top = high;
         r.scale = most;
@@ -206,7 +218,8 @@ __device__ __forceinline__ Joined join_parts(const float *part, int splits, int 
         for (int k = 0; k < 16; ++k) {
             const float w = s0 + k < splits ? __builtin_amdgcn_exp2f(ml[k][0] - r.top) : 0.0f;
             r.l += ml[k][1] * w;
-            r.o += y[k] * (w * relative(scale[k], most, 0));
+            r.divisor += divisor[k][1] * w;
+            r.o += y[k] * (w * relative((int)divisor[k][0], most, 0));
         }
     }
     return r;
@@ -214,8 +227,8 @@ __device__ __forceinline__ Joined join_parts(const float *part, int splits, int 
 
 // Four channels of a row's result, and the log of its sum.
 template <typename E>
-__device__ __forceinline__ u32x2 result(const f32x4 &o, float l, int scale) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+__device__ __forceinline__ u32x2 result(const f32x4 &o, float divisor, int scale) {
+    const float inv = divisor == 0.0f ? 0.0f : 1.0f / divisor;
     // codes' means are at most 448 * 2^kUp: only the last factor leaves float32's middle
     const int e = scale - 127 - kUp<E>;
     float x[4];

@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     if (mine) {
         if (h == 0) {
             put(my + P::state(at_row), f32x2{top, l});
-            put(my + P::state(at_row) + 2, f32x2{(float)biggest, 0.0f});
+            put(my + P::state(at_row) + 2, f32x2{(float)biggest, l});
         }
 #pragma unroll
         for (int c = 0; c < D / 64; ++c)
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
             (int64_t)(seq.start + (row0 + rr) / p.group) * (p.kv_heads * p.group) +
             head * p.group + (row0 + rr) % p.group;
         *reinterpret_cast<u32x2 *>((typename E::T *)p.out + to * D + 4 * quad) =
-            result<E>(j.o, j.l, j.scale);
+            result<E>(j.o, j.divisor, j.scale);
         if (p.lse && quad == 0) p.lse[to] = log_sum(j.top, j.l);
     }
 }

@@ -110,11 +110,11 @@ struct Queries {
     }
 };
 
-// A row's state: running maximum of scores (log2), this lane's share of the sum, and the
-// sums of weighted values: o[4c + x][i] of lane (n, g) is row n, channel 64c + 16g + 4i + x.
+// A row's state: running maximum of scores (log2), this lane's share of the sum and
+// of what results are divided by, and the sums of weighted values: o[4c + x][i] of lane (n, g) is row n, channel 64c + 16g + 4i + x.
 template <int D>
 struct RowState {
-    float m, l;
+    float m, l, divisor;
     f32x4 o[D / 16];
 };
 
@@ -122,17 +122,45 @@ struct RowState {
 template <int D, int C>
 struct Shared {
     f32x4 o[kWaves][D / 4][16 * C];
-    f32x2 ml[kWaves][16 * C];
+    f32x4 ml[kWaves][16 * C];                  // m, l, divisor
     int scale[kWaves];
     int last;
     static_assert(sizeof(o[0]) >= (D <= 64 ? 64 : 32) * D, "a step's keys");
 };
 
+// What a weight's rounding does to results shows most in rows that go by few tokens, and in
+// calls of few rows.  In tiles of up to 8 rows of a sequence that has no more than 64, the
+// products' other eight columns, lanes n >= 8, take what is left of each weight once its
+// leading bits, kCut, are cut off: results are as with float32 weights (errors against 64 bits
+// 1.0 times those of rounding the result, with rounded weights 1.2 and up to 1.9; 0 to 1 % of
+// a decoding step's time).  In its taller tiles they are divided by the sum of the rounded
+// weights, so that a row that goes by one token has that token's values.  In the many rows of a
+// prompt they are divided by the sum itself: the other would take 4 % of them in tiles of 16
+// rows, 3 of 32, 7 of 128.
+enum class Weights { kPlain, kRounded, kPaired };
+
+// The bits of a float32 that are an E::T's.
+template <typename E>
+constexpr uint32_t kCut = __is_same(E, F16) ? 0xFFFFE000u : 0xFFFF0000u;
+
+__device__ __forceinline__ float cut(float x, uint32_t mask) {
+    return bits_as<float>(bits_as<uint32_t>(x) & mask);
+}
+
+// A pair of E::T, what they cannot hold cut off.
+template <typename E>
+__device__ __forceinline__ uint32_t cut_pair(float x, float y) {
+    if constexpr (__is_same(E, F16))
+        return bits_as<uint32_t>(__builtin_amdgcn_cvt_pkrtz(x, y));
+    else
+        return __builtin_amdgcn_perm(bits_as<uint32_t>(y), bits_as<uint32_t>(x), 0x07060302u);
+}
+
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
 // Scores times c, plus `offset`, are in log2 units.
 template <typename E, int D, int kTiles>
 __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4 (&p)[kTiles / 2],
-                                      float c, float offset) {
+                                      float c, float offset, Weights kind, uint32_t taken) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -147,6 +175,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
         const float f = __builtin_amdgcn_exp2f(st.m - all);
         st.m = all;
         st.l *= f;
+        st.divisor *= f;
 #pragma unroll
         for (int m = 0; m < D / 16; ++m) st.o[m] *= f;
     }
@@ -160,20 +189,37 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
     }
     // summed by themselves: a long sequence's many small ones would be rounded one by one
     // to the last place of a large sum
-    float sum = 0.0f;
+    float sum = 0.0f, rounded = 0.0f;
     const float minus = offset - st.m;
+    float w[kTiles][4];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        float w[4];
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, minus));
-            sum += w[i];
+            w[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], c, minus));
+            sum += w[t][i];
         }
-        p[t / 2][t % 2 * 2] = pack_pair<E>(w[0], w[1]);
-        p[t / 2][t % 2 * 2 + 1] = pack_pair<E>(w[2], w[3]);
+    const auto pairs = [&](auto f) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                p[t / 2][t % 2 * 2 + i] = f(w[t][2 * i], w[t][2 * i + 1]);
+    };
+    if (kind == Weights::kPaired) {
+        pairs([&](float x, float y) { return cut_pair<E>(x - cut(x, taken), y - cut(y, taken)); });
+    } else {
+        pairs([](float x, float y) { return pack_pair<E>(x, y); });
+        if (kind == Weights::kRounded) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    rounded = add_rounded(E(), p[t / 2][t % 2 * 2 + i], rounded);
+        }
     }
     st.l += sum;
+    st.divisor += kind == Weights::kRounded ? rounded : sum;
 }
 
 }  // namespace
@@ -231,15 +277,20 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
     const int row0 = tile * kRows;
     const int valid = min(rows - row0, kRows);
     const int prefix = p.prefix ? p.prefix[seq.index] : 0;
+    const Weights kind = C > 1 || rows > 64 ? Weights::kPlain
+                         : valid <= 8       ? Weights::kPaired
+                                            : Weights::kRounded;
+    const uint32_t taken = kind == Weights::kPaired && n >= 8 ? kCut<E> : 0u;
+    const int nr = kind == Weights::kPaired ? n & 7 : n;
     // this lane's row of each sixteen
     int i[C], hq[C];
     bool mine[C];
     Span span[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int row = row0 + 16 * c + n;
+        const int row = row0 + 16 * c + nr;
         i[c] = row / p.group, hq[c] = head * p.group + row % p.group;
-        mine[c] = 16 * c + n < valid;
+        mine[c] = 16 * c + nr < valid;
         span[c] = visible(seq, i[c], p.causal, p.window, prefix);
     }
     // spans move up with the rows: the tile's first and last row bound them
@@ -261,7 +312,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         st[c].m = kNone;
-        st[c].l = 0.0f;
+        st[c].l = st[c].divisor = 0.0f;
 #pragma unroll
         for (int m = 0; m < D / 16; ++m) st[c].o[m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         q[c].load((const uint16_t *)p.q + (int64_t)(seq.start + i[c]) * p.q_token +
@@ -392,7 +443,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) weigh<E, D, S::kTiles>(st[c], s[c], w[c], scale, offset);
+        for (int c = 0; c < C; ++c) weigh<E, D, S::kTiles>(st[c], s[c], w[c], scale, offset, kind, taken);
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
@@ -424,8 +475,9 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const float l = across_rows(st[c].l, [](float x, float y) { return x + y; });
-        if (g == 0) sh.ml[wave][16 * c + n] = f32x2{st[c].m, l};
+        const auto add = [](float x, float y) { return x + y; };
+        const float l = across_rows(st[c].l, add), divisor = across_rows(st[c].divisor, add);
+        if (g == 0) sh.ml[wave][16 * c + n] = f32x4{st[c].m, l, divisor, 0.0f};
 #pragma unroll
         for (int h = 0; h < S::kChunks; ++h)
 #pragma unroll
@@ -439,12 +491,13 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
 
     // a thread for every four channels of a row, rows next to each other
     const int shift = valid > 1 ? 32 - __builtin_clz(valid - 1) : 0;   // rows, a power of two
-    const auto write = [&](int r, int quad, const f32x4 &o, float top, float l, int scale) {
+    const auto write = [&](int r, int quad, const f32x4 &o, float top, float l, float divisor,
+                           int scale) {
         const int rr = row0 + r;
         const int64_t at = (int64_t)(seq.start + rr / p.group) * (p.kv_heads * p.group) +
                            head * p.group + rr % p.group;
         *reinterpret_cast<u32x2 *>((typename E::T *)p.out + at * D + 4 * quad) =
-            result<E>(o, l, scale);
+            result<E>(o, divisor, scale);
         if (p.lse && quad == 0) p.lse[at] = log_sum(top, l);
     };
     typedef Part<D, kRows> P;
@@ -460,22 +513,25 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         float top = sh.ml[0][r][0];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh.ml[w][r][0]);
-        float l = 0.0f;
+        float l = 0.0f, divisor = 0.0f;
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const f32x2 ml = sh.ml[w][r];
+            const f32x4 ml = sh.ml[w][r];
             const float f = __builtin_amdgcn_exp2f(ml[0] - top);
             l += ml[1] * f;
-            o += sh.o[w][quad][r] * (f * relative(sh.scale[w], most, 0));
+            divisor += ml[2] * f;
+            f32x4 x = sh.o[w][quad][r];
+            if (kind == Weights::kPaired) x += sh.o[w][quad][r + 8];
+            o += x * (f * relative(sh.scale[w], most, 0));
         }
         if (splits == 1) {
-            write(r, quad, o, top, l, most);
+            write(r, quad, o, top, l, divisor, most);
         } else {
             // several splits: this one's state into the workspace
             if (quad == 0) {
                 put(my + P::state(r), f32x2{top, l});
-                put(my + P::state(r) + 2, f32x2{(float)most, 0.0f});
+                put(my + P::state(r) + 2, f32x2{(float)most, divisor});
             }
             float *to = my + P::sums(valid, r, quad);
             put(to, f32x2{o[0], o[1]});
@@ -495,7 +551,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         const int r = x & ((1 << shift) - 1), quad = x >> shift;
         if (r >= valid) continue;
         const Joined j = join_parts<D, kRows>(part, splits, valid, r, quad);
-        write(r, quad, j.o, j.top, j.l, j.scale);
+        write(r, quad, j.o, j.top, j.l, j.divisor, j.scale);
     }
 }
 

@@ -151,7 +151,8 @@ class Batch:
         m = (j <= p) | (j < (prefix[b] if prefix is not None else 0)) if causal else np.ones(n, bool)
         return m & (j > p - window) if window else m
 
-    def attention(self, scale, causal=True, window=0, cap=0.0, slopes=None, prefix=None):
+    def attention(self, scale, causal=True, window=0, cap=0.0, slopes=None, prefix=None,
+                  weights=None):
         """out, lse and what they may be off by.
 
         A score's products are exact (float16: of keys held to 2^-33 of their page's largest
@@ -160,7 +161,8 @@ class Batch:
         last place off by 2 * (dim + 8) * 2^-24 * (reach + 1).  A cap adds its exponential
         and reciprocal (a last place each of 1 - 2/(e + 1), in all 2^-21 of the cap), a
         slope its own rounding and the product's, 2^-22 of the bias.  Each weight is off by
-        its score's error and by half a unit of its type where it is rounded, the result by
+        its score's error and by half a unit of its type where it is rounded (or by `weights`), the
+        result by
         half a unit of its type, sums of n float32 terms by n * 2^-24 of the sum of their
         absolute values.  float16 weights have a last place of 2^-31 of the largest,
         values one of 2^-32 of the largest scale, results one of 2^-24."""
@@ -199,7 +201,8 @@ class Batch:
                         w = e / e.sum()
                         out[t, h] = w @ v
                         # (a mean's error is at most twice that of its weights times the values)
-                        rel = np.expm1(err) + u + (len(w) + 64) * 2.0 ** -24
+                        rel = (np.expm1(err) + (u if weights is None else weights)
+                               + (len(w) + 64) * 2.0 ** -24)
                         mean = np.abs(w @ v)
                         bound[t, h] = (w * rel) @ np.abs(v) + (w @ rel) * mean + u * 1.01 * mean
                         if half:

@@ -180,7 +180,7 @@ def check(batch, lce_args=None, **kw):
     """The call against the oracle, within the bounds that the oracle derives."""
     opts = {k: v for k, v in kw.items() if k in ("causal", "window", "cap", "slopes", "prefix")}
     scale = batch.dim ** -0.5
-    want, want_lse, bound, lse_bound = batch.attention(scale, **opts)
+    want, want_lse, bound, lse_bound = batch.attention(scale, weights=kw.get("weights"), **opts)
     cache, q, table, start, lengths = batch.device(lce)
     opts["softcap"] = opts.pop("cap", 0.0)
     for name, dtype in (("slopes", torch.float32), ("prefix", torch.int32)):
@@ -211,6 +211,21 @@ SOME = [0, 1, 5, 0, 17, 2, 64, 3, 7, 20]
 @pytest.mark.parametrize("queries", [ONE, SOME])
 def test_attention(q_heads, kv_heads, dim, dtype, queries):
     check(ref.Batch(dim + q_heads, LENGTHS, queries, q_heads, kv_heads, dim, dtype))
+
+
+@pytest.mark.parametrize("dtype,weights", [("bf16", 2.0 ** -14), ("f16", 2.0 ** -20)])
+@pytest.mark.parametrize("q_heads,kv_heads,dim", [(8, 2, 64), (7, 1, 128), (16, 2, 256)])
+@pytest.mark.parametrize("chunk", [0, 1])
+def test_few_rows_have_weights_of_two_parts(q_heads, kv_heads, dim, dtype, weights, chunk):
+    """Up to eight rows of a head: a weight's leading bits (bfloat16: cut off below 2^-7 of it,
+    float16: 2^-10) and as many of what is left."""
+    queries = [1 if n else 0 for n in LENGTHS]
+    if q_heads // kv_heads <= 4:
+        queries[5] = queries[-1] = 2
+    batch = ref.Batch(dim + q_heads, LENGTHS, queries, q_heads, kv_heads, dim, dtype, loud=3.0)
+    with lce.tuning(kv8_chunk=chunk):
+        check(batch, weights=weights)
+        check(batch, weights=weights, cap=20.0, window=100)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
