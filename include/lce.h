@@ -457,6 +457,173 @@ lce_status lce_kv4_workspace_size(const lce_kv4_cache_desc *desc, const lce_kv4_
  * of channels that are at least 2^-13 of the largest |q| of their group (of 32
  * channels, as they share a scale in a key); smaller ones are held to 2^-21 of
  * it (float16: 2^-25).  Sums, the running maximum and the running sum are
+ * float32; softmax weights are rounded to `type` where they multiply the values
+ * (float16: with a last place of at most 2^-31 of a row's largest weight), and
+ * out is rounded to it once.
+ * A row that sees nothing is 0 with lse -infinity.
+ *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
+ *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a
+ *           length are not read; tokens on a page outside the cache are hidden
+ *   q_start int32 [seqs+1], not decreasing, lengths int32 [seqs] (device);
+ *           values outside [0, tokens] and [0, 64*table_width] are taken as the
+ *           nearest bound
+ *   pages   with query->list > 0, int32 [tokens][kv_heads][list] (device): only
+ *           tokens j on the pages j/64 named here are visible; numbers that
+ *           are negative or past the length name nothing; naming a page twice
+ *           counts it twice.  Otherwise ignored
+ *   out     [tokens][q_heads][head_dim] of query->type, contiguous (device,
+ *           16-byte aligned); rows of no sequence are left as they are
+ *   lse     float32 [tokens][q_heads] or NULL
+ *   workspace, workspace_bytes: see lce_kv4_attention_workspace_size
+ * A query row that holds an infinity or a NaN gives NaN.  With LCE_FLOAT16,
+ * cached values of 65536 and more count as 65504, the largest float16 (and
+ * -65536 and less as -65504), not as the infinities that lce_kv4_read makes of
+ * them; what shares a scale with them is not affected.  Those below 2^-23 count
+ * as the nearest multiple of 2^-24.
+ * Errors: LCE_EINVAL (null pointer, bad field, small workspace),
+ *         LCE_EUNSUPPORTED (head_dim, type, more than 65535 kv_heads, a
+ *         table_width or a list over 2^24, more rows or tiles than a grid
+ *         holds),
+ *         LCE_EALIGN, LCE_EHIP. */
+lce_status lce_kv4_attention(const lce_kv4_cache_desc *desc, const void *cache,
+                             const lce_kv4_query_desc *query, const void *q, const int32_t *table,
+                             const int32_t *q_start, const int32_t *lengths, const int32_t *pages,
+                             void *out, float *lse, void *workspace, int64_t workspace_bytes,
+                             hipStream_t stream);
+
+/* Choose query->list pages for each new token and cache head, by the signs of
+ * queries and keys.  A page scores
+ *     max over its visible tokens j of  sum over the query heads g of the
+ *     cache head, and the channels c, of  sgn(q_gc) * sgn(k_jc)
+ * (an XOR and a population count; sgn = -1 iff x < 0).  With n pages up to the
+ * last visible token, the pages below keep_first and those from n - keep_last
+ * on rank before all others; then higher scores, and lower page numbers among
+ * equal ones.  pages int32 [tokens][kv_heads][list] (device) gets the chosen
+ * page numbers in ascending order, then -1.  Pages on which the window leaves
+ * nothing, or that the table names outside the cache, are not chosen.
+ * The other arguments as for lce_kv4_attention (workspace: see
+ * lce_kv4_select_workspace_size).
+ * Errors: as lce_kv4_attention, plus LCE_EINVAL (list < 1, keep < 0) and
+ *         LCE_EUNSUPPORTED (q_heads / kv_heads * head_dim > 65280). */
+lce_status lce_kv4_select(const lce_kv4_cache_desc *desc, const void *cache,
+                          const lce_kv4_query_desc *query, const void *q, const int32_t *table,
+                          const int32_t *q_start, const int32_t *lengths, int32_t keep_first,
+                          int32_t keep_last, int32_t *pages, void *workspace,
+                          int64_t workspace_bytes, hipStream_t stream);
+
+/* ---- 8-bit key/value cache ----------------------------------------------
+ *
+ * The same cache with a byte a channel, for models that lose too much in four bits:
+ * 8-bit floats (e4m3: a sign, four bits of exponent, three of mantissa; multiples of
+ * 2^-9 up to 448) that share one power of two per LCE_KV8_BLOCK = 16 tokens of a head,
+ * one for its keys and one for its values.
+ *
+ * A block's scale is the smallest power of two, of 2^-126 and more, with which no
+ * channel of the tokens that one call appends to it is past 448, or the scale that the
+ * block had, where it holds older tokens and that is larger:
+ *     code = x / scale rounded to the nearest e4m3 value, ties to even;
+ *     the value held is code * scale.
+ * Where a call raises the scale of a block that holds older tokens, their codes are
+ * rounded once more, to the new scale's values (which changes only those below 2^-6 of
+ * it).  A token that holds an infinity or a NaN in its key or its value gets the NaN
+ * code in all channels of its key, and 0 for what is not finite in its value: every row
+ * that attends to it is NaN, and no other row.
+ *
+ * The cache is one device buffer of pages of LCE_KV8_PAGE = 64 tokens, each page
+ * holding a record of 128*D + 128 bytes per head (D = head_dim), with token t of the
+ * page at
+ *     key codes     byte  t*D + c                       (channel c)
+ *     value codes   byte  64*D + (t/4*D + c)*4 + t%4
+ *     key scales    byte  128*D + t/16                  (2^(byte-127))
+ *     value scales  byte  128*D + 4 + t/16
+ * and 120 bytes that nothing uses, so that records begin with a line of memory.  A
+ * sequence is a row of page numbers (its table) and a length; its token j is in slot
+ * table[j/64]*64 + j%64. */
+#define LCE_KV8_PAGE 64
+#define LCE_KV8_BLOCK 16
+
+typedef struct {
+    int32_t pages;       /* pages of the buffer, >= 1                        */
+    int32_t kv_heads;    /* heads of keys and values, >= 1                   */
+    int32_t head_dim;    /* channels of a head: 64, 128 or 256               */
+} lce_kv8_cache_desc;
+
+/* Bytes of the cache buffer of `desc`: pages * kv_heads * 128 * (head_dim + 1).  Its
+ * contents need no initialization: what was never written may be anything as long as
+ * no length covers it.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim). */
+lce_status lce_kv8_cache_size(const lce_kv8_cache_desc *desc, int64_t *bytes);
+
+/* Quantize the last tokens of sequences into the cache: `tokens` rows of keys and
+ * values, those of sequence b at q_start[b] .. q_start[b+1]-1; with n of them, number i
+ * is the sequence's token lengths[b] - n + i (lengths count the new tokens).
+ *   cache  buffer of lce_kv8_cache_size bytes             (device, 16-byte aligned)
+ *   k, v   [tokens][kv_heads][head_dim] of `type`         (device, 16-byte aligned),
+ *          channels contiguous; token and head strides in elements, each a
+ *          multiple of 16 bytes
+ *   table, q_start, lengths   as for lce_kv8_attention
+ * Tokens before a sequence's beginning (n > lengths[b]) and tokens on a page outside
+ * the cache are dropped.  Older tokens of a block are those before its first new one;
+ * what a block holds behind the last new one is lost.  No two sequences may append to
+ * one block in a call, nor one that has a page twice.  Appending the same tokens again, nothing having been appended
+ * behind them, changes nothing.
+ * tokens == 0 is a no-op (pointers may then be NULL).
+ * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0), LCE_EUNSUPPORTED
+ *         (head_dim, kv_heads > 65535, table_width over 2^24, more blocks than a grid
+ *         holds), LCE_EALIGN (pointer or stride), LCE_EHIP. */
+lce_status lce_kv8_append(const lce_kv8_cache_desc *desc, void *cache, int32_t type,
+                          const void *k, int64_t k_token_stride, int64_t k_head_stride,
+                          const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                          int32_t tokens, int32_t seqs, int32_t table_width, const int32_t *table,
+                          const int32_t *q_start, const int32_t *lengths, hipStream_t stream);
+
+/* Read tokens back: k and v [tokens][kv_heads][head_dim] of `type`, contiguous
+ * (device, 16-byte aligned), get the values that the cache holds for `slots` (int64
+ * [tokens], device), zeros for a slot outside the cache.  float32 holds every value
+ * exactly, bfloat16 those of 2^-126 and more; float16 rounds those below 2^-20 to the
+ * nearest multiple of 2^-24 and has infinities for those of 65536 and more.
+ * Errors: LCE_EINVAL (null pointer, bad field, tokens < 0 or >= 2^31), LCE_EUNSUPPORTED
+ *         (head_dim, kv_heads > 65535), LCE_EALIGN, LCE_EHIP. */
+lce_status lce_kv8_read(const lce_kv8_cache_desc *desc, const void *cache, const int64_t *slots,
+                        int64_t tokens, int32_t type, void *k, void *v, hipStream_t stream);
+
+/* New tokens that attend over cached sequences (see lce_kv4_query_desc). */
+typedef struct {
+    int32_t tokens;        /* query tokens over all sequences, >= 0                    */
+    int32_t q_heads;       /* a multiple of kv_heads; head hq reads cache head
+                              hq / (q_heads / kv_heads)                                */
+    int32_t seqs;          /* sequences, >= 1                                          */
+    int32_t table_width;   /* page numbers per row of the table, >= 1                  */
+    int32_t type;          /* LCE_FLOAT16 or LCE_BFLOAT16: q and out                   */
+    int32_t causal;        /* 1: position p sees tokens j <= p, and a prefix; 0: all   */
+    int32_t window;        /* > 0: only tokens j > p - window; 0: no such bound        */
+    int32_t max_q;         /* hints for the split of the work, 0 = unknown: the most   */
+    int32_t max_len;       /* new tokens, the longest length.  Wrong ones cost speed.  */
+    float scale;           /* of the scores, finite and > 0                            */
+    float softcap;         /* 0: none, or what scores are capped at, 1e-30 .. 1e30     */
+    int64_t q_token_stride, q_head_stride;   /* elements, multiples of 8               */
+} lce_kv8_query_desc;
+
+/* Bytes of workspace that lce_kv8_attention calls with these tokens or fewer, q_heads,
+ * seqs and table_width can need (the other fields do not matter): 128 KiB, and at most
+ * 36 MB (heads of 64: 18, of 256: 69) of partial results.  The workspace is 16-byte
+ * aligned device memory whose first LCE_KV8_WORKSPACE_ZERO bytes are zero before its
+ * first use; each call leaves them zero.  Calls that may run at the same time need one
+ * each.
+ * Errors: LCE_EINVAL (null pointer, bad field), LCE_EUNSUPPORTED (head_dim, as
+ *         lce_kv8_attention). */
+#define LCE_KV8_WORKSPACE_ZERO 131072
+lce_status lce_kv8_workspace_size(const lce_kv8_cache_desc *desc, const lce_kv8_query_desc *query,
+                                  int64_t *bytes);
+
+/* Attention of new tokens over the cache: per token (position p) and query head
+ *     s_j = scale * (q . k_j)                        over the visible tokens j,
+ *     s_j = softcap * tanh(s_j / softcap)            with a softcap,
+ *     s_j = s_j - slopes[head] * |p - j|             with slopes,
+ *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)
+ * with k and v as the cache holds them.  Token j is visible where j <= p or j <
+ * prefix[b] (causal) or anywhere in the sequence (not causal), and j > p - window where
+ * there is a window.  Sums, scores, the running maximum and the running sum are
  * float32; softmax weights are rounded to `type` where they multiply the values, or, where
  * a sequence has up to 8 rows of a cache head, split into two of that type (float16: with a
  * last place of at most 2^-31 of a row's largest weight), and out is
