@@ -298,11 +298,16 @@ def _raw_stream():
 _raw = None
 
 
-def _stream_handle(t) -> int:
+def _stream_of(index) -> int:
+    """The handle of device `index`'s current stream."""
     global _raw
     if _raw is None:
         _raw = _raw_stream()
-    return _raw(t.device.index)
+    return _raw(index)
+
+
+def _stream_handle(t) -> int:
+    return _stream_of(t.device.index)
 
 
 def _require(t, dtype, name):
@@ -804,10 +809,11 @@ class _PagedCache:
         # what every call compares its tensors with
         self._index = data.get_device()
         self._int32, self._int64 = torch.int32, torch.int64
-        self._uint8, self._float32 = torch.uint8, torch.float32
+        self._uint8, self._float32, self._bfloat16 = torch.uint8, torch.float32, torch.bfloat16
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
         self._scale = head_dim ** -0.5
         self._empty, self._empty_like, self._device = torch.empty, torch.empty_like, data.device
+        self._contiguous = torch.contiguous_format
 
     @property
     def data(self):
@@ -1199,30 +1205,37 @@ def kv8_append(cache: KV8Cache, k, v, table, q_start, lengths) -> None:
         _int32_refused(tokens=n, sequences=seqs, table=width)
     _launch(cache._index, lib().lce_kv8_append, cache._ref, cache._data.data_ptr(), code,
             k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], n, seqs, width,
-            table.data_ptr(), q_start.data_ptr(), lengths.data_ptr(), _stream_handle(k))
+            table.data_ptr(), q_start.data_ptr(), lengths.data_ptr(), _stream_of(cache._index))
 
 
 def kv8_read(cache: KV8Cache, slots, *, dtype=None, out=None):
     """The values that the cache holds for `slots` (int64 [tokens]): a pair k, v
     [tokens, kv_heads, head_dim] of `dtype` (default bfloat16), or into the pair
     `out`.  Slots outside the cache read as zeros."""
-    import torch
-    _require_cache(cache, KV8Cache)
-    if not isinstance(slots, torch.Tensor) or not cache._holds(slots, torch.int64):
-        _require_like(slots, torch.int64, cache.data.device, "slots")
-    if slots.dim() != 1:
-        raise ValueError("slots must have one dimension")
-    shape = (slots.shape[0], cache.kv_heads, cache.head_dim)
+    try:
+        n, = slots.shape
+        fine = type(cache) is KV8Cache and cache._holds(slots, cache._int64)
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _require_cache(cache, KV8Cache)
+        _require_like(slots, cache._int64, cache.data.device, "slots")
+        if slots.dim() != 1:
+            raise ValueError("slots must have one dimension")
+        n, = slots.shape
+    shape = (n, cache.kv_heads, cache.head_dim)
     if out is None:
         if dtype is None:
-            dtype = torch.bfloat16
-        code = _float_type(dtype, "dtype")
-        k = torch.empty(shape, dtype=dtype, device=cache._device)
-        v = torch.empty_like(k)
+            dtype = cache._bfloat16
+        code = cache._types.get(dtype)
+        if code is None:
+            code = _float_type(dtype, "dtype")
+        k = cache._data.new_empty(shape, dtype=dtype)
+        v = cache._empty_like(k)
     else:
         k, v = out
         if dtype is None:
-            dtype = getattr(k, "dtype", torch.bfloat16)
+            dtype = getattr(k, "dtype", cache._bfloat16)
         for t, name in ((k, "out[0]"), (v, "out[1]")):
             _require_like(t, dtype, slots.device, name)
             if t.shape != shape:
@@ -1231,7 +1244,7 @@ def kv8_read(cache: KV8Cache, slots, *, dtype=None, out=None):
             raise ValueError("out must be two tensors")
         code = _float_type(dtype, "out")
     _launch(cache._index, lib().lce_kv8_read, cache._ref, cache._data.data_ptr(),
-            slots.data_ptr(), shape[0], code, k.data_ptr(), v.data_ptr(), _stream_handle(slots))
+            slots.data_ptr(), n, code, k.data_ptr(), v.data_ptr(), _stream_of(cache._index))
     return k, v
 
 
@@ -1320,13 +1333,12 @@ def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optiona
         raise TypeError(f"scale {scale!r}, softcap {softcap!r}, window {window!r}, max_q "
                         f"{max_q!r} and max_len {max_len!r} must be numbers ({e})") from None
     if out is None:
-        out = cache._empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
+        out = cache._empty_like(q, memory_format=cache._contiguous)
     else:
         _require_like(out, q.dtype, q.device, "out")
         if out.shape != q.shape:
             raise ValueError(f"out must be {list(q.shape)}, got {list(out.shape)}")
-    lse = (cache._empty((tokens, heads), dtype=cache._float32, device=cache._device) if return_lse
-           else None)
+    lse = q.new_empty((tokens, heads), dtype=cache._float32) if return_lse else None
     if workspace is None:
         workspace = kv8_workspace(cache, q, table)
     elif not cache._holds(workspace, cache._uint8):
@@ -1336,7 +1348,7 @@ def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optiona
             lengths.data_ptr(), None if slopes is None else slopes.data_ptr(),
             None if prefix is None else prefix.data_ptr(), out.data_ptr(),
             None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
-            _stream_handle(q))
+            _stream_of(cache._index))
     return (out, lse) if return_lse else out
 
 
@@ -1389,7 +1401,8 @@ class Rotary:
         # (as int64: the same bits)
         self._turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns],
                                    dtype=torch.int64).to(device)
-        self._index = self._turns.get_device()
+        self._index, self._turns_ptr = self._turns.get_device(), self._turns.data_ptr()
+        self._interleaved = int(self.interleaved)
         # what every call compares its tensors with
         self._int64, self._empty_like = torch.int64, torch.empty_like
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -1461,25 +1474,28 @@ def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=No
             shape, y = k.shape, k.stride()
     if (n | heads) >> 31 or k is not None and shape[1] >> 31:
         _int32_refused(tokens=n, heads=heads if k is None else max(heads, shape[1]))
+    second = None
     if out is None:
-        outs = tuple(_empty_rows(plan, t) for t in ((q,) if k is None else (q, k)))
+        first = _empty_rows(plan, q)
+        if k is not None:
+            second = _empty_rows(plan, k)
     elif k is None:
-        outs = (_rotary_out(q, out, "q"),)
+        first = _rotary_out(q, out, "q")
     else:
         if len(out) != 2:
             raise ValueError("out must be a pair of tensors")
-        outs = (_rotary_out(q, out[0], "q"), _rotary_out(k, out[1], "k"))
-    to = outs[0].stride()
-    qr = _pack_rotary_rows(heads, q.data_ptr(), outs[0].data_ptr(), x[0], x[1], to[0], to[1])
+        first, second = _rotary_out(q, out[0], "q"), _rotary_out(k, out[1], "k")
+    to = first.stride()
+    qr = _pack_rotary_rows(heads, q.data_ptr(), first.data_ptr(), x[0], x[1], to[0], to[1])
     kr = None
     if k is not None:
-        to = outs[1].stride()
-        kr = _pack_rotary_rows(shape[1], k.data_ptr(), outs[1].data_ptr(), y[0], y[1], to[0], to[1])
+        to = second.stride()
+        kr = _pack_rotary_rows(shape[1], k.data_ptr(), second.data_ptr(), y[0], y[1], to[0], to[1])
     _launch(plan._index, lib().lce_rotary,
-            _pack_rotary(n, dim, plan.rot_dim, code, 1 if plan.interleaved else 0,
-                         1 if backward else 0, plan.scale),
-            plan._turns.data_ptr(), positions.data_ptr(), qr, kr, _stream_handle(q))
-    return outs[0] if k is None else outs
+            _pack_rotary(n, dim, plan.rot_dim, code, plan._interleaved, 1 if backward else 0,
+                         plan.scale),
+            plan._turns_ptr, positions.data_ptr(), qr, kr, _stream_of(plan._index))
+    return first if k is None else (first, second)
 
 
 def _empty_rows(plan, t):
