@@ -89,10 +89,16 @@ __device__ __forceinline__ float add_rounded(F16, uint32_t w, float sum) {
     return __builtin_amdgcn_fdot2(bits_as<f16x2>(w), one, sum, false);
 }
 
-// What a call does to scores between their product and the softmax; the same for all lanes.
-struct Change {
+// What a call does to scores between their product and the softmax: nothing, a cap of up to
+// kNearCap by itself, or a cap, a bias by distance or both.  (The second has a kernel of its own
+// because values that several branches make are copied where these meet: prompts in tiles
+// of 32 rows @A@ us without one, @B@ with.)
+enum class Change { kNone, kCapped, kAny };
+constexpr float kNearCap = 256.0f;         // log2 units
+static_assert(kNearCap + kLag + F16::kLift < kLarge, "capped scores are not large");
+
+struct Cap {
     float cap, inverse;    // log2 units, 0: none; 1 / cap
-    bool sloped;
 
     // Caps scores, which times `by` are in log2 units: each(f) puts f(x) in the place of
     // every score x, and what times `by` plus `offset` is in log2 units is then
@@ -100,7 +106,7 @@ struct Change {
     // infinity, give -1 and 1, known to 2^-22 of the cap.  That is enough of caps in use; under
     // large ones small u take the power series (|u| < 1/4: up to u^9, off by less than 2^-26
     // of it).
-    template <typename Each>
+    template <Change C, typename Each>
     __device__ __forceinline__ void limit(float &by, float &offset, Each each) const {
         // (finite: a score of 0 stays one)
         const float u1 = by * inverse;
@@ -108,14 +114,14 @@ struct Change {
         const auto part = [&](float x) {
             return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(x * twice));
         };
-        if (cap <= 256.0f && !sloped) {
+        if constexpr (C == Change::kCapped) {
             each(part);
             by = 2.0f * cap;
             offset = cap;
             return;
         }
         const auto far = [&](float x) { return __builtin_fmaf(2.0f * cap, part(x), cap); };
-        if (cap <= 256.0f) {
+        if (cap <= kNearCap) {
             each(far);
         } else {
             each([&](float x) {
@@ -239,6 +245,20 @@ __device__ __forceinline__ u32x2 result(const f32x4 &o, float divisor, int scale
 
 __device__ __forceinline__ float log_sum(float top, float l) {
     return l == 0.0f ? -__builtin_inff() : (top + __builtin_log2f(l)) * 0.69314718055994531f;
+}
+
+// The kernel that a call takes, by what it does to scores: launch(kind), kind::value being
+// a Change.
+template <Change C>
+struct ChangeOf {
+    static constexpr Change value = C;
+};
+
+template <typename Launch>
+void by_change(const AttendParams &p, Launch launch) {
+    if (p.slopes || p.cap_log2 > kNearCap) launch(ChangeOf<Change::kAny>());
+    else if (p.cap_log2 > 0.0f) launch(ChangeOf<Change::kCapped>());
+    else launch(ChangeOf<Change::kNone>());
 }
 
 }  // namespace kv8

@@ -119,7 +119,7 @@ __device__ __forceinline__ void lds_barrier() {
 // TFLOP/s; 4 sequences of up to 2048 new tokens on up to 16384, causal, 616 us, 998 TFLOP/s
 // of visible pairs (a large library product: 1170 to 1390); of up to 1700 on up to 6500, of
 // which one has 85 % of the work, 192 us, 930 TFLOP/s.
-template <typename E, int D, bool CHANGE>
+template <typename E, int D, Change CHANGE>
 __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) {
     __shared__ Page<D> pages[2];
     __shared__ int last;
@@ -159,9 +159,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     Queries<D> q;
     q.load((const uint16_t *)p.q + (int64_t)(seq.start + i) * p.q_token + (int64_t)hq * p.q_head,
            mine, h);
-    const Change change = {p.cap_log2, p.cap_inverse, p.slopes != nullptr};
+    const Cap cap = {p.cap_log2, p.cap_inverse};
     Slope slope;
-    if constexpr (CHANGE)
+    if constexpr (CHANGE == Change::kAny)
         slope.set(p.slopes && mine ? p.slopes[hq] : 0.0f, seq.length - seq.queries + i);
 
     // the state of a row: running maximum (log2), this lane's share of the sum, sums of
@@ -247,18 +247,17 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
     // before, against the maximum so far, wait to be added.
     const auto judge = [&](int t, int of, float by, bool there) {
         const int t0 = of * kPage + 32 * t;
-        if constexpr (CHANGE) {
-            const auto all = [&](auto f) {
+        const auto all = [&](auto f) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) s[t][k] = f(s[t][k], 8 * (k / 4) + k % 4);
-            };
-            if (change.cap > 0.0f)
-                change.limit(by, offset, [&](auto f) { all([&](float x, int) { return f(x); }); });
-            if (change.sloped) {
-                const float far = slope.from(t0 + 4 * h);
-                all([&](float x, int j) { return slope(x * by, far - (float)j); });
-                by = 1.0f;
-            }
+            for (int k = 0; k < 16; ++k) s[t][k] = f(s[t][k], 8 * (k / 4) + k % 4);
+        };
+        if (CHANGE == Change::kCapped || (CHANGE == Change::kAny && cap.cap > 0.0f))
+            cap.limit<CHANGE>(by, offset,
+                              [&](auto f) { all([&](float x, int) { return f(x); }); });
+        if (CHANGE == Change::kAny && p.slopes) {
+            const float far = slope.from(t0 + 4 * h);
+            all([&](float x, int j) { return slope(x * by, far - (float)j); });
+            by = 1.0f;
         }
         if (!there || t0 < wz.lo || t0 + 32 > wa.hi) {
             const int lo = span.lo - t0 - 4 * h, hi = there ? span.hi - t0 - 4 * h : lo;
@@ -287,8 +286,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         }
         // the fused product differs from the rounded one that the maximum is: where that
         // could show, round the scores' products too
-        const bool large = __builtin_fabsf(top) > kLarge;
-        if (__builtin_amdgcn_ballot_w64(large)) {
+        const bool large = CHANGE != Change::kCapped && __builtin_fabsf(top) > kLarge;
+        if (CHANGE != Change::kCapped && __builtin_amdgcn_ballot_w64(large)) {
             s[t] = large ? s[t] * by : s[t];
             by = large ? 1.0f : by;
         }
@@ -517,10 +516,10 @@ namespace {
 
 template <typename E, int D>
 void launch_d(const AttendParams &p, dim3 grid, hipStream_t s) {
-    if (p.slopes || p.cap_log2 > 0.0f)
-        hipLaunchKernelGGL((attend128_kernel<E, D, true>), grid, dim3(kThreads), 0, s, p);
-    else
-        hipLaunchKernelGGL((attend128_kernel<E, D, false>), grid, dim3(kThreads), 0, s, p);
+    by_change(p, [&](auto kind) {
+        hipLaunchKernelGGL((attend128_kernel<E, D, decltype(kind)::value>), grid, dim3(kThreads), 0,
+                           s, p);
+    });
 }
 
 template <typename E>

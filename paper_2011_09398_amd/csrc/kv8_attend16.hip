@@ -30,8 +30,8 @@ struct Step {
 // there is: wide heads (of 128: 67 us against 87 of 48 sequences of up to 8192 tokens, when
 // keys did not come through LDS yet), and 32 rows of 64 with scores to change (47 against 50
 // us of the prompts below; without, 41 against 37).
-template <int D, int C, bool CHANGE>
-constexpr int kTilesOf = D <= 64 && !(C == 2 && CHANGE) ? 4 : 2;
+template <int D, int C, Change CHANGE>
+constexpr int kTilesOf = D <= 64 && !(C == 2 && CHANGE != Change::kNone) ? 4 : 2;
 
 // Key codes of a step as they come from memory, whole lines of it: 16 bytes a lane at a
 // time, pieces lane, lane + 64 .. of the step's.  The wave's own part of LDS turns them into
@@ -158,7 +158,7 @@ __device__ __forceinline__ uint32_t cut_pair(float x, float y) {
 
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
 // Scores times c, plus `offset`, are in log2 units.
-template <typename E, int D, int kTiles>
+template <typename E, int D, Change CHANGE, int kTiles>
 __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4 (&p)[kTiles / 2],
                                       float c, float offset, Weights kind, uint32_t taken) {
     float top = s[0][0];
@@ -181,8 +181,8 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
     }
     // The fused product below differs from the rounded one that the maximum is: where
     // that could show (scores past kLarge), round the scores' products too.
-    const bool large = __builtin_fabsf(st.m) > kLarge;
-    if (__builtin_amdgcn_ballot_w64(large)) {
+    const bool large = CHANGE != Change::kCapped && __builtin_fabsf(st.m) > kLarge;
+    if (CHANGE != Change::kCapped && __builtin_amdgcn_ballot_w64(large)) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) s[t] = large ? s[t] * c : s[t];
         c = large ? 1.0f : c;
@@ -246,7 +246,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
 // more a wave is 0.8, 1.6 and 2.3 us in heads of 64, 128 and 256.  Prompts by instruction
 // issue: three of up to 2500 tokens behind prefixes, 16 heads of 64 on 2, float16, capped,
 // 47 to 52 us in tiles of 32 rows.
-template <typename E, int D, int C, bool CHANGE, bool ONCE>
+template <typename E, int D, int C, Change CHANGE, bool ONCE>
 __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) void attend16_kernel(
     AttendParams p) {
     constexpr int kRows = 16 * C;
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
 
     RowState<D> st[C];
     Queries<D> q[C];
-    const Change change = {p.cap_log2, p.cap_inverse, p.slopes != nullptr};
+    const Cap cap = {p.cap_log2, p.cap_inverse};
     Slope slope[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         q[c].load((const uint16_t *)p.q + (int64_t)(seq.start + i[c]) * p.q_token +
                       (int64_t)hq[c] * p.q_head,
                   mine[c], g);
-        if constexpr (CHANGE) {
+        if constexpr (CHANGE == Change::kAny) {
             slope[c].set(p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
                          seq.length - seq.queries + i[c]);
         }
@@ -407,25 +407,23 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         float scale = score_factor<E>(p.scale_log2, km);
         float offset = 0.0f;
-        if constexpr (CHANGE) {
-            const auto all = [&](auto f) {
+        const auto all = [&](auto f) {
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int t = 0; t < S::kTiles; ++t)
+                for (int t = 0; t < S::kTiles; ++t)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) s[c][t][k] = f(s[c][t][k], c, 16 * t + k);
-            };
-            if (change.cap > 0.0f)
-                change.limit(scale, offset,
-                             [&](auto f) { all([&](float x, int, int) { return f(x); }); });
-            if (change.sloped) {
-                float far[C];
+                    for (int k = 0; k < 4; ++k) s[c][t][k] = f(s[c][t][k], c, 16 * t + k);
+        };
+        if (CHANGE == Change::kCapped || (CHANGE == Change::kAny && cap.cap > 0.0f))
+            cap.limit<CHANGE>(scale, offset,
+                              [&](auto f) { all([&](float x, int, int) { return f(x); }); });
+        if (CHANGE == Change::kAny && p.slopes) {
+            float far[C];
 #pragma unroll
-                for (int c = 0; c < C; ++c) far[c] = slope[c].from(t0 + 4 * g);
-                all([&](float x, int c, int j) { return slope[c](x * scale, far[c] - (float)j); });
-                scale = 1.0f;
-            }
+            for (int c = 0; c < C; ++c) far[c] = slope[c].from(t0 + 4 * g);
+            all([&](float x, int c, int j) { return slope[c](x * scale, far[c] - (float)j); });
+            scale = 1.0f;
         }
         if (masked) {
 #pragma unroll
@@ -443,7 +441,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) weigh<E, D, S::kTiles>(st[c], s[c], w[c], scale, offset, kind, taken);
+        for (int c = 0; c < C; ++c) weigh<E, D, CHANGE, S::kTiles>(st[c], s[c], w[c], scale, offset, kind, taken);
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
@@ -559,10 +557,10 @@ namespace {
 
 template <typename E, int D, int C, bool ONCE>
 void launch_c(const AttendParams &p, dim3 grid, hipStream_t s) {
-    if (p.slopes || p.cap_log2 > 0.0f)
-        hipLaunchKernelGGL((attend16_kernel<E, D, C, true, ONCE>), grid, dim3(kThreads), 0, s, p);
-    else
-        hipLaunchKernelGGL((attend16_kernel<E, D, C, false, ONCE>), grid, dim3(kThreads), 0, s, p);
+    by_change(p, [&](auto kind) {
+        hipLaunchKernelGGL((attend16_kernel<E, D, C, decltype(kind)::value, ONCE>), grid,
+                           dim3(kThreads), 0, s, p);
+    });
 }
 
 template <typename E, int D>
