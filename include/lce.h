@@ -625,8 +625,8 @@ lce_status lce_kv8_workspace_size(const lce_kv8_cache_desc *desc, const lce_kv8_
  * prefix[b] (causal) or anywhere in the sequence (not causal), and j > p - window where
  * there is a window.  Sums, scores, the running maximum and the running sum are
  * float32; softmax weights are rounded to `type` where they multiply the values, or, where
- * a sequence has up to 8 rows of a cache head, split into two of that type (float16: with a
- * last place of at most 2^-31 of a row's largest weight), and out is
+ * max_q (0: the mean) new tokens make up to 8 rows of a cache head, split into two of that
+ * type (float16: with a last place of at most 2^-31 of a row's largest weight), and out is
  * rounded to it once (float16: what is past 65504 to that).  With LCE_FLOAT16, keys are
  * multiplied as multiples of 2^-32 times the largest scale of their page, or of less,
  * values as multiples of 2^-32 times the largest scale that a row's sequence has: this

@@ -98,7 +98,8 @@ int64_t most_pages(const lce_kv8_query_desc &q, bool prefix) {
 // The most rows that read the same pages, as far as the call says: the new tokens of a
 // sequence times the heads that share a cache head.
 int64_t query_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
-    return (int64_t)(q.max_q > 0 ? q.max_q : q.tokens / q.seqs) * (q.q_heads / d.kv_heads);
+    return (q.max_q > 0 ? q.max_q : ((int64_t)q.tokens + q.seqs - 1) / q.seqs) *
+           (q.q_heads / d.kv_heads);
 }
 
 // Query rows of a tile.  In tiles of 128 rows a page's codes become two-byte floats once
@@ -366,7 +367,8 @@ lce_status lce_kv8_attention(const lce_kv8_cache_desc *desc, const void *cache,
     if (rows == 128)
         lce::kv8::launch_attend128(p, query->type, desc->head_dim, grid, stream);
     else
-        lce::kv8::launch_attend16(p, query->type, desc->head_dim, rows, once, grid, stream);
+        lce::kv8::launch_attend16(p, query->type, desc->head_dim, rows, !several, once, grid,
+                                   stream);
     return check_launch("lce_kv8_attention launch");
 }
 

@@ -76,10 +76,10 @@ __device__ __forceinline__ Span visible(const Sequence &s, int i, int causal, in
 
 void launch_append(const AppendParams &p, int type, int dim, hipStream_t s);
 void launch_read(const ReadParams &p, int type, int dim, hipStream_t s);
-// 16 or 32 query rows a workgroup; grid = (tiles * kv_heads, splits); once: loads past
-// the caches
-void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool once, dim3 grid,
-                     hipStream_t s);
+// 16 or 32 query rows a workgroup; grid = (tiles * kv_heads, splits); few: rows of a sequence
+// and head; once (of few): loads past the caches
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool few, bool once,
+                     dim3 grid, hipStream_t s);
 // 128 query rows a workgroup, heads of up to 128; grid = (tiles * kv_heads, splits)
 void launch_attend128(const AttendParams &p, int type, int dim, dim3 grid, hipStream_t s);
 

@@ -90,8 +90,8 @@ __device__ __forceinline__ float add_rounded(F16, uint32_t w, float sum) {
 }
 
 // What a call does to scores between their product and the softmax: nothing, a cap of up to
-// kNearCap by itself, or a cap, a bias by distance or both.  (The second has a kernel of its own
-// because values that several branches make are copied where these meet: prompts in tiles
+// kNearCap by itself, or a cap, a bias by distance or both.  (The second has a kernel of its
+// own because values that several branches make are copied where these meet: prompts in tiles
 // of 32 rows @A@ us without one, @B@ with.)
 enum class Change { kNone, kCapped, kAny };
 constexpr float kNearCap = 256.0f;         // log2 units

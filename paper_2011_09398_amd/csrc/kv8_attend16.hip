@@ -28,10 +28,10 @@ struct Step {
 
 // Half a page where the codes of a whole one would leave too few registers for what else
 // there is: wide heads (of 128: 67 us against 87 of 48 sequences of up to 8192 tokens, when
-// keys did not come through LDS yet), and 32 rows of 64 with scores to change (47 against 50
-// us of the prompts below; without, 41 against 37).
+// keys did not come through LDS yet), and 32 rows of 64 with a bias (50 against 55 us of the
+// prompts below, if they had one and no cap; with their cap 49.5 against 46.6).
 template <int D, int C, Change CHANGE>
-constexpr int kTilesOf = D <= 64 && !(C == 2 && CHANGE != Change::kNone) ? 4 : 2;
+constexpr int kTilesOf = D <= 64 && !(C == 2 && CHANGE == Change::kAny) ? 4 : 2;
 
 // Key codes of a step as they come from memory, whole lines of it: 16 bytes a lane at a
 // time, pieces lane, lane + 64 .. of the step's.  The wave's own part of LDS turns them into
@@ -129,16 +129,14 @@ struct Shared {
 };
 
 // What a weight's rounding does to results shows most in rows that go by few tokens, and in
-// calls of few rows.  In tiles of up to 8 rows of a sequence that has no more than 64, the
-// products' other eight columns, lanes n >= 8, take what is left of each weight once its
-// leading bits, kCut, are cut off: results are as with float32 weights (errors against 64 bits
-// 1.0 times those of rounding the result, with rounded weights 1.2 and up to 1.9; 0 to 1 % of
-// a decoding step's time).  In its taller tiles they are divided by the sum of the rounded
-// weights, so that a row that goes by one token has that token's values.  In the many rows of a
-// prompt they are divided by the sum itself: the other would take 4 % of them in tiles of 16
-// rows, 3 of 32, 7 of 128.
-enum class Weights { kPlain, kRounded, kPaired };
-
+// calls of few rows (FEW: up to 64 of a sequence and cache head).  In tiles of up to 8 rows
+// of such calls, the products' other eight columns, lanes n >= 8, take what is left of each
+// weight once its leading bits, kCut, are cut off: results are as with float32 weights (errors
+// against 64 bits 1.0 times those of rounding the result, with rounded weights 1.2 and up to
+// 1.9; 0 to 2 % of a decoding step's time).  In their taller tiles they are divided by the sum
+// of the rounded weights, so that a row that goes by one token has that token's values.  In
+// the many rows of a prompt they are divided by the sum itself: the other would take 4 % of
+// them in tiles of 16 rows, 3 of 32, 7 of 128.
 // The bits of a float32 that are an E::T's.
 template <typename E>
 constexpr uint32_t kCut = __is_same(E, F16) ? 0xFFFFE000u : 0xFFFF0000u;
@@ -158,9 +156,9 @@ __device__ __forceinline__ uint32_t cut_pair(float x, float y) {
 
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
 // Scores times c, plus `offset`, are in log2 units.
-template <typename E, int D, Change CHANGE, int kTiles>
+template <typename E, int D, Change CHANGE, bool FEW, int kTiles>
 __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4 (&p)[kTiles / 2],
-                                      float c, float offset, Weights kind, uint32_t taken) {
+                                      float c, float offset, bool paired, uint32_t taken) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -206,11 +204,11 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
             for (int i = 0; i < 2; ++i)
                 p[t / 2][t % 2 * 2 + i] = f(w[t][2 * i], w[t][2 * i + 1]);
     };
-    if (kind == Weights::kPaired) {
+    if (FEW && paired) {
         pairs([&](float x, float y) { return cut_pair<E>(x - cut(x, taken), y - cut(y, taken)); });
     } else {
         pairs([](float x, float y) { return pack_pair<E>(x, y); });
-        if (kind == Weights::kRounded) {
+        if constexpr (FEW) {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -219,7 +217,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
         }
     }
     st.l += sum;
-    st.divisor += kind == Weights::kRounded ? rounded : sum;
+    st.divisor += FEW && !paired ? rounded : sum;
 }
 
 }  // namespace
@@ -245,8 +243,8 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
 // states in) where it does not: one of 30011, 32 heads of 128 on 8 (61 MB) 18 us.  A page
 // more a wave is 0.8, 1.6 and 2.3 us in heads of 64, 128 and 256.  Prompts by instruction
 // issue: three of up to 2500 tokens behind prefixes, 16 heads of 64 on 2, float16, capped,
-// 47 to 52 us in tiles of 32 rows.
-template <typename E, int D, int C, Change CHANGE, bool ONCE>
+// 42 to 47 us in tiles of 32 rows.
+template <typename E, int D, int C, Change CHANGE, bool FEW, bool ONCE>
 __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) void attend16_kernel(
     AttendParams p) {
     constexpr int kRows = 16 * C;
@@ -277,11 +275,9 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
     const int row0 = tile * kRows;
     const int valid = min(rows - row0, kRows);
     const int prefix = p.prefix ? p.prefix[seq.index] : 0;
-    const Weights kind = C > 1 || rows > 64 ? Weights::kPlain
-                         : valid <= 8       ? Weights::kPaired
-                                            : Weights::kRounded;
-    const uint32_t taken = kind == Weights::kPaired && n >= 8 ? kCut<E> : 0u;
-    const int nr = kind == Weights::kPaired ? n & 7 : n;
+    const bool paired = FEW && valid <= 8;
+    const uint32_t taken = paired && n >= 8 ? kCut<E> : 0u;
+    const int nr = paired ? n & 7 : n;
     // this lane's row of each sixteen
     int i[C], hq[C];
     bool mine[C];
@@ -441,7 +437,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) weigh<E, D, CHANGE, S::kTiles>(st[c], s[c], w[c], scale, offset, kind, taken);
+        for (int c = 0; c < C; ++c) weigh<E, D, CHANGE, FEW, S::kTiles>(st[c], s[c], w[c], scale, offset, paired, taken);
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
@@ -520,7 +516,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
             l += ml[1] * f;
             divisor += ml[2] * f;
             f32x4 x = sh.o[w][quad][r];
-            if (kind == Weights::kPaired) x += sh.o[w][quad][r + 8];
+            if (paired) x += sh.o[w][quad][r + 8];
             o += x * (f * relative(sh.scale[w], most, 0));
         }
         if (splits == 1) {
@@ -555,36 +551,38 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
 
 namespace {
 
-template <typename E, int D, int C, bool ONCE>
+template <typename E, int D, int C, bool FEW, bool ONCE>
 void launch_c(const AttendParams &p, dim3 grid, hipStream_t s) {
     by_change(p, [&](auto kind) {
-        hipLaunchKernelGGL((attend16_kernel<E, D, C, decltype(kind)::value, ONCE>), grid,
+        hipLaunchKernelGGL((attend16_kernel<E, D, C, decltype(kind)::value, FEW, ONCE>), grid,
                            dim3(kThreads), 0, s, p);
     });
 }
 
 template <typename E, int D>
-void launch_d(const AttendParams &p, int rows, bool once, dim3 grid, hipStream_t s) {
+void launch_d(const AttendParams &p, int rows, bool few, bool once, dim3 grid, hipStream_t s) {
     if constexpr (D <= 128) {
-        if (rows == 32) return launch_c<E, D, 2, false>(p, grid, s);
+        if (rows == 32) return launch_c<E, D, 2, false, false>(p, grid, s);
     }
-    if (once) return launch_c<E, D, 1, true>(p, grid, s);
-    launch_c<E, D, 1, false>(p, grid, s);
+    if (once) return launch_c<E, D, 1, true, true>(p, grid, s);
+    if (few) return launch_c<E, D, 1, true, false>(p, grid, s);
+    launch_c<E, D, 1, false, false>(p, grid, s);
 }
 
 template <typename E>
-void launch_t(const AttendParams &p, int dim, int rows, bool once, dim3 grid, hipStream_t s) {
-    if (dim == 64) launch_d<E, 64>(p, rows, once, grid, s);
-    else if (dim == 128) launch_d<E, 128>(p, rows, once, grid, s);
-    else launch_d<E, 256>(p, rows, once, grid, s);
+void launch_t(const AttendParams &p, int dim, int rows, bool few, bool once, dim3 grid,
+              hipStream_t s) {
+    if (dim == 64) launch_d<E, 64>(p, rows, few, once, grid, s);
+    else if (dim == 128) launch_d<E, 128>(p, rows, few, once, grid, s);
+    else launch_d<E, 256>(p, rows, few, once, grid, s);
 }
 
 }  // namespace
 
-void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool once, dim3 grid,
-                     hipStream_t s) {
-    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, rows, once, grid, s);
-    else launch_t<Bf16>(p, dim, rows, once, grid, s);
+void launch_attend16(const AttendParams &p, int type, int dim, int rows, bool few, bool once,
+                     dim3 grid, hipStream_t s) {
+    if (type == LCE_FLOAT16) launch_t<F16>(p, dim, rows, few, once, grid, s);
+    else launch_t<Bf16>(p, dim, rows, few, once, grid, s);
 }
 
 }  // namespace kv8
