@@ -111,19 +111,19 @@ int64_t query_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
 // than registers.  Measured in graphs (us, tiles of 16 / 32 / 128; 32 heads on 8 if not said
 // otherwise; the last two columns float16):
 //                                          128 channels      64 channels      128, capped
-//   16 of 4064 tokens, 64 of them new      48 / 55 / 99      29 / 38 / 80     54 / 65 / 140
-//   one of 5024, 1024 new                 142 / 111 / 121    81 / 65 / 97    165 / 136 / 169
-//   one of 6048, 2048 new                 279 / 222 / 183   162 / 123 / 129  336 / 287 / 246
-//   one of 8096, 4096 new                 640 / 512 / 413   366 / 277 / 286  769 / 660 / 558
-//   four of up to 4512, up to 512 new      86 / 75 / 111     52 / 41 / 89    100 / 91 / 157
-//   four of up to 5024, up to 1024 new    166 / 137 / 126   101 / 76 / 100   205 / 173 / 173
-//   four of up to 6048, up to 2048 new    330 / 272 / 206   197 / 149 / 145  391 / 342 / 280
-//   16 of up to 1024, up to 128 new        34 / 34 / 33      25 / 22 / 26     38 / 38 / 46
-//   one prompt of 1024                     29 / 28 / 31      21 / 20 / 25     34 / 32 / 44
-//   one prompt of 2048                     81 / 71 / 61      50 / 40 / 47     93 / 83 / 84
-//   two of up to 5025, 359 new, 8 on 2     30 / 31 / 60      18 / 20 / 40     35 / 37 / 70
-//   four prompts of up to 1943, 2 on 1     19 / 23 / 49      12 / 16 / 31     22 / 28 / 54
-//   three prompts of up to 2500, 16 on 2   66 / 62 / 67      45 / 37 / 54     81 / 74 / 94
+//   16 of 4064 tokens, 64 of them new      48 / 55 / 99      29 / 38 / 80     54 / 65 / 130
+//   one of 5024, 1024 new                 142 / 111 / 121    81 / 65 / 97    158 / 130 / 157
+//   one of 6048, 2048 new                 279 / 222 / 183   162 / 123 / 129  324 / 274 / 238
+//   one of 8096, 4096 new                 640 / 512 / 413   366 / 277 / 286  767 / 627 / 531
+//   four of up to 4512, up to 512 new      86 / 75 / 111     52 / 41 / 89    98 / 88 / 146
+//   four of up to 5024, up to 1024 new    166 / 137 / 126   101 / 76 / 100   190 / 165 / 162
+//   four of up to 6048, up to 2048 new    330 / 272 / 206   197 / 149 / 145  390 / 325 / 269
+//   16 of up to 1024, up to 128 new        34 / 34 / 33      25 / 22 / 26     36 / 37 / 43
+//   one prompt of 1024                     29 / 28 / 31      21 / 20 / 25     33 / 32 / 41
+//   one prompt of 2048                     81 / 71 / 61      50 / 40 / 47     91 / 80 / 80
+//   two of up to 5025, 359 new, 8 on 2     30 / 31 / 60      18 / 20 / 40     32 / 36 / 67
+//   four prompts of up to 1943, 2 on 1     19 / 23 / 49      12 / 16 / 31     20 / 26 / 51
+//   three prompts of up to 2500, 16 on 2   66 / 62 / 67      45 / 37 / 54     78 / 70 / 88
 int tile_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
     if (d.head_dim > 128) return 16;
     const int forced = tuning(LCE_TUNE_KV8_ROWS);

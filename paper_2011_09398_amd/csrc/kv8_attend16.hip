@@ -236,9 +236,9 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
 // the values against the largest that the wave has seen.
 //
 // Bound by memory where a call reads much: 48 sequences of up to 8192 tokens, 32 heads of
-// 128 on 8, bfloat16 (265 MB) 58 us, 4.5 TB/s with the launch (a large copy 4.8 to 5.4, by
-// the card); 24 of up to 4001, 32 heads of 64 on 32 with a bias (170 MB) 36 us; 16 with 4
-// drafted tokens and a window of 4096, 16 heads of 256 on 8, float16, capped (191 MB) 45 us.
+// 128 on 8, bfloat16 (265 MB) 60 us, 4.4 TB/s with the launch (a large copy 4.8 to 5.4, by
+// the card); 24 of up to 4001, 32 heads of 64 on 32 with a bias (170 MB) 37 us; 16 with 4
+// drafted tokens and a window of 4096, 16 heads of 256 on 8, float16, capped (191 MB) 44 us.
 // By latencies in a row (launch, lengths, table, a page, the states out, the ticket, the
 // states in) where it does not: one of 30011, 32 heads of 128 on 8 (61 MB) 18 us.  A page
 // more a wave is 0.8, 1.6 and 2.3 us in heads of 64, 128 and 256.  Prompts by instruction
