@@ -155,7 +155,8 @@ struct Slope {
 };
 
 // A split's state in the workspace: of each row its maximum and its sum of weights, the scale
-// byte of its sums of values and what they are divided by, then the sums of four channels at a time, `rows` rows next to each other.
+// byte of its sums of values and what they are divided by, then the sums of four channels at a
+// time, `rows` rows next to each other.
 template <int D, int ROWS>
 struct Part {
     static constexpr int kFloats = ROWS * (D + 4);

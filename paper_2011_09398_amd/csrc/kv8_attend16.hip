@@ -110,8 +110,9 @@ struct Queries {
     }
 };
 
-// A row's state: running maximum of scores (log2), this lane's share of the sum and
-// of what results are divided by, and the sums of weighted values: o[4c + x][i] of lane (n, g) is row n, channel 64c + 16g + 4i + x.
+// A row's state: running maximum of scores (log2), this lane's share of the sum and of what
+// results are divided by, and the sums of weighted values: o[4c + x][i] of lane (n, g) is row n,
+// channel 64c + 16g + 4i + x.
 template <int D>
 struct RowState {
     float m, l, divisor;
@@ -437,7 +438,8 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         }
         u32x4 w[C][S::kTiles / 2];
 #pragma unroll
-        for (int c = 0; c < C; ++c) weigh<E, D, CHANGE, FEW, S::kTiles>(st[c], s[c], w[c], scale, offset, paired, taken);
+        for (int c = 0; c < C; ++c)
+            weigh<E, D, CHANGE, FEW, S::kTiles>(st[c], s[c], w[c], scale, offset, paired, taken);
         if (vm > biggest) {
             const float f = relative(biggest, vm, 0);
             biggest = vm;
