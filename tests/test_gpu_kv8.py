@@ -265,6 +265,43 @@ def test_every_schedule(dim, dtype, rows, chunk):
         assert name.startswith("kv8-") and name.endswith("-split") == split
 
 
+def launched(length, queries, heads, kv_heads, dim, rows=0, seqs=1, **kw):
+    """The schedule of a call over an empty table (every page is outside the cache), and that
+    its rows see nothing."""
+    cache = lce.KV8Cache(kv_heads, dim, pages=1)
+    table = torch.full((seqs, -(-length // 64)), -1, dtype=torch.int32, device="cuda")
+    start = torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * queries
+    q = torch.randn(seqs * queries, heads, dim, device="cuda").bfloat16()
+    with lce.tuning(kv8_rows=rows):
+        out, lse = lce.kv8_attention(cache, q, table, start, torch.full_like(start[1:], length),
+                                     return_lse=True, **kw)
+    assert not out.any() and torch.isneginf(lse).all()
+    return lce.last_schedule()
+
+
+def test_the_rule_for_heights():
+    for rows in (16, 32, 128):
+        assert launched(70, 3, 4, 2, 64, rows=rows) == f"kv8-{rows}"
+        assert launched(70, 3, 4, 2, 256, rows=rows) == "kv8-16"      # no other has a kernel
+    # one token each, a few tokens, long sequences
+    assert launched(100, 1, 8, 2, 128, seqs=3) == "kv8-16"
+    assert launched(20000, 1, 8, 2, 128) == "kv8-16-split"
+    assert launched(300, 5, 24, 4, 64, seqs=4).startswith("kv8-16")
+    # 512 tiles of 128 rows, of 64 channels 2048
+    assert launched(2048, 2048, 32, 8, 128) == "kv8-128"
+    assert launched(2047, 2047, 32, 8, 128) == "kv8-32"
+    assert launched(8192, 8192, 32, 8, 64) == "kv8-128"
+    assert launched(2048, 2048, 32, 8, 64) == "kv8-32"
+    # 1024 tiles of 32
+    assert launched(1024, 1024, 32, 8, 128).startswith("kv8-32")
+    assert launched(1023, 1023, 32, 8, 128).startswith("kv8-16")
+    # rows that share pages: 128 of them, 256
+    assert launched(1000, 32, 32, 8, 128, seqs=80).startswith("kv8-128")
+    assert launched(1000, 31, 32, 8, 128, seqs=80).startswith("kv8-16")
+    assert launched(1000, 64, 32, 8, 128, seqs=16).startswith("kv8-32")
+    assert launched(1000, 63, 32, 8, 128, seqs=17).startswith("kv8-16")
+
+
 def test_longest_hints_and_workspaces():
     batch = ref.Batch(3, [2000, 77, 640], [1, 1, 3], 8, 2, 128, "bf16")
     cache, q, table, start, lengths = batch.device(lce)
