@@ -90,10 +90,11 @@ __device__ __forceinline__ float add_rounded(F16, uint32_t w, float sum) {
 }
 
 // What a call does to scores between their product and the softmax: nothing, a cap of up to
-// kNearCap by itself, or a cap, a bias by distance or both.  (The second has a kernel of its
-// own because values that several branches make are copied where these meet: prompts in tiles
-// of 32 rows @A@ us without one, @B@ with.)
-enum class Change { kNone, kCapped, kAny };
+// kNearCap, a bias by distance, or another cap or both.  (The first three have kernels of their
+// own because values that several branches make are copied where these meet: the prompts of
+// the 16-row kernel's comment 52 us in the last's, 47 in their own.)
+enum class Change { kNone, kCapped, kSloped, kAny };
+constexpr bool has_slopes(Change c) { return c == Change::kSloped || c == Change::kAny; }
 constexpr float kNearCap = 256.0f;         // log2 units
 static_assert(kNearCap + kLag + F16::kLift < kLarge, "capped scores are not large");
 
@@ -257,7 +258,8 @@ struct ChangeOf {
 
 template <typename Launch>
 void by_change(const AttendParams &p, Launch launch) {
-    if (p.slopes || p.cap_log2 > kNearCap) launch(ChangeOf<Change::kAny>());
+    if (p.slopes && p.cap_log2 == 0.0f) launch(ChangeOf<Change::kSloped>());
+    else if (p.slopes || p.cap_log2 > kNearCap) launch(ChangeOf<Change::kAny>());
     else if (p.cap_log2 > 0.0f) launch(ChangeOf<Change::kCapped>());
     else launch(ChangeOf<Change::kNone>());
 }

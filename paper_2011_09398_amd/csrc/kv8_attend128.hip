@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
            mine, h);
     const Cap cap = {p.cap_log2, p.cap_inverse};
     Slope slope;
-    if constexpr (CHANGE == Change::kAny)
+    if constexpr (has_slopes(CHANGE))
         slope.set(p.slopes && mine ? p.slopes[hq] : 0.0f, seq.length - seq.queries + i);
 
     // the state of a row: running maximum (log2), this lane's share of the sum, sums of
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         if (CHANGE == Change::kCapped || (CHANGE == Change::kAny && cap.cap > 0.0f))
             cap.limit<CHANGE>(by, offset,
                               [&](auto f) { all([&](float x, int) { return f(x); }); });
-        if (CHANGE == Change::kAny && p.slopes) {
+        if (CHANGE == Change::kSloped || (CHANGE == Change::kAny && p.slopes)) {
             const float far = slope.from(t0 + 4 * h);
             all([&](float x, int j) { return slope(x * by, far - (float)j); });
             by = 1.0f;

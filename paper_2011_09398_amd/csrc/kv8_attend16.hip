@@ -28,8 +28,8 @@ struct Step {
 
 // Half a page where the codes of a whole one would leave too few registers for what else
 // there is: wide heads (of 128: 67 us against 87 of 48 sequences of up to 8192 tokens, when
-// keys did not come through LDS yet), and 32 rows of 64 with a bias (50 against 55 us of the
-// prompts below, if they had one and no cap; with their cap 49.5 against 46.6).
+// keys did not come through LDS yet), and 32 rows of 64 with a cap and a bias (62 against 63
+// us of the prompts below, if they had a bias; with their cap alone 49.5 against 46.6).
 template <int D, int C, Change CHANGE>
 constexpr int kTilesOf = D <= 64 && !(C == 2 && CHANGE == Change::kAny) ? 4 : 2;
 
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         q[c].load((const uint16_t *)p.q + (int64_t)(seq.start + i[c]) * p.q_token +
                       (int64_t)hq[c] * p.q_head,
                   mine[c], g);
-        if constexpr (CHANGE == Change::kAny) {
+        if constexpr (has_slopes(CHANGE)) {
             slope[c].set(p.slopes && mine[c] ? p.slopes[hq[c]] : 0.0f,
                          seq.length - seq.queries + i[c]);
         }
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         if (CHANGE == Change::kCapped || (CHANGE == Change::kAny && cap.cap > 0.0f))
             cap.limit<CHANGE>(scale, offset,
                               [&](auto f) { all([&](float x, int, int) { return f(x); }); });
-        if (CHANGE == Change::kAny && p.slopes) {
+        if (CHANGE == Change::kSloped || (CHANGE == Change::kAny && p.slopes)) {
             float far[C];
 #pragma unroll
             for (int c = 0; c < C; ++c) far[c] = slope[c].from(t0 + 4 * g);
