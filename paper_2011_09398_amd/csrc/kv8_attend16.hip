@@ -155,6 +155,12 @@ __device__ __forceinline__ uint32_t cut_pair(float x, float y) {
         return __builtin_amdgcn_perm(bits_as<uint32_t>(y), bits_as<uint32_t>(x), 0x07060302u);
 }
 
+// How far under the largest score (log2) weights are taken.  What is cut off of float16's
+// smallest numbers is a whole last place, and not half of one: where weights are cut, the
+// largest is 2^3 as large, for a maximum that moves a little more often.
+template <typename E, bool FEW>
+constexpr float kUnder = E::kLift + (FEW && E::kLift > 0.0f ? 3.0f : 0.0f);
+
 // A step's scores into the rows' maximum and sum; its weights, ready to be multiplied.
 // Scores times c, plus `offset`, are in log2 units.
 template <typename E, int D, Change CHANGE, bool FEW, int kTiles>
@@ -170,7 +176,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
     // its own maximum, so that no bit of it depends on the rows beside it.)
     if (__builtin_amdgcn_ballot_w64(top - st.m > kLag + E::kLift)) {
         const float high = across_rows(top, [](float a, float b) { return fmaxf(a, b); });
-        const float all = high - st.m > kLag + E::kLift ? high - E::kLift : st.m;
+        const float all = high - st.m > kLag + E::kLift ? high - kUnder<E, FEW> : st.m;
         const float f = __builtin_amdgcn_exp2f(st.m - all);
         st.m = all;
         st.l *= f;

@@ -1,4 +1,6 @@
 """The 8-bit cache's operators on the GPU against their definitions in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -410,6 +412,28 @@ def test_largest_values_stay_finite():
                 out = lce.kv8_attention(s.handle, q, *args).double()
             assert torch.isfinite(out).all()
             assert ((out / held - 1).abs() <= 4 * ref.HALF_ULP[dtype]).all()
+
+
+@pytest.mark.parametrize("queries", [1, 9, 80])
+@pytest.mark.parametrize("under", [30.1, 31.6, 27.3])
+def test_float16_weights_far_under_the_largest(queries, under):
+    """A token of weight 1 and value 0, and many of weight 2^-under and value 1: weights have a
+    last place of 2^-31 of the largest, of which half is lost."""
+    n, dim = 20000, 64
+    cache = lce.KV8Cache(1, dim, pages=-(-n // 64))
+    table = torch.arange(cache.pages, dtype=torch.int32, device="cuda")[None]
+    k, v = torch.zeros(n, 1, dim).half(), torch.ones(n, 1, dim).half()
+    k[0, 0, 0], v[0] = 16, 0
+    length = torch.tensor([n], dtype=torch.int32).cuda()
+    lce.kv8_append(cache, k.cuda(), v.cuda(), table, torch.tensor([0, n]).int().cuda(), length)
+    q = torch.zeros(queries, 1, dim).half()
+    q[:, 0, 0] = 16
+    out = lce.kv8_attention(cache, q.cuda(), table, torch.tensor([0, queries]).int().cuda(), length,
+                            scale=under * math.log(2) / 256, causal=False)
+    want = (n - 1) * 2.0 ** -under / (1 + (n - 1) * 2.0 ** -under)
+    # scores of 22 in float32 are off by 2^-20 or less, the result by half a step of 2^-24
+    bound = n * 2.0 ** -32 + want * 2.0 ** -11 + 2.0 ** -25
+    assert (out.double().cpu() - want).abs().max().item() <= bound
 
 
 @pytest.mark.parametrize("rows", [16, 32, 128])
