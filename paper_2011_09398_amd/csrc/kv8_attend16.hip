@@ -138,6 +138,7 @@ struct Shared {
 // of the rounded weights, so that a row that goes by one token has that token's values.  In
 // the many rows of a prompt they are divided by the sum itself: the other would take 4 % of
 // them in tiles of 16 rows, 3 of 32, 7 of 128.
+
 // The bits of a float32 that are an E::T's.
 template <typename E>
 constexpr uint32_t kCut = __is_same(E, F16) ? 0xFFFFE000u : 0xFFFF0000u;
