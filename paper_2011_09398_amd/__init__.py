@@ -1474,11 +1474,9 @@ def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=No
             shape, y = k.shape, k.stride()
     if (n | heads) >> 31 or k is not None and shape[1] >> 31:
         _int32_refused(tokens=n, heads=heads if k is None else max(heads, shape[1]))
-    second = None
     if out is None:
-        first = _empty_rows(plan, q)
-        if k is not None:
-            second = _empty_rows(plan, k)
+        first = plan._empty_like(q)
+        second = None if k is None else plan._empty_like(k)
     elif k is None:
         first = _rotary_out(q, out, "q")
     else:
@@ -1486,22 +1484,22 @@ def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=No
             raise ValueError("out must be a pair of tensors")
         first, second = _rotary_out(q, out[0], "q"), _rotary_out(k, out[1], "k")
     to = first.stride()
+    if to[2] != 1 and out is None:          # like a q whose channels are not next to each other
+        first = q.new_empty(q.shape)
+        to = first.stride()
     qr = _pack_rotary_rows(heads, q.data_ptr(), first.data_ptr(), x[0], x[1], to[0], to[1])
     kr = None
     if k is not None:
         to = second.stride()
+        if to[2] != 1 and out is None:
+            second = k.new_empty(k.shape)
+            to = second.stride()
         kr = _pack_rotary_rows(shape[1], k.data_ptr(), second.data_ptr(), y[0], y[1], to[0], to[1])
     _launch(plan._index, lib().lce_rotary,
             _pack_rotary(n, dim, plan.rot_dim, code, plan._interleaved, 1 if backward else 0,
                          plan.scale),
             plan._turns_ptr, positions.data_ptr(), qr, kr, _stream_of(plan._index))
     return first if k is None else (first, second)
-
-
-def _empty_rows(plan, t):
-    """A tensor like t with contiguous channels."""
-    out = plan._empty_like(t)
-    return out if out.stride(2) == 1 else t.new_empty(t.shape)
 
 
 class PreparedBitpack:
