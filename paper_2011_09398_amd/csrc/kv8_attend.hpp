@@ -34,10 +34,13 @@ __device__ __forceinline__ float relative(int e, int of, int up) {
 }
 
 // What the scores of keys whose largest scale byte is `most` are multiplied by: finite, so
-// that a score of 0 stays one.
+// that a score of 0 stays one, and more than 0, so that a hidden token's of -infinity does.
+// (2^-149 at least, which is within 2^-21 of what any finite score times less would be.
+// Positive floats are in the order of their bits.)
 template <typename E>
 __device__ __forceinline__ float score_factor(float scale_log2, int most) {
-    return __builtin_fminf(__builtin_amdgcn_ldexpf(scale_log2, most - 127 - kUp<E>), __FLT_MAX__);
+    const float f = __builtin_amdgcn_ldexpf(scale_log2, most - 127 - kUp<E>);
+    return bits_as<float>(clampi(bits_as<int>(f), 1, 0x7F7FFFFF));
 }
 
 // The scale bytes (byte i: block i) of a page of which some row sees tokens [lo, hi):
