@@ -43,6 +43,17 @@ __device__ __forceinline__ float score_factor(float scale_log2, int most) {
     return bits_as<float>(clampi(bits_as<int>(f), 1, 0x7F7FFFFF));
 }
 
+// Two query channels of type E::T, infinities as NaNs: an infinity times a key is one or the
+// other infinity, which as a score may be below all (and weigh nothing) or be capped, a NaN
+// makes its row one whatever it is multiplied by.
+template <typename E>
+__device__ __forceinline__ uint32_t without_infinities(uint32_t w) {
+    constexpr uint32_t exponents = __is_same(E, F16) ? 0x7C007C00u : 0x7F807F80u;
+    constexpr uint32_t one = __is_same(E, F16) ? 0x04000400u : 0x00800080u;
+    constexpr int quiet = __is_same(E, F16) ? 6 : 9;        // the mantissa's highest bit
+    return w | ((((w & exponents) + one) >> quiet) & (0x80008000u >> quiet));
+}
+
 // The scale bytes (byte i: block i) of a page of which some row sees tokens [lo, hi):
 // blocks that no row sees weigh next to nothing, whatever their bytes are.
 __device__ __forceinline__ uint32_t settled_scales(uint32_t scales, int lo, int hi) {

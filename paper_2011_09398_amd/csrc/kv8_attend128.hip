@@ -80,6 +80,13 @@ struct Queries {
             if (valid) q[j] = *reinterpret_cast<const u32x4 *>(row + 16 * j + 8 * h);
         }
     }
+    template <typename E>
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) q[j][x] = without_infinities<E>(q[j][x]);
+    }
 };
 
 __device__ __forceinline__ float across_halves(float x, bool sum) {
@@ -393,6 +400,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         if (number[1] >= 0) values.load(rec[1], wave, r, g);
         if (number[2] >= 0) load_keys(rec[2]);
         else value_scales = scales[1];
+        q.template settle<E>();
         lds_barrier();
 #pragma unroll
         for (int t = 0; t < 2; ++t) {

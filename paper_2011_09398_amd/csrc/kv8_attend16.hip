@@ -108,6 +108,14 @@ struct Queries {
             }
         }
     }
+    template <typename E>
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                q[c][x / 4][x % 4] = without_infinities<E>(q[c][x / 4][x % 4]);
+    }
 };
 
 // A row's state: running maximum of scores (log2), this lane's share of the sum and of what
@@ -367,6 +375,10 @@ __global__ __launch_bounds__(kThreads, D == 64 || (D == 128 && C == 1) ? 3 : 2) 
         scales = *reinterpret_cast<const u32x2 *>(rec + Record<D>::kScale);
         keys.template load<ONCE>(rec, step % S::kPerPage, lane);
         values.template load<ONCE>(rec, step % S::kPerPage, n, g);
+        // (behind the loads: the queries have been on their way since before the page numbers)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < C; ++c) q[c].template settle<E>();
     }
     while (more) {
         const int t0 = step * S::kTokens;

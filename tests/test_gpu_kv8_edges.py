@@ -1,5 +1,5 @@
 """Attention over the 8-bit cache at the ends of what its entry point takes: the smallest
-scales, and calls that the smaller tests do not reach."""
+scales, queries that are not finite, calls that the smaller tests do not reach."""
 import numpy as np
 import pytest
 import torch
@@ -45,3 +45,35 @@ def test_smallest_scales(dim, dtype, scale, rows, zero):
     with lce.tuning(kv8_rows=rows):
         for opts in (dict(), dict(window=20), dict(causal=False)):
             check(batch, scale, **opts)
+
+
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("opts", [dict(), dict(softcap=5.0), dict(softcap=1e6), dict(slopes=True),
+                                  dict(softcap=5.0, slopes=True)], ids=str)
+def test_an_infinity_in_a_query_makes_its_row_nan(dim, dtype, rows, opts):
+    """Also where its products with the keys all are the same infinity, which no score of the
+    row is larger than, or which a cap makes finite; rows beside it stay, and a row that sees
+    nothing is 0."""
+    every = slice(None)
+    odd = [(b, every, every, 7, "k", -1.0) for b in range(3)]
+    batch = ref.Batch(dim + rows, [1, 70, 2], [1, 40, 3], 4, 2, dim, dtype, odd=odd)
+    inf = float("inf")
+    batch.q[0, 0, 7], batch.q[3, 2, 7], batch.q[20, 1, 7], batch.q[33, 3, 7] = inf, inf, -inf, -inf
+    batch.q[41, 0, 7] = inf                        # before the sequence's beginning
+    batch.q[42, 3, 7] = inf
+    if opts.get("slopes"):
+        opts = dict(opts, slopes=torch.tensor([0.5, 0.0, 0.1, 0.25]).cuda())
+    cache, q, table, start, lengths = batch.device(lce)
+    with lce.tuning(kv8_rows=rows):
+        out, lse = lce.kv8_attention(cache, q, table, start, lengths, return_lse=True, **opts)
+        clean = torch.where(torch.isinf(q), 0.0, q)
+        want, want_lse = lce.kv8_attention(cache, clean, table, start, lengths, return_lse=True,
+                                           **opts)
+    bad = torch.zeros(44, 4, dtype=torch.bool, device="cuda")
+    for token, head in ((0, 0), (3, 2), (20, 1), (33, 3), (42, 3)):
+        bad[token, head] = True
+    assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all()
+    assert torch.equal(out[~bad], want[~bad]) and torch.equal(lse[~bad], want_lse[~bad])
+    assert not out[41].any() and torch.isneginf(lse[41]).all()
