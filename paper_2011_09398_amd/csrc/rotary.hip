@@ -270,8 +270,12 @@ lce_status lce_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling,
     double first = 0, last = 1;
     if (scaling == LCE_ROTARY_YARN) {
         const double turn = 2 * M_PI;
-        first = std::fmax(std::floor(r * std::log(original / (32 * turn)) / (2 * std::log(base))), 0);
-        last = std::fmin(std::ceil(r * std::log(original / turn) / (2 * std::log(base))), r - 1);
+        // (past r - 1 for both where every pair turns far more than 32 times: none is slowed)
+        const auto number = [&](double turns) {
+            return r * std::log(original / (turns * turn)) / (2 * std::log(base));
+        };
+        first = std::fmin(std::fmax(std::floor(number(32)), 0), r - 1);
+        last = std::fmin(std::ceil(number(1)), r - 1);
         if (first == last) last += 0.001;
     }
     for (int i = 0; i < rot_dim / 2; ++i) {
