@@ -681,8 +681,9 @@ lce_status lce_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling,
                                   double original, double *freqs, float *scale);
 
 /* The form in which lce_rotary takes frequencies (both host, [count]): turns a position
- * in multiples of 2^-64, whole turns left out, so that position times frequency is exact
- * at any position.
+ * in multiples of 2^-64, whole turns left out.  Frequencies of up to one turn a position are
+ * rounded to the nearest, larger ones to the last place of a 64-bit mantissa; position times
+ * what that leaves is exact.
  * Errors: LCE_EINVAL (null pointer, count < 1, a frequency that is not finite). */
 lce_status lce_rotary_turns(const double *freqs, int32_t count, uint64_t *turns);
 
@@ -711,7 +712,9 @@ typedef struct {
 /* Turn `q`, and `k` unless it is NULL, in one launch.
  *   turns      uint64 [rot_dim/2] (device): see lce_rotary_turns
  *   positions  int64 [tokens] (device), any values
- * Angles are known to 2^-33 turns and products are float32, rounded once to `type`.
+ * Angles of position p are known to 2^-33 + 0.6 |p| 2^-64 turns (frequencies of up to one
+ * turn a position: 2^-32 for the first 2^32 positions), and products are float32, rounded
+ * once to `type`.
  * rot_dim a multiple of 32 bytes, head_dim of 16, and x, y and strides of 16 bytes take
  * the widest loads; others work.
  * tokens == 0 is a no-op (pointers may then be NULL).

@@ -80,8 +80,9 @@ struct Span {
 };
 
 // Cosine and sine of position * turns / 2^64 turns.  The product modulo 2^64 drops whole
-// turns exactly, so that far positions are as exact as near ones: what is left is known
-// to 2^-33 turns, and of that the nearest quarter is taken off as a whole number.  On an
+// turns exactly (the frequency's rounding to 2^-64 turns is all that grows with the
+// position): what is left is known to 2^-33 turns, and of that the nearest quarter is taken
+// off as a whole number.  On an
 // eighth of a turn either way (|t| <= pi/4) the power series up to t^9 and t^10 are off
 // by less than 2^-28.
 __device__ __forceinline__ void angle(int64_t position, uint64_t turns, float &c, float &s) {
