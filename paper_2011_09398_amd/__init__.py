@@ -1297,7 +1297,7 @@ def kv8_attention(cache: KV8Cache, q, table, q_start, lengths, *, scale: Optiona
     slope times the distance off them; prefix int32 [seqs] is the number of a sequence's
     first tokens that all its rows see (causal).  max_q and max_len, the most new tokens
     and the longest length, help to split the work.  Returns out, or (out, lse float32
-    [tokens, q_heads])."""
+    [tokens, q_heads]); autograd does not follow them."""
     try:
         tokens, heads, dim = q.shape
         seqs, width = table.shape
@@ -1405,6 +1405,7 @@ class Rotary:
         self._interleaved = int(self.interleaved)
         # what every call compares its tensors with
         self._int64, self._empty_like = torch.int64, torch.empty_like
+        self._is_grad_enabled = torch.is_grad_enabled
         self._types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -1447,12 +1448,54 @@ def _rotary_out(t, out, name):
     return out
 
 
+_recorded_rotary = None
+
+
+def _rotary_recorded(plan, positions, q, k, backward, out):
+    """rotary() of tensors that autograd follows: the gradients of a turn are the turn back."""
+    global _recorded_rotary
+    import torch
+    if out is not None:
+        raise ValueError("out does not go with tensors that require a gradient: leave it away, or "
+                         "call under torch.no_grad()")
+    # (a captured backward pass beside an eager one of the same leaves can end the process)
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("rotary of tensors that require a gradient is not captured: call it "
+                           "under torch.no_grad(), and with backward=True for gradients")
+    if _recorded_rotary is None:
+        class Recorded(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, plan, backward, positions, q, k):
+                ctx.plan, ctx.turned_back = plan, backward
+                ctx.save_for_backward(positions)
+                ctx.set_materialize_grads(False)
+                return rotary(plan, positions, q, k, backward=backward)
+
+            @staticmethod
+            def backward(ctx, *grads):
+                positions, = ctx.saved_tensors
+                # (sums' gradients are views of one number)
+                there = [i for i, g in enumerate(grads) if g is not None and ctx.needs_input_grad[3 + i]]
+                xs = [grads[i] if grads[i].stride(2) == 1 else grads[i].contiguous() for i in there]
+                out = [None, None]
+                if xs:
+                    ys = rotary(ctx.plan, positions, *xs, backward=not ctx.turned_back)
+                    for i, y in zip(there, ys if len(xs) == 2 else (ys,)):
+                        out[i] = y
+                return (None, None, None, *out)
+
+        _recorded_rotary = Recorded
+    return _recorded_rotary.apply(plan, bool(backward), positions, q, k)
+
+
 def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=None):
     """q [tokens, q_heads, head_dim], and k [tokens, kv_heads, head_dim] unless it is None,
     turned to `positions` (int64 [tokens]) in one launch (lce_rotary): float32, float16 or
     bfloat16, any token and head strides.  backward: q and k are gradients of what was
     turned, and get turned back (and scaled) to those of what went in.  Returns new
-    tensors, or writes `out` (q's, or a pair), which may be q and k themselves."""
+    tensors, or writes `out` (q's, or a pair), which may be q and k themselves.  Autograd
+    follows q and k where they require a gradient and there is no `out` (which is then
+    refused, as is a call that is being captured into a graph)."""
     try:
         n, heads, dim = q.shape
         x = q.stride()
@@ -1474,6 +1517,8 @@ def rotary(plan: Rotary, positions, q, k=None, *, backward: bool = False, out=No
             shape, y = k.shape, k.stride()
     if (n | heads) >> 31 or k is not None and shape[1] >> 31:
         _int32_refused(tokens=n, heads=heads if k is None else max(heads, shape[1]))
+    if (q.requires_grad or k is not None and k.requires_grad) and plan._is_grad_enabled():
+        return _rotary_recorded(plan, positions, q, k, backward, out)
     if out is None:
         first = plan._empty_like(q)
         second = None if k is None else plan._empty_like(k)

@@ -32,3 +32,96 @@ def test_far_positions_of_ordinary_frequencies(base, interleaved):
         bound = (2.0 ** -21 + far) * size + 2.0 ** -24 * np.abs(want[..., part])
         off = np.abs(got[..., part] - want[..., part]) - bound
         assert off.max() <= 0, (off.max(), np.argwhere(off > 0)[:4].tolist())
+
+
+def tensors(seed, n, heads, dim, dtype):
+    rng = np.random.default_rng(seed)
+    return [torch.from_numpy(rng.standard_normal((n, h, dim))).to(ref.DTYPES[dtype]).cuda()
+            for h in heads]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("backward", [False, True])
+def test_autograd_follows_queries_and_keys(dtype, interleaved, backward):
+    plan = lce.Rotary(96, rot_dim=64, interleaved=interleaved, scaling="yarn", factor=4.0)
+    at = torch.arange(7, 300, 9).cuda()
+    n = len(at)
+    q, k, gq, gk = tensors(2, n, (5, 2, 5, 2), 96, dtype)
+    q.requires_grad_()
+    k.requires_grad_()
+    want = lce.rotary(plan, at, q.detach(), k.detach(), backward=backward)
+    got = lce.rotary(plan, at, q, k, backward=backward)
+    assert all(torch.equal(a, b) and b.requires_grad for a, b in zip(want, got))
+    torch.autograd.backward(got, (gq, gk))
+    back = lce.rotary(plan, at, gq, gk, backward=not backward)
+    assert torch.equal(q.grad, back[0]) and torch.equal(k.grad, back[1])
+    # against the formula: angles and products to 2^-21 of a pair's size, and one rounding
+    half = (slice(0, 64, 2), slice(1, 64, 2)) if interleaved else (slice(0, 32), slice(32, 64))
+    for g, grad in ((gq, q.grad), (gk, k.grad)):
+        g, grad = g.cpu().double().numpy(), grad.cpu().double().numpy()
+        exact = ref.rotary(g, at.cpu().numpy(), plan.freqs.numpy(), plan.scale, interleaved,
+                           not backward)
+        bound = ref.HALF_ULP[dtype] * 1.01 * np.abs(exact) + (2.0 ** -25 if dtype == "f16" else 0)
+        size = 2.0 ** -21 * np.hypot(g[..., half[0]], g[..., half[1]]) * plan.scale
+        for part in half:
+            bound[..., part] += size
+        assert (np.abs(grad - exact) <= bound).all()
+
+
+def test_autograd_of_one_tensor_of_one_gradient_and_of_gradients():
+    plan = lce.Rotary(64)
+    at = torch.arange(11).cuda()
+    q, k, g = tensors(3, 11, (4, 4, 4), 64, "f32")
+    x = q.clone().requires_grad_()
+    y = lce.rotary(plan, at, x)
+    y.sum().backward()                             # a gradient that is a view of one number
+    assert torch.equal(x.grad, lce.rotary(plan, at, torch.ones_like(q), backward=True))
+    # keys alone are used, or alone require a gradient
+    for need in ((True, True), (False, True)):
+        a, b = q.clone().requires_grad_(need[0]), k.clone().requires_grad_(need[1])
+        (lce.rotary(plan, at, a, b)[1] * g).sum().backward()
+        assert a.grad is None and torch.equal(b.grad, lce.rotary(plan, at, g, backward=True))
+    # one tensor twice, heads that share one
+    a = q[:, :1].clone().requires_grad_()
+    u, w = lce.rotary(plan, at, a.expand(11, 4, 64), a)
+    ((u * g).sum() + (w * g[:, :1]).sum()).backward()
+    all_heads = torch.cat((g, g[:, :1]), 1)
+    want = lce.rotary(plan, at, all_heads, backward=True).double().sum(1, keepdim=True)
+    # five products, each rounded to float32, and sums of them
+    assert (a.grad.double() - want).abs().max() <= 10 * 2.0 ** -24 * 5 * 8
+    # of a gradient: the turn again
+    x, d = q.clone().requires_grad_(), g.clone().requires_grad_()
+    grad, = torch.autograd.grad(lce.rotary(plan, at, x), x, d, create_graph=True)
+    again, = torch.autograd.grad(grad, d, k)
+    assert torch.equal(again, lce.rotary(plan, at, k))
+
+
+def test_autograd_needs_what_it_saved():
+    plan = lce.Rotary(64)
+    at = torch.arange(3).cuda()
+    x = tensors(4, 3, (2,), 64, "f32")[0].requires_grad_()
+    y = lce.rotary(plan, at, x)
+    at += 1
+    with pytest.raises(RuntimeError):              # the positions are others now
+        y.sum().backward()
+
+
+def test_what_autograd_cannot_follow_is_refused(monkeypatch):
+    plan = lce.Rotary(64)
+    at = torch.arange(3).cuda()
+    q, k = (t.requires_grad_() for t in tensors(5, 3, (2, 1), 64, "bf16"))
+    plain = q.detach()
+    for args, out in (((q,), torch.empty_like(plain)), ((plain, k), (plain, torch.empty_like(k)))):
+        before = plain.clone()
+        with pytest.raises(ValueError):
+            lce.rotary(plan, at, *args, out=out)
+        assert torch.equal(plain, before)
+        with torch.no_grad():
+            lce.rotary(plan, at, *args, out=out)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError):
+        lce.rotary(plan, at, q)
+    with torch.no_grad():
+        assert not lce.rotary(plan, at, q).requires_grad
+    assert not lce.rotary(plan, at, q.detach()).requires_grad
