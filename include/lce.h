@@ -701,7 +701,8 @@ typedef struct {
 /* Heads of one tensor, read from x and written to y: channels contiguous, strides in
  * elements.  y may be x (with the same strides); other overlaps are not allowed.  Rows of
  * y do not lie between each other: its smaller stride is head_dim or more, its larger one
- * all that the rows of the other axis take, or more. */
+ * all that the rows of the other axis take, or more.  Of two tensors, neither's y overlaps
+ * the other's x or y. */
 typedef struct {
     int32_t heads;         /* >= 1                                                     */
     const void *x;

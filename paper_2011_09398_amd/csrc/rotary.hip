@@ -361,8 +361,12 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const uint64_t *turns, const 
         return fail(LCE_EUNSUPPORTED, "%d tokens of %lld heads: too many for one call", d.tokens,
                     (long long)heads);
     if (const lce_status st = validate_apart(q, "q", d.tokens, d.head_dim)) return st;
-    if (k)
+    if (k) {
         if (const lce_status st = validate_apart(k, "k", d.tokens, d.head_dim)) return st;
+        // either's results would be written over the other's, or over what it still reads
+        if (q->y == k->y || q->y == k->x || k->y == q->x)
+            return fail(LCE_EINVAL, "q and k: y of one is x or y of the other");
+    }
     const dim3 grid((unsigned)groups);
     if (d.type == LCE_FLOAT32)
         n > 1 ? launch<float, 4>(p, grid, stream) : launch<float, 1>(p, grid, stream);

@@ -41,3 +41,24 @@ def test_yarn_by_the_number_of_turns(rot, base, original, factor):
     assert np.allclose(ratio[turns * step < 1], factor, rtol=1e-13)
     assert (ratio >= 1 - 1e-13).all() and (ratio <= factor * (1 + 1e-13)).all()
     assert (np.diff(ratio) >= -1e-13).all()
+
+
+def rows(**kw):
+    return lce.RotaryRows(**{**dict(heads=4, x=P, y=P, x_token_stride=256, x_head_stride=64,
+                                    y_token_stride=256, y_head_stride=64), **kw})
+
+
+def call(q, k=None, **kw):
+    d = lce.RotaryDesc(**{**dict(tokens=3, head_dim=64, rot_dim=64, type=2, interleaved=0, backward=0,
+                                 scale=1.0), **kw})
+    return lce.lib().lce_rotary(ctypes.byref(d), P, P, ctypes.byref(q),
+                                ctypes.byref(k) if k is not None else None, None)
+
+
+def test_queries_and_keys_in_one_place_are_refused():
+    """Results of one where the other's are written or are still to be read."""
+    far = 1 << 20
+    for q, k in ((rows(y=far), rows(y=far)), (rows(), rows()), (rows(x=P, y=far), rows(x=far, y=P)),
+                 (rows(y=far), rows(x=far, y=2 * far)), (rows(x=far, y=2 * far), rows(y=far))):
+        assert call(q, k) == lce.LCE_EINVAL
+        assert "q and k" in lce.last_error()
