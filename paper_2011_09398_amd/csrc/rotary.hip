@@ -351,11 +351,12 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const uint64_t *turns, const 
     if (heads > 1 << 20) return fail(LCE_EUNSUPPORTED, "%lld heads: too many", (long long)heads);
     // threads that share a token's heads: as many as there are heads where the call is
     // short, fewer (and angles computed less often) once that is enough threads
-    const int64_t most = (int64_t)d.tokens * p.units * heads;
+    // (the product with all heads can pass 64 bits)
+    const int64_t each = (int64_t)d.tokens * p.units;
     int64_t lanes = heads;
-    while (lanes > 1 && most / heads * lanes > 256 * 2048) lanes = (lanes + 1) / 2;
+    while (lanes > 1 && each > 256 * 2048 / lanes) lanes = (lanes + 1) / 2;
     p.lanes = (int)lanes;
-    p.items = (int64_t)d.tokens * p.units * lanes;
+    p.items = each * lanes;
     const int64_t groups = (p.items + kThreads - 1) / kThreads;
     if (groups > (1 << 24) - 1)
         return fail(LCE_EUNSUPPORTED, "%d tokens of %lld heads: too many for one call", d.tokens,

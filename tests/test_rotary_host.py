@@ -62,3 +62,13 @@ def test_queries_and_keys_in_one_place_are_refused():
                  (rows(y=far), rows(x=far, y=2 * far)), (rows(x=far, y=2 * far), rows(y=far))):
         assert call(q, k) == lce.LCE_EINVAL
         assert "q and k" in lce.last_error()
+
+
+def test_counts_past_64_bits_are_refused():
+    """Tokens times heads times channels that an int64 does not hold."""
+    wide = dict(heads=1 << 20, y_head_stride=65536, y_token_stride=1 << 36)
+    for x in (P, P + 2):                           # 16 bytes at a time, and one channel
+        assert call(rows(x=x, y=1 << 30, **wide), tokens=2 ** 31 - 1, head_dim=65536,
+                    rot_dim=65536) == lce.LCE_EUNSUPPORTED
+    assert call(rows(x=P + 2, **{**wide, "heads": (1 << 20) - 1}), tokens=2 ** 30 + 12345,
+                head_dim=65536, rot_dim=65534) == lce.LCE_EUNSUPPORTED
