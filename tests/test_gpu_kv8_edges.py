@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2011_09398_amd as lce
+from tests import kv8_exact as exact
 from tests import kv8_util as ref
 
 pytestmark = pytest.mark.gpu
@@ -77,3 +78,86 @@ def test_an_infinity_in_a_query_makes_its_row_nan(dim, dtype, rows, opts):
     assert torch.isnan(out[bad]).all() and torch.isnan(lse[bad]).all()
     assert torch.equal(out[~bad], want[~bad]) and torch.equal(lse[~bad], want_lse[~bad])
     assert not out[41].any() and torch.isneginf(lse[41]).all()
+
+
+SLOPES = [0.5, 0.0, -0.01, 2.0, 0.1, 1.0, 0.01, 0.3]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+@pytest.mark.parametrize("opts", [
+    dict(slopes=SLOPES), dict(slopes=SLOPES, causal=False), dict(slopes=SLOPES, window=90),
+    dict(cap=5.0, slopes=SLOPES), dict(cap=1e6), dict(cap=1e6, slopes=SLOPES, causal=False),
+    dict(cap=5.0, slopes=SLOPES, prefix=[600, 2, 0, 70, 310])], ids=str)
+def test_every_change_of_scores_in_every_tile(dim, dtype, rows, opts):
+    """Biases by distance, far caps and both in tiles of each height and in calls of many rows,
+    over several pages, whole and split."""
+    batch = ref.Batch(dim + rows, [700, 130, 1, 64, 333], [40, 9, 1, 2, 33], 8, 2, dim, dtype, loud=3.0)
+    want = batch.attention(dim ** -0.5, **opts)
+    batch.attention = lambda *args, **kw: want     # the same for every split
+    for chunk in (0, 1, 3):
+        with lce.tuning(kv8_rows=rows, kv8_chunk=chunk):
+            check(batch, **opts)
+            name = lce.last_schedule()
+        assert name.startswith("kv8-16" if dim == 256 else f"kv8-{rows}")
+        assert chunk != 1 or name.endswith("-split")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("opts", [dict(), dict(cap=20.0), dict(slopes=SLOPES[:4]),
+                                  dict(cap=20.0, slopes=SLOPES[:4], window=200)], ids=str)
+def test_pages_that_go_past_the_caches(dim, dtype, opts):
+    """Calls whose table says that they read more than 240 MiB, of single tokens and of a few,
+    load pages past the caches; the same calls with a table as wide as their pages do not, and
+    give the same bits where they split the work alike."""
+    lengths = [0, 1, 15, 64, 130, 3000, 300, 65]
+    queries = [0, 1, 2, 1, 3, 1, 2, 1]
+    seqs, width = len(lengths), 20000
+    assert 128 * dim * width * seqs >= 240 << 20
+    batch = ref.Batch(dim, lengths, queries, 4, 2, dim, dtype, width=width)
+    out, lse = check(batch, **opts)
+    kw = dict(softcap=opts.get("cap", 0.0), window=opts.get("window", 0), return_lse=True)
+    if "slopes" in opts:
+        kw["slopes"] = torch.tensor(opts["slopes"]).cuda()
+    cache, q, table, start, lens = batch.device(lce)
+    # one workgroup a tile in both
+    wide, narrow = table, table[:, :-(-max(lengths) // ref.PAGE)].contiguous()
+    got = []
+    for t in (wide, narrow):
+        with lce.tuning(kv8_chunk=width // 2):
+            got.append(lce.kv8_attention(cache, q, t, start, lens, **kw))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("dtype,weights", [("bf16", 2.0 ** -14), ("f16", 2.0 ** -20)])
+@pytest.mark.parametrize("q_heads,kv_heads,dim", [(8, 2, 64), (7, 1, 128), (16, 2, 256)])
+@pytest.mark.parametrize("chunk", [0, 1])
+def test_weights_of_two_parts_where_results_are_small(q_heads, kv_heads, dim, dtype, weights, chunk):
+    """Exact scores, and values that nearly cancel: a weight rounded once would show."""
+    b = exact.batch(dim, [5, 30, 100], [1, 1, 1], q_heads, kv_heads, dim, dtype)
+    want, bound, _ = exact.expected(b, weights)
+    with lce.tuning(kv8_chunk=chunk):
+        out = lce.kv8_attention(*b.device(lce), scale=exact.SCALE).cpu().double().numpy()
+    off = np.abs(out - want) - bound
+    assert off.max() <= 0, (off.max(), np.argwhere(off > 0)[:5].tolist())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [16, 32, 128])
+def test_a_sequences_bits_do_not_depend_on_the_others(dtype, rows):
+    """A sequence alone and beside others, of longer and shorter lengths, with the same hints
+    and the same pages a workgroup."""
+    lengths, queries = [900, 70, 300, 5, 450], [4, 1, 40, 5, 1]
+    batch = ref.Batch(10, lengths, queries, 8, 2, 128, dtype)
+    cache, q, table, start, lens = batch.device(lce)
+    kw = dict(return_lse=True, max_q=40, max_len=900)
+    with lce.tuning(kv8_rows=rows, kv8_chunk=3):
+        out, lse = lce.kv8_attention(cache, q, table, start, lens, **kw)
+        for b, n in enumerate(queries):
+            at = slice(int(batch.start[b]), int(batch.start[b]) + n)
+            one, one_lse = lce.kv8_attention(cache, q[at], table[b:b + 1],
+                                             torch.tensor([0, n], dtype=torch.int32).cuda(),
+                                             lens[b:b + 1], **kw)
+            assert torch.equal(one, out[at]) and torch.equal(one_lse, lse[at]), b
