@@ -40,7 +40,7 @@ __device__ __forceinline__ float relative(int e, int of, int up) {
 template <typename E>
 __device__ __forceinline__ float score_factor(float scale_log2, int most) {
     const float f = __builtin_amdgcn_ldexpf(scale_log2, most - 127 - kUp<E>);
-    return bits_as<float>(clampi(bits_as<int>(f), 1, 0x7F7FFFFF));
+    return bits_as<float>(max(bits_as<uint32_t>(__builtin_fminf(f, __FLT_MAX__)), 1u));
 }
 
 // Two query channels of type E::T, infinities as NaNs: an infinity times a key is one or the
@@ -48,10 +48,13 @@ __device__ __forceinline__ float score_factor(float scale_log2, int most) {
 // makes its row one whatever it is multiplied by.
 template <typename E>
 __device__ __forceinline__ uint32_t without_infinities(uint32_t w) {
-    constexpr uint32_t exponents = __is_same(E, F16) ? 0x7C007C00u : 0x7F807F80u;
-    constexpr uint32_t one = __is_same(E, F16) ? 0x04000400u : 0x00800080u;
-    constexpr int quiet = __is_same(E, F16) ? 6 : 9;        // the mantissa's highest bit
-    return w | ((((w & exponents) + one) >> quiet) & (0x80008000u >> quiet));
+    if constexpr (__is_same(E, F16)) {
+        const f16x2 x = bits_as<f16x2>(w);
+        return bits_as<uint32_t>(__builtin_elementwise_fma(x, f16x2{0, 0}, x));
+    } else {
+        // exponents of all ones carry into the sign's place, from there to the quiet bit
+        return w | ((((w & 0x7F807F80u) + 0x00800080u) >> 9) & 0x00400040u);
+    }
 }
 
 // The scale bytes (byte i: block i) of a page of which some row sees tokens [lo, hi):
