@@ -598,7 +598,8 @@ typedef struct {
     int32_t causal;        /* 1: position p sees tokens j <= p, and a prefix; 0: all   */
     int32_t window;        /* > 0: only tokens j > p - window; 0: no such bound        */
     int32_t max_q;         /* hints for the split of the work, 0 = unknown: the most   */
-    int32_t max_len;       /* new tokens, the longest length.  Wrong ones cost speed.  */
+    int32_t max_len;       /* new tokens, the longest length.  Wrong ones cost speed
+                              (and max_q says how weights are rounded: see below)      */
     float scale;           /* of the scores, finite and > 0                            */
     float softcap;         /* 0: none, or what scores are capped at, 1e-30 .. 1e30     */
     int64_t q_token_stride, q_head_stride;   /* elements, multiples of 8               */
@@ -624,13 +625,19 @@ lce_status lce_kv8_workspace_size(const lce_kv8_cache_desc *desc, const lce_kv8_
  * with k and v as the cache holds them.  Token j is visible where j <= p or j <
  * prefix[b] (causal) or anywhere in the sequence (not causal), and j > p - window where
  * there is a window.  Sums, scores, the running maximum and the running sum are
- * float32; softmax weights are rounded to `type` where they multiply the values, or, where
- * max_q (0: the mean) new tokens make up to 8 rows of a cache head, split into two of that
- * type (float16: with a last place of at most 2^-31 of a row's largest weight), and out is
- * rounded to it once (float16: what is past 65504 to that).  With LCE_FLOAT16, keys are
- * multiplied as multiples of 2^-32 times the largest scale of their page, or of less,
- * values as multiples of 2^-32 times the largest scale that a row's sequence has: this
- * rounds only what is under a scale 2^-22 times as large.
+ * float32, and out is rounded to `type` once (float16: what is past 65504 to that).
+ * Softmax weights are rounded to `type` where they multiply the values (float16: with a last
+ * place of at most 2^-31 of a row's largest weight).  Where max_q (0: the mean number of) new
+ * tokens make up to 64 rows of a cache head, results are divided by the sum of the rounded
+ * weights; and of a sequence's rows of a cache head (its tokens times the query heads that
+ * share it, in that order) the last ones, if they are up to 8 more than a multiple of 16,
+ * have weights of two parts of `type`, which is next to float32 ones.  A row's bits may so
+ * depend on how many rows its sequence has and on max_q, as on the split of the work.
+ * With LCE_FLOAT16, keys are multiplied as multiples of 2^-32 times the largest scale of
+ * their page, or of less, values as multiples of 2^-32 times the largest scale that a row's
+ * sequence has: this rounds only what is under a scale 2^-22 times as large.  With
+ * LCE_BFLOAT16 the same holds of 2^-126, and products are summed in float32 before their
+ * scales are multiplied in: queries of 2^111 and more may pass its range.
  * A row that sees nothing is 0 with lse -infinity.
  *   q       [tokens][q_heads][head_dim] of query->type (device, 16-byte aligned)
  *   table   int32 [seqs][table_width]  (device): a row's pages; entries past a

@@ -108,7 +108,10 @@ int64_t query_rows(const lce_kv8_cache_desc &d, const lce_kv8_query_desc &q) {
 // rows alone, and their waves share the pages.  Heads of 64 channels have half the products
 // for the same softmax, which the smaller tiles' third wave a SIMD does better, until there
 // are many tiles.  Heads of 256 channels stay at 16: 32 rows of them, or 128, have more state
-// than registers.  Measured in graphs (us, tiles of 16 / 32 / 128; 32 heads on 8 if not said
+// than the registers of two waves a SIMD (one wave a SIMD is not tried).  The rule is short and
+// not the least of every line: 16 sequences of 64 new tokens take 32 rows, for 15 to 31 % more
+// time than 16, and the last line's prompts of 128 channels 128 rows, for 8 to 26 % more than
+// 32.  Measured in graphs (us, tiles of 16 / 32 / 128; 32 heads on 8 if not said
 // otherwise; the last two columns float16):
 //                                          128 channels      64 channels      128, capped
 //   16 of 4064 tokens, 64 of them new      48 / 55 / 99      29 / 38 / 80     54 / 65 / 130

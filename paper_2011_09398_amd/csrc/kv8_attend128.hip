@@ -122,10 +122,11 @@ __device__ __forceinline__ void lds_barrier() {
 // pipe in 0.59 (counters of the first case).  With two waves a SIMD the sum hardly passes 1:
 // a matrix instruction holds up about six vector ones, measured alone (32x32x16 products
 // with 8, 12 and 16 independent fused multiply-adds each: 21, 28 and 33 ns, 15 without).
-// Measured, bfloat16, 32 heads on 8 of 128 channels: 4096 tokens seeing 8192, 550 us, 999
-// TFLOP/s; 4 sequences of up to 2048 new tokens on up to 16384, causal, 616 us, 998 TFLOP/s
-// of visible pairs (a large library product: 1170 to 1390); of up to 1700 on up to 6500, of
-// which one has 85 % of the work, 192 us, 930 TFLOP/s.
+// Measured, bfloat16, 32 heads on 8 of 128 channels: 4096 tokens seeing 8192, 550 to 558 us,
+// 985 to 999 TFLOP/s; 4 sequences of up to 2048 new tokens on up to 16384, causal, 887 to 998
+// TFLOP/s of visible pairs, by how alike their lengths are (a large library product: 1170 to
+// 1390); of up to 1700 on up to 6500, of which one has 85 % of the work, 196 to 204 us, 875
+// to 910 TFLOP/s, by the card.
 template <typename E, int D, Change CHANGE>
 __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) {
     __shared__ Page<D> pages[2];
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend128_kernel(AttendParams p) 
         for (int k = 1; k < 16; ++k) high = fmaxf(high, s[t][k]);
         high = __builtin_fmaf(high, by, offset);
         // (of large maxima, the difference is exact where a sum is not; each row goes by
-        // its own maximum, so that no bit of it depends on the rows beside it)
+        // its own maximum, so that no bit of it depends on what the rows beside it hold)
         if (__builtin_amdgcn_ballot_w64(high - top > kLag + E::kLift)) {
             add(t ^ 1);
             w[2 * (t ^ 1)] = w[2 * (t ^ 1) + 1] = u32x4{0, 0, 0, 0};

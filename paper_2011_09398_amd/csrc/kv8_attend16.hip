@@ -182,7 +182,8 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
     top = __builtin_fmaf(top, c, offset);
     // (Of large maxima, the difference is exact where a sum is not.  Each row goes by
-    // its own maximum, so that no bit of it depends on the rows beside it.)
+    // its own maximum, so that no bit of it depends on what the rows beside it hold; how
+    // many they are does count, by `paired`.)
     if (__builtin_amdgcn_ballot_w64(top - st.m > kLag + E::kLift)) {
         const float high = across_rows(top, [](float a, float b) { return fmaxf(a, b); });
         const float all = high - st.m > kLag + E::kLift ? high - kUnder<E, FEW> : st.m;
@@ -253,7 +254,7 @@ __device__ __forceinline__ void weigh(RowState<D> &st, f32x4 (&s)[kTiles], u32x4
 //
 // Bound by memory where a call reads much: 48 sequences of up to 8192 tokens, 32 heads of
 // 128 on 8, bfloat16 (265 MB) 60 us, 4.4 TB/s with the launch (a large copy 4.8 to 5.4, by
-// the card); 24 of up to 4001, 32 heads of 64 on 32 with a bias (170 MB) 37 us; 16 with 4
+// the card); 24 of up to 4001, 32 heads of 64 on 32 with a bias (170 MB) 36 us; 16 with 4
 // drafted tokens and a window of 4096, 16 heads of 256 on 8, float16, capped (191 MB) 44 us.
 // By latencies in a row (launch, lengths, table, a page, the states out, the ticket, the
 // states in) where it does not: one of 30011, 32 heads of 128 on 8 (61 MB) 18 us.  A page
